@@ -53,7 +53,8 @@ enum {
   MOE_ENOTPLANNED = -7 /* moe_run / moe_combine on a slot with no moe_plan               */
 };
 
-enum { MOE_DTYPE_BF16 = 0, MOE_DTYPE_FP8_E4M3 = 1 };
+/* fp16 and fp32: of rows that are sorted, merged or quantised; a context computes in the first two */
+enum { MOE_DTYPE_BF16 = 0, MOE_DTYPE_FP8_E4M3 = 1, MOE_DTYPE_FP16 = 2, MOE_DTYPE_FP32 = 3 };
 enum { MOE_CLASS_DECODE = 0, MOE_CLASS_PREFILL = 1 };
 /* How an op's activations are laid out (Section 2.4).  GATHERED: x is [T, H] in token order and the
  * plan packs the routed rows per expert (the contiguous layout).  MASKED: x already sits in per-expert
@@ -275,6 +276,73 @@ int moe_plan_static(const int32_t* topk_ids, int32_t n_tokens, int32_t top_k, in
  * <= n_experts, else MOE_EINVAL.  Logits must be finite. */
 int moe_route(const float* logits, int32_t n_tokens, int32_t n_experts, int32_t top_k,
               int32_t* topk_ids, float* topk_w, void* stream);
+
+/* The router's gradient: from d_topk_w [T, k], the gradient of the router weights of moe_route, to that of the logits,
+ *     d_logits[t, e] = sum_{j: topk_ids[t,j] = e} w_j (dw_j - sum_i w_i dw_i),   0 for an expert that was not chosen
+ * (the weights are a softmax over the chosen logits).  Every entry of d_logits [T, E] fp32 is written.  A slot whose id is
+ * outside [0, n_experts) is left out of both sums.  Limits as for moe_route. */
+int moe_route_grad(const int32_t* topk_ids, const float* topk_w, const float* d_topk_w, int32_t n_tokens,
+                   int32_t n_experts, int32_t top_k, float* d_logits, void* stream);
+
+/* Rows sorted by expert and put together again, for experts that the caller computes (in training, or with other weights than
+ * moe_run knows), and the gradients of both.  R = n_tokens * top_k; sorted_to_flat and flat_to_sorted [R] are the permutation
+ * that moe_plan or moe_plan_static wrote (inverses of one another), topk_w [T, k] the router weights:
+ *   moe_sort_rows        xs[flat_to_sorted[t*k+j], :] = x[t, :]
+ *   moe_sort_rows_grad   dx[t, :] = sum_j dxs[flat_to_sorted[t*k+j], :]
+ *   moe_merge_rows       y[t, :] = sum_j topk_w[t,j] rows[flat_to_sorted[t*k+j], :]
+ *   moe_merge_rows_grad  drows[flat_to_sorted[t*k+j], :] = topk_w[t,j] dy[t, :],
+ *                        d_topk_w[t,j] = <dy[t, :], rows[flat_to_sorted[t*k+j], :]>
+ * No context, no workspace; all pointers are device pointers of the current device.
+ *   - dtype: MOE_DTYPE_BF16, FP16 or FP32, of all row arguments of a call; moe_sort_rows, which computes nothing, takes
+ *     MOE_DTYPE_FP8_E4M3 too (the scales of such rows are fp32 rows of hidden/128 columns: another call).  Sums are fp32 in slot
+ *     order, rounded once; a call's result does not depend on the schedule.
+ *   - *_stride: elements from a row to the next of that input, at least `hidden`; outputs are contiguous [R or T, hidden].
+ *     hidden >= 1, any; rows that are 16-byte aligned (addresses, strides and hidden) take the fast path.
+ *   - a slot whose entry of flat_to_sorted is outside [0, R) -- a rejected expert id -- has no row: it contributes nothing and its
+ *     d_topk_w is 0.  A row whose entry of sorted_to_flat is outside [0, R) belongs to no token: xs and drows are 0 there.
+ *     moe_plan_static leaves the entries of rejected ids as it finds them: preset both arrays to -1 where ids may be rejected.
+ *   - inputs and outputs must not overlap.  top_k <= 32, R < 2^27, else MOE_EINVAL; n_tokens = 0 does nothing. */
+int moe_sort_rows(const void* x, int64_t x_stride, int32_t dtype, int32_t n_tokens, int32_t top_k, int32_t hidden,
+                  const int32_t* sorted_to_flat, const int32_t* flat_to_sorted, void* xs, void* stream);
+int moe_sort_rows_grad(const void* dxs, int64_t dxs_stride, int32_t dtype, int32_t n_tokens, int32_t top_k, int32_t hidden,
+                       const int32_t* flat_to_sorted, void* dx, void* stream);
+int moe_merge_rows(const void* rows, int64_t rows_stride, int32_t dtype, const float* topk_w, int32_t n_tokens,
+                   int32_t top_k, int32_t hidden, const int32_t* flat_to_sorted, void* y, void* stream);
+int moe_merge_rows_grad(const void* dy, int64_t dy_stride, const void* rows, int64_t rows_stride, int32_t dtype,
+                        const float* topk_w, int32_t n_tokens, int32_t top_k, int32_t hidden,
+                        const int32_t* sorted_to_flat, const int32_t* flat_to_sorted, void* drows, float* d_topk_w,
+                        void* stream);
+
+/* Microscaled 4-bit rows (OCP MX): e2m1 codes, two to a byte with the even column in the low half, and a scale byte per 32
+ * neighbouring columns, the exponent of a power of two plus 127.  [rows, cols] values are codes [rows, cols/2] and scales
+ * [rows, cols/32].  The scale of a block is 2^(floor(log2 amax) - 2), at least 2^-127; values are rounded to nearest, ties to the
+ * even code, magnitudes above 6 scales to 6.  A block that holds NaN or infinity has scale byte 255: all of it is NaN (its codes
+ * say nothing).
+ *
+ * moe_mx_quantize: x [T, cols] -> codes and scales.  With sorted_to_flat and flat_to_sorted the result is sorted by expert
+ * as in moe_sort_rows: [T*k, cols/2] and [T*k, cols/32], zero where a row belongs to no token.  With both NULL (top_k = 1) row t
+ * of x is row t of the result: expert weights [E, n, cols] are quantised as E*n rows.  dtype BF16, FP16 or FP32; cols a multiple
+ * of 32; codes 4-byte aligned.
+ * moe_mx_dequantize: the values that codes and scales stand for, rounded to dtype; values 16-byte aligned. */
+int moe_mx_quantize(const void* x, int64_t x_stride, int32_t dtype, int32_t n_tokens, int32_t top_k, int32_t cols,
+                    const int32_t* sorted_to_flat, const int32_t* flat_to_sorted, void* codes, void* scales, void* stream);
+int moe_mx_dequantize(const void* codes, const void* scales, int64_t n_rows, int32_t cols, int32_t dtype, void* values,
+                      void* stream);
+
+/* Sorted 4-bit rows times the experts' 4-bit matrices: rows [R, K], weights [E, n, K] (K contiguous), offsets [E+1] as moe_plan
+ * wrote them (rows offsets[e] .. offsets[e+1]-1 are expert e's; offsets must not decrease).  One dense matrix is E = 1.
+ *   moe_mx_product  out[p, :] = rows[p, :] . w[e]^T, bf16 [R, n_cols], fp32 accumulation, one rounding
+ *   moe_mx_swiglu   weights [E, 2*inter, K], gate rows first: silu(gate) * up, computed in fp32 and quantised as by
+ *                   moe_mx_quantize: codes [R, inter/2], scales [R, inter/32], the rows of the down product
+ * The experts of a layer: moe_mx_quantize (sorting) -> moe_mx_swiglu -> moe_mx_product -> moe_merge_rows.
+ * Rows that belong to no expert (before offsets[0], from offsets[E] on) are 0.  k_cols a multiple of 128, inter one of 32, n_cols >= 1,
+ * R < 2^27, E <= 1024; codes and w_codes 16-byte aligned, scales and w_scales 4-byte aligned, else MOE_EINVAL.  No context, no
+ * workspace.  Waits inside the kernel are bounded (2 s); what a launch that gave up has not computed is NaN. */
+int moe_mx_product(const void* codes, const void* scales, const void* w_codes, const void* w_scales, const int32_t* offsets,
+                   int32_t n_rows, int32_t n_experts, int32_t n_cols, int32_t k_cols, void* out, void* stream);
+int moe_mx_swiglu(const void* codes, const void* scales, const void* w_codes, const void* w_scales, const int32_t* offsets,
+                  int32_t n_rows, int32_t n_experts, int32_t inter, int32_t k_cols, void* out_codes, void* out_scales,
+                  void* stream);
 
 /* Multiprocessor count of the context's device (the default persistent grid). */
 int moe_sm_count(moe_ctx_t* ctx);

@@ -22,7 +22,7 @@ LIB_PATH = os.path.join(_HERE, "libmoe_apk.so")
 
 MOE_OK, MOE_EINVAL, MOE_ENOSPC, MOE_ECUDA = 0, -1, -2, -3
 MOE_ETIMEOUT, MOE_EBADID, MOE_EBOUNDS, MOE_ENOTPLANNED = -4, -5, -6, -7
-MOE_DTYPE_BF16, MOE_DTYPE_FP8_E4M3 = 0, 1
+MOE_DTYPE_BF16, MOE_DTYPE_FP8_E4M3, MOE_DTYPE_FP16, MOE_DTYPE_FP32 = 0, 1, 2, 3
 MOE_CLASS_DECODE, MOE_CLASS_PREFILL = 0, 1
 MOE_LAYOUT_GATHERED, MOE_LAYOUT_MASKED = 0, 1
 MOE_TILE_M = 128
@@ -30,7 +30,9 @@ MOE_TILE_M = 128
 EXPORTS = ("moe_workspace_bytes", "moe_create", "moe_destroy", "moe_plan", "moe_run",
            "moe_combine", "moe_set_budget", "moe_set_budget_scaled", "moe_get_budget", "moe_status", "moe_footprint",
            "moe_read_tile_table", "moe_read_tile_log", "moe_sm_count", "moe_ctas_per_tile", "moe_strerror",
-           "moe_plan_static", "moe_route", "moe_run_plain", "moe_plan_pair")
+           "moe_plan_static", "moe_route", "moe_run_plain", "moe_plan_pair", "moe_route_grad", "moe_sort_rows",
+           "moe_sort_rows_grad", "moe_merge_rows", "moe_merge_rows_grad", "moe_mx_quantize", "moe_mx_dequantize",
+           "moe_mx_product", "moe_mx_swiglu")
 MOE_PLAN_STATIC_MAX_ROWS, MOE_PLAN_STATIC_MAX_EXPERTS = 32768, 256
 
 
@@ -101,6 +103,16 @@ def lib() -> C.CDLL:
         L.moe_read_tile_log.argtypes = [vp, vp, C.c_int, C.POINTER(C.c_int)]
         L.moe_plan_static.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, vp]
         L.moe_route.argtypes = [vp, i32, i32, i32, vp, vp, vp]
+        i64 = C.c_int64
+        L.moe_route_grad.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp]
+        L.moe_sort_rows.argtypes = [vp, i64, i32, i32, i32, i32, vp, vp, vp, vp]
+        L.moe_sort_rows_grad.argtypes = [vp, i64, i32, i32, i32, i32, vp, vp, vp]
+        L.moe_merge_rows.argtypes = [vp, i64, i32, vp, i32, i32, i32, vp, vp, vp]
+        L.moe_merge_rows_grad.argtypes = [vp, i64, vp, i64, i32, vp, i32, i32, i32, vp, vp, vp, vp, vp]
+        L.moe_mx_quantize.argtypes = [vp, i64, i32, i32, i32, i32, vp, vp, vp, vp, vp]
+        L.moe_mx_dequantize.argtypes = [vp, vp, i64, i32, i32, vp, vp]
+        L.moe_mx_product.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp]
+        L.moe_mx_swiglu.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp]
         L.moe_sm_count.argtypes = [vp]
         L.moe_ctas_per_tile.argtypes = [vp]
         L.moe_strerror.argtypes = [C.c_int]
@@ -430,3 +442,16 @@ class Context:
     @property
     def ctas_per_tile(self) -> int:
         return moe_ctas_per_tile(self.ctx)
+
+
+_IN_ROWS = ("sort_rows", "sort_rows_grad", "merge_rows", "merge_rows_grad", "route_grad", "mx_quantize", "mx_dequantize", "mx_product",
+            "mx_swiglu")
+
+
+def __getattr__(name):
+    """The calls on tensors of rows.py, which needs torch: loaded by the first that is asked for."""
+    if name not in _IN_ROWS:
+        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    from . import rows
+    globals().update((n, getattr(rows, n)) for n in _IN_ROWS)
+    return globals()[name]

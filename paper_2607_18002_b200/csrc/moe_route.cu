@@ -81,7 +81,58 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_kernel(const float* __
   }
 }
 
+// moe_route_grad: the gradient of the router weights carried on to the logits.  w = softmax over the chosen k logits, so
+//     dz[t, e] = sum_{j: ids[t,j] = e} w_j (dw_j - sum_i w_i dw_i),   0 for an expert that was not chosen.
+// One warp per token, lane j has slot j; the row is written as zeros and the chosen entries over them by the same warp, in that order.  Bound by
+// the T*E*4 bytes that it writes.
+__global__ void __launch_bounds__(kRouteWarps * 32) route_grad_kernel(const int* __restrict__ ids, const float* __restrict__ w,
+                                                                      const float* __restrict__ dw, int T, int E, int k, bool vec,
+                                                                      float* __restrict__ dz) {
+  const int lane = threadIdx.x & 31;
+  const int t = blockIdx.x * kRouteWarps + (threadIdx.x >> 5);
+  grid_dep_wait();
+  if (t >= T) return;
+  float* row = dz + (size_t)t * E;
+  const int id = lane < k ? ids[(size_t)t * k + lane] : -1;
+  const bool on = (unsigned)id < (unsigned)E;
+  const float wj = on ? w[(size_t)t * k + lane] : 0.f, dj = on ? dw[(size_t)t * k + lane] : 0.f;
+  if (vec)
+    for (int e = 4 * lane; e < E; e += 128) *reinterpret_cast<float4*>(row + e) = make_float4(0.f, 0.f, 0.f, 0.f);
+  else
+    for (int e = lane; e < E; e += 32) row[e] = 0.f;
+  float mean = wj * dj;
+#pragma unroll
+  for (int b = 16; b >= 1; b >>= 1) mean += __shfl_xor_sync(0xffffffffu, mean, b);
+  float mine = wj * (dj - mean);
+  // an expert that the token names more than once: its first slot adds the others up, in order
+  const unsigned same = __match_any_sync(0xffffffffu, on ? id : -1 - lane);
+  const bool first = (same & ((1u << lane) - 1u)) == 0;
+  if (__any_sync(0xffffffffu, !first)) {
+    float sum = 0.f;
+    for (int j = 0; j < k; ++j) {
+      const float v = __shfl_sync(0xffffffffu, mine, j);
+      if (same >> j & 1) sum += v;
+    }
+    mine = sum;
+  }
+  __syncwarp();
+  if (on && first) row[id] = mine;
+}
+
 }  // namespace moe
+
+extern "C" int moe_route_grad(const int32_t* topk_ids, const float* topk_w, const float* d_topk_w, int32_t n_tokens, int32_t n_experts,
+                              int32_t top_k, float* d_logits, void* stream) {
+  using namespace moe;
+  if (n_tokens < 0 || n_experts < 1 || n_experts > kRouteMaxE || top_k < 1 || top_k > 32 || top_k > n_experts)
+    return MOE_EINVAL;
+  if (n_tokens == 0) return MOE_OK;
+  if (!topk_ids || !topk_w || !d_topk_w || !d_logits) return MOE_EINVAL;
+  const int blocks = (n_tokens + kRouteWarps - 1) / kRouteWarps;
+  const bool vec = n_experts % 4 == 0 && (reinterpret_cast<uintptr_t>(d_logits) & 15) == 0;
+  return launch_after(route_grad_kernel, blocks, kRouteWarps * 32, 0, static_cast<cudaStream_t>(stream), topk_ids, topk_w, d_topk_w, n_tokens,
+                      n_experts, top_k, vec, d_logits) == cudaSuccess ? MOE_OK : MOE_ECUDA;
+}
 
 extern "C" int moe_route(const float* logits, int32_t n_tokens, int32_t n_experts, int32_t top_k,
                          int32_t* topk_ids, float* topk_w, void* stream) {

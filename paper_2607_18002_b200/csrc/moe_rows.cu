@@ -1,0 +1,344 @@
+// moe_sort_rows / moe_merge_rows and their gradients: the rows of a batch laid out by expert and put together again, on the
+// permutation that a plan left (flat_to_sorted and its inverse sorted_to_flat, R = T*k entries each).
+//
+//   sort        xs[f2s[t*k+j], :] = x[t, :]                  merge        y[t, :] = sum_j w[t,j] rows[f2s[t*k+j], :]
+//   sort grad   dx[t, :] = sum_j dxs[f2s[t*k+j], :]          merge grad   drows[f2s[t*k+j], :] = w[t,j] dy[t, :]
+//                                                                         dw[t,j] = <dy[t, :], rows[f2s[t*k+j], :]>
+//
+// All four are bound by memory: the R rows cross HBM once, and so do the T rows, because every kernel walks tokens: a token's row is
+// read once and written (or added up) for all of its k slots.  Walking sorted rows instead reads a token's row k times, far apart
+// in time, and a prefill chunk does not stay in L2 that long.  Sums are fp32 in slot order, rounded once; there are no
+// atomics, so results do not depend on the schedule.  Addresses are 64 bits wide.  An entry of f2s outside [0, R) names no row: nothing is read
+// or written for it; a row whose entry of s2f is outside [0, R) belongs to no token and is set to zero where rows are the output.
+#include <cuda_fp16.h>
+
+#include "moe_dev.cuh"
+
+namespace moe {
+namespace {
+
+constexpr int kRowThreads = 256;
+
+// kBytes of memory at a time: the widest that the row length, the strides and the addresses divide into
+template <int kBytes> struct Unit;
+template <> struct Unit<16> { using type = uint4; static __device__ uint4 zero() { return make_uint4(0u, 0u, 0u, 0u); } };
+template <> struct Unit<8> { using type = uint2; static __device__ uint2 zero() { return make_uint2(0u, 0u); } };
+template <> struct Unit<4> { using type = unsigned; static __device__ unsigned zero() { return 0u; } };
+template <> struct Unit<2> { using type = unsigned short; static __device__ unsigned short zero() { return 0; } };
+template <> struct Unit<1> { using type = unsigned char; static __device__ unsigned char zero() { return 0; } };
+
+// Columns of one token's row for a thread: `tpt` threads share a token (a power of two), a block holds kRowThreads / tpt tokens and one of
+// `slices` parts of their columns.
+struct Walk {
+  int tpt_log2, slices;
+};
+Walk walk_of(long long units, int per_thread) {
+  Walk w{3, 1};
+  while ((1 << w.tpt_log2) < kRowThreads && (long long)per_thread << w.tpt_log2 < units) ++w.tpt_log2;
+  w.slices = (int)((units + ((long long)per_thread << w.tpt_log2) - 1) / ((long long)per_thread << w.tpt_log2));
+  return w;
+}
+long long blocks_of(const Walk& w, int T) {
+  const int tokens = kRowThreads >> w.tpt_log2;
+  return ((long long)T + tokens - 1) / tokens * w.slices;
+}
+__device__ __forceinline__ int my_token(const Walk& w) {
+  return (int)(blockIdx.x / (unsigned)w.slices) * (kRowThreads >> w.tpt_log2) + (int)(threadIdx.x >> w.tpt_log2);
+}
+__device__ __forceinline__ int my_column(const Walk& w, int per_thread) {
+  return (int)(blockIdx.x % (unsigned)w.slices) * (per_thread << w.tpt_log2) + (int)(threadIdx.x & ((1u << w.tpt_log2) - 1));
+}
+
+// ------------------------------------------------------------------ sort
+template <int kBytes, int kPer>
+__global__ void __launch_bounds__(kRowThreads)
+sort_rows_kernel(const typename Unit<kBytes>::type* __restrict__ x, long long x_stride, typename Unit<kBytes>::type* __restrict__ xs,
+                 const int* __restrict__ s2f, const int* __restrict__ f2s, int T, int k, int units, Walk walk) {
+  grid_dep_wait();
+  const int t = my_token(walk), c0 = my_column(walk, kPer), step = 1 << walk.tpt_log2;
+  if (t >= T) return;
+  const unsigned R = (unsigned)T * (unsigned)k;
+  typename Unit<kBytes>::type v[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+    if (c0 + i * step < units) v[i] = x[t * x_stride + c0 + i * step];
+  const int* mine = f2s + (size_t)t * k;
+  const int* rows = s2f + (size_t)t * k;      // every row of the result is some token's to look after
+#pragma unroll 4
+  for (int j = 0; j < k; ++j) {
+    const unsigned p = (unsigned)mine[j];
+    if (p < R) {
+      typename Unit<kBytes>::type* to = xs + (size_t)p * units + c0;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+        if (c0 + i * step < units) to[i * step] = v[i];
+    }
+    if ((unsigned)rows[j] >= R) {
+      typename Unit<kBytes>::type* to = xs + ((size_t)t * k + j) * units + c0;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+        if (c0 + i * step < units) to[i * step] = Unit<kBytes>::zero();
+    }
+  }
+}
+
+// ------------------------------------------------------------------ elements
+template <class E> __device__ __forceinline__ float to_float(E v);
+template <> __device__ __forceinline__ float to_float(float v) { return v; }
+template <> __device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+template <> __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <class E> __device__ __forceinline__ E from_float(float v);
+template <> __device__ __forceinline__ float from_float(float v) { return v; }
+template <> __device__ __forceinline__ __half from_float(float v) { return __float2half_rn(v); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float(float v) { return __float2bfloat16_rn(v); }
+
+// kV neighbouring elements: one 16-byte access, or a single element where rows are not 16-byte aligned
+template <class E, int kV>
+struct __align__(sizeof(E) * kV) Pack {
+  E e[kV];
+};
+
+// ------------------------------------------------------------------ merge, and the gradient of sort (kWeights = false)
+// A thread owns kV columns of a token and has the rows of eight slots in flight.
+template <class E, int kV, bool kWeights>
+__global__ void __launch_bounds__(kRowThreads)
+merge_rows_kernel(const E* __restrict__ rows, long long stride, const float* __restrict__ w, const int* __restrict__ f2s,
+                  E* __restrict__ y, int T, int k, int H, Walk walk) {
+  grid_dep_wait();
+  using P = Pack<E, kV>;
+  const int t = my_token(walk), c = my_column(walk, 1) * kV;
+  if (t >= T || c >= H) return;
+  const unsigned R = (unsigned)T * (unsigned)k;
+  float acc[kV];
+#pragma unroll
+  for (int i = 0; i < kV; ++i) acc[i] = 0.f;
+  for (int j0 = 0; j0 < k; j0 += 8) {
+    P d[8];
+    float wj[8];
+    bool on[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int j = j0 + i;
+      const unsigned p = j < k ? (unsigned)f2s[(size_t)t * k + j] : R;
+      on[i] = p < R;
+      wj[i] = 1.f;
+      if (kWeights && on[i]) wj[i] = w[(size_t)t * k + j];
+      if (on[i]) d[i] = *reinterpret_cast<const P*>(rows + p * stride + c);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (on[i]) {
+#pragma unroll
+        for (int n = 0; n < kV; ++n) acc[n] = kWeights ? fmaf(wj[i], to_float(d[i].e[n]), acc[n]) : acc[n] + to_float(d[i].e[n]);
+      }
+  }
+  P out;
+#pragma unroll
+  for (int n = 0; n < kV; ++n) out.e[n] = from_float<E>(acc[n]);
+  *reinterpret_cast<P*>(y + (size_t)t * H + c) = out;
+}
+
+// ------------------------------------------------------------------ gradient of merge
+// A block owns a token: its threads share the columns, every one of them keeps the partial dot products of eight slots, and the block adds
+// them up in a fixed order.  dy is read once for eight slots, each row of `rows` once, each row of drows written once.
+constexpr int kGradMaxThreads = 256;
+template <class E, int kV>
+__global__ void __launch_bounds__(kGradMaxThreads)
+merge_grad_kernel(const E* __restrict__ dy, long long dy_stride, const E* __restrict__ rows, long long stride, const float* __restrict__ w,
+                  const int* __restrict__ s2f, const int* __restrict__ f2s, E* __restrict__ drows, float* __restrict__ dw, int k, int H) {
+  grid_dep_wait();
+  using P = Pack<E, kV>;
+  __shared__ float part[kGradMaxThreads / 32][8];
+  const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_warps = blockDim.x >> 5;
+  const unsigned R = gridDim.x * (unsigned)k;
+  for (int j0 = 0; j0 < k; j0 += 8) {
+    unsigned p[8];
+    float wj[8], dot[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int j = j0 + i;
+      p[i] = j < k ? (unsigned)f2s[(size_t)t * k + j] : R;
+      wj[i] = p[i] < R ? w[(size_t)t * k + j] : 0.f;
+      dot[i] = 0.f;
+    }
+    for (int c = tid * kV; c < H; c += blockDim.x * kV) {
+      const P g = *reinterpret_cast<const P*>(dy + t * dy_stride + c);
+      P d[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (p[i] < R) d[i] = *reinterpret_cast<const P*>(rows + p[i] * stride + c);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (p[i] < R) {
+          P out;
+#pragma unroll
+          for (int n = 0; n < kV; ++n) {
+            const float gn = to_float(g.e[n]);
+            dot[i] = fmaf(gn, to_float(d[i].e[n]), dot[i]);
+            out.e[n] = from_float<E>(wj[i] * gn);
+          }
+          *reinterpret_cast<P*>(drows + (size_t)p[i] * H + c) = out;
+        }
+    }
+    // eight sums over 32 lanes: lanes halve the set of slots that they keep while they add, nine exchanges instead of forty
+#pragma unroll
+    for (int s = 4, b = 16; s >= 1; s >>= 1, b >>= 1) {
+      const bool high = lane & b;
+#pragma unroll
+      for (int i = 0; i < s; ++i) {
+        const float give = high ? dot[i] : dot[i + s], keep = high ? dot[i + s] : dot[i];
+        dot[i] = keep + __shfl_xor_sync(0xffffffffu, give, b);
+      }
+    }
+    dot[0] += __shfl_xor_sync(0xffffffffu, dot[0], 2);
+    dot[0] += __shfl_xor_sync(0xffffffffu, dot[0], 1);
+    if (j0) __syncthreads();                          // the sums of the eight slots before have been read
+    if ((lane & 3) == 0) part[warp][lane >> 2] = dot[0];
+    __syncthreads();
+    if (tid < 8 && j0 + tid < k) {
+      float sum = 0.f;
+      for (int i = 0; i < n_warps; ++i) sum += part[i][tid];
+      dw[(size_t)t * k + j0 + tid] = sum;             // 0 for a slot that names no row
+    }
+  }
+  for (int j = 0; j < k; ++j)                         // rows that belong to no token
+    if ((unsigned)s2f[(size_t)t * k + j] >= R) {
+      P zero;
+#pragma unroll
+      for (int n = 0; n < kV; ++n) zero.e[n] = from_float<E>(0.f);
+      for (int c = tid * kV; c < H; c += blockDim.x * kV) *reinterpret_cast<P*>(drows + ((size_t)t * k + j) * H + c) = zero;
+    }
+}
+
+// ------------------------------------------------------------------ host
+int element_bytes(int dtype) {
+  return dtype == MOE_DTYPE_FP32 ? 4 : dtype == MOE_DTYPE_BF16 || dtype == MOE_DTYPE_FP16 ? 2 : dtype == MOE_DTYPE_FP8_E4M3 ? 1 : 0;
+}
+// sizes shared by the four calls; MOE_OK with *empty set where there is nothing to do
+int check_sizes(int T, int k, int H, int dtype, bool bytes_ok, bool* empty) {
+  if (T < 0 || k < 1 || k > 32 || H < 1) return MOE_EINVAL;
+  if (!element_bytes(dtype) || (dtype == MOE_DTYPE_FP8_E4M3 && !bytes_ok)) return MOE_EINVAL;
+  if ((long long)T * k >= (1ll << kRowSlotShift)) return MOE_EINVAL;        // as in a context
+  *empty = T == 0;
+  return MOE_OK;
+}
+bool element_aligned(int) { return true; }
+template <class... More>
+bool element_aligned(int el, const void* p, More... more) {
+  return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(el - 1)) == 0 && element_aligned(el, more...);
+}
+// widest access (16, 8, 4, 2 or 1 bytes) that divides all of these
+int widest(unsigned long long all) {
+  int b = 16;
+  while (all & (unsigned long long)(b - 1)) b >>= 1;
+  return b;
+}
+unsigned long long bits(const void* p) { return reinterpret_cast<uintptr_t>(p); }
+
+template <int kBytes>
+cudaError_t sort_launch(const void* x, long long x_stride_bytes, void* xs, const int* s2f, const int* f2s, int T, int k, long long row_bytes,
+                        cudaStream_t stream) {
+  using U = typename Unit<kBytes>::type;
+  const long long units = row_bytes / kBytes;
+  // Four accesses a thread where there are rows enough to fill the GPU, else one: shorter chains and more SMs at work.
+  const bool few = (long long)T * units < 148ll * 2048 * 4;
+  const Walk w = walk_of(units, few ? 1 : 4);
+  const long long blocks = blocks_of(w, T);
+  if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
+  return launch_after(few ? sort_rows_kernel<kBytes, 1> : sort_rows_kernel<kBytes, 4>, (int)blocks, kRowThreads, 0, stream, static_cast<const U*>(x),
+                      x_stride_bytes / kBytes, static_cast<U*>(xs), s2f, f2s, T, k, (int)units, w);
+}
+
+template <class E, bool kWeights>
+cudaError_t merge_launch(const void* rows, long long stride, const float* w, const int* f2s, void* y, int T, int k, int H, cudaStream_t stream) {
+  constexpr int kV = 16 / sizeof(E);
+  const bool wide = widest(bits(rows) | bits(y) | (unsigned long long)stride * sizeof(E) | (unsigned long long)H * sizeof(E)) == 16;
+  const Walk walk = walk_of(wide ? H / kV : H, 1);
+  const long long blocks = blocks_of(walk, T);
+  if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
+  return launch_after(wide ? merge_rows_kernel<E, kV, kWeights> : merge_rows_kernel<E, 1, kWeights>, (int)blocks, kRowThreads, 0, stream,
+                      static_cast<const E*>(rows), stride, w, f2s, static_cast<E*>(y), T, k, H, walk);
+}
+
+template <class E>
+cudaError_t grad_launch(const void* dy, long long dy_stride, const void* rows, long long stride, const float* w, const int* s2f, const int* f2s,
+                        void* drows, float* dw, int T, int k, int H, cudaStream_t stream) {
+  constexpr int kV = 16 / sizeof(E);
+  const bool wide = widest(bits(dy) | bits(rows) | bits(drows) | (unsigned long long)dy_stride * sizeof(E) |
+                           (unsigned long long)stride * sizeof(E) | (unsigned long long)H * sizeof(E)) == 16;
+  const int units = wide ? H / kV : H;
+  int threads = 32;
+  while (threads < kGradMaxThreads && threads < units) threads *= 2;
+  return launch_after(wide ? merge_grad_kernel<E, kV> : merge_grad_kernel<E, 1>, T, threads, 0, stream, static_cast<const E*>(dy), dy_stride,
+                      static_cast<const E*>(rows), stride, w, s2f, f2s, static_cast<E*>(drows), dw, k, H);
+}
+
+template <bool kWeights>
+int merge_any(const void* rows, int64_t stride, int dtype, const float* w, int T, int k, int H, const int* f2s, void* y, void* stream) {
+  bool empty = false;
+  const int rc = check_sizes(T, k, H, dtype, false, &empty);
+  if (rc || empty) return rc;
+  if (!rows || !f2s || !y || (kWeights && !w) || stride < H) return MOE_EINVAL;
+  if (!element_aligned(element_bytes(dtype), rows, y) || !element_aligned(4, w, f2s)) return MOE_EINVAL;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const cudaError_t e = dtype == MOE_DTYPE_FP32   ? merge_launch<float, kWeights>(rows, stride, w, f2s, y, T, k, H, st)
+                        : dtype == MOE_DTYPE_FP16 ? merge_launch<__half, kWeights>(rows, stride, w, f2s, y, T, k, H, st)
+                                                  : merge_launch<__nv_bfloat16, kWeights>(rows, stride, w, f2s, y, T, k, H, st);
+  return e == cudaSuccess ? MOE_OK : MOE_ECUDA;
+}
+
+}  // namespace
+}  // namespace moe
+
+extern "C" {
+
+int moe_sort_rows(const void* x, int64_t x_stride, int32_t dtype, int32_t n_tokens, int32_t top_k, int32_t hidden,
+                  const int32_t* sorted_to_flat, const int32_t* flat_to_sorted, void* xs, void* stream) {
+  using namespace moe;
+  bool empty = false;
+  const int rc = check_sizes(n_tokens, top_k, hidden, dtype, true, &empty);
+  if (rc || empty) return rc;
+  if (!x || !sorted_to_flat || !flat_to_sorted || !xs || x_stride < hidden) return MOE_EINVAL;
+  const int el = element_bytes(dtype);
+  if (!element_aligned(el, x, xs) || !element_aligned(4, sorted_to_flat, flat_to_sorted)) return MOE_EINVAL;
+  const long long row = (long long)hidden * el, step = x_stride * el;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaError_t e = cudaErrorInvalidValue;
+  switch (widest(bits(x) | bits(xs) | (unsigned long long)row | (unsigned long long)step)) {
+    case 16: e = sort_launch<16>(x, step, xs, sorted_to_flat, flat_to_sorted, n_tokens, top_k, row, st); break;
+    case 8: e = sort_launch<8>(x, step, xs, sorted_to_flat, flat_to_sorted, n_tokens, top_k, row, st); break;
+    case 4: e = sort_launch<4>(x, step, xs, sorted_to_flat, flat_to_sorted, n_tokens, top_k, row, st); break;
+    case 2: e = sort_launch<2>(x, step, xs, sorted_to_flat, flat_to_sorted, n_tokens, top_k, row, st); break;
+    default: e = sort_launch<1>(x, step, xs, sorted_to_flat, flat_to_sorted, n_tokens, top_k, row, st); break;
+  }
+  return e == cudaSuccess ? MOE_OK : MOE_ECUDA;
+}
+
+int moe_sort_rows_grad(const void* dxs, int64_t dxs_stride, int32_t dtype, int32_t n_tokens, int32_t top_k, int32_t hidden,
+                       const int32_t* flat_to_sorted, void* dx, void* stream) {
+  return moe::merge_any<false>(dxs, dxs_stride, dtype, nullptr, n_tokens, top_k, hidden, flat_to_sorted, dx, stream);
+}
+
+int moe_merge_rows(const void* rows, int64_t rows_stride, int32_t dtype, const float* topk_w, int32_t n_tokens, int32_t top_k,
+                   int32_t hidden, const int32_t* flat_to_sorted, void* y, void* stream) {
+  return moe::merge_any<true>(rows, rows_stride, dtype, topk_w, n_tokens, top_k, hidden, flat_to_sorted, y, stream);
+}
+
+int moe_merge_rows_grad(const void* dy, int64_t dy_stride, const void* rows, int64_t rows_stride, int32_t dtype, const float* topk_w,
+                        int32_t n_tokens, int32_t top_k, int32_t hidden, const int32_t* sorted_to_flat, const int32_t* flat_to_sorted,
+                        void* drows, float* d_topk_w, void* stream) {
+  using namespace moe;
+  bool empty = false;
+  const int rc = check_sizes(n_tokens, top_k, hidden, dtype, false, &empty);
+  if (rc || empty) return rc;
+  if (!dy || !rows || !topk_w || !sorted_to_flat || !flat_to_sorted || !drows || !d_topk_w || dy_stride < hidden || rows_stride < hidden)
+    return MOE_EINVAL;
+  if (!element_aligned(element_bytes(dtype), dy, rows, drows) || !element_aligned(4, topk_w, sorted_to_flat, flat_to_sorted, d_topk_w))
+    return MOE_EINVAL;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const auto launch = dtype == MOE_DTYPE_FP32 ? grad_launch<float> : dtype == MOE_DTYPE_FP16 ? grad_launch<__half> : grad_launch<__nv_bfloat16>;
+  const cudaError_t e = launch(dy, dy_stride, rows, rows_stride, topk_w, sorted_to_flat, flat_to_sorted, drows, d_topk_w, n_tokens, top_k, hidden, st);
+  return e == cudaSuccess ? MOE_OK : MOE_ECUDA;
+}
+
+}  // extern "C"

@@ -322,7 +322,7 @@ int moe_merge_rows_grad(const void* dy, int64_t dy_stride, const void* rows, int
  * moe_mx_quantize: x [T, cols] -> codes and scales.  With sorted_to_flat and flat_to_sorted the result is sorted by expert
  * as in moe_sort_rows: [T*k, cols/2] and [T*k, cols/32], zero where a row belongs to no token.  With both NULL (top_k = 1) row t
  * of x is row t of the result: expert weights [E, n, cols] are quantised as E*n rows.  dtype BF16, FP16 or FP32; cols a multiple
- * of 32; codes 4-byte aligned.
+ * of 32; codes 16-byte aligned; T * cols < 2^37.
  * moe_mx_dequantize: the values that codes and scales stand for, rounded to dtype; values 16-byte aligned. */
 int moe_mx_quantize(const void* x, int64_t x_stride, int32_t dtype, int32_t n_tokens, int32_t top_k, int32_t cols,
                     const int32_t* sorted_to_flat, const int32_t* flat_to_sorted, void* codes, void* scales, void* stream);

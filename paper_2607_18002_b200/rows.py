@@ -18,198 +18,212 @@ A permutation is the pair (sorted_to_flat, flat_to_sorted) of a plan, int32 [T*k
 """
 from __future__ import annotations
 
-import contextlib
-
 import torch
 
 import paper_2607_18002_b200 as moe
 
-_DTYPES = {torch.bfloat16: moe.MOE_DTYPE_BF16, torch.float16: moe.MOE_DTYPE_FP16, torch.float32: moe.MOE_DTYPE_FP32}
-_SORTED_DTYPES = {**_DTYPES, torch.float8_e4m3fn: moe.MOE_DTYPE_FP8_E4M3, torch.uint8: moe.MOE_DTYPE_FP8_E4M3}
+_BF16, _FP32, _I32, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
+_DTYPES = {_BF16: moe.MOE_DTYPE_BF16, torch.float16: moe.MOE_DTYPE_FP16, _FP32: moe.MOE_DTYPE_FP32}
+_SORTED_DTYPES = {**_DTYPES, torch.float8_e4m3fn: moe.MOE_DTYPE_FP8_E4M3, _U8: moe.MOE_DTYPE_FP8_E4M3}
+_Tensor = torch.Tensor
+_current_device = torch.cuda.current_device
+_stream = moe.Context._stream
 
 
 def _refuse(what):
     raise ValueError(what)
 
 
-def _rows(t, name, dtypes, device=None, dtype=None):
-    """[n, H] with neighbouring columns -> elements from a row to the next."""
-    if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.dtype not in dtypes or not t.is_cuda:
+def _rows(t, name, dtypes):
+    """[n, H] with neighbouring columns -> n, H, elements from a row to the next."""
+    if not isinstance(t, _Tensor) or t.dtype not in dtypes or not t.is_cuda or t.dim() != 2:
         _refuse(f"{name} must be a CUDA tensor [rows, columns] of one of {sorted(map(str, dtypes))}")
-    if (device is not None and t.device != device) or (dtype is not None and t.dtype != dtype):
-        _refuse(f"{name} must be on {device} with {dtype}, as the other rows")
     n, h = t.shape
-    if h < 1 or (t.stride(1) != 1 and h > 1) or (n > 1 and t.stride(0) < h):
+    step, one = t.stride()
+    if h < 1 or (one != 1 and h > 1) or (n > 1 and step < h):
         _refuse(f"{name}: the columns of a row must be neighbours and rows must not overlap")
-    return max(t.stride(0), h)
+    return n, h, step if step > h else h
 
 
 def _plain(t, name, dtype, shape, device):
     """A contiguous tensor of this type and shape."""
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or tuple(t.shape) != shape or t.device != device or not t.is_contiguous():
-        _refuse(f"{name} must be a contiguous {dtype} tensor {shape} on {device}")
+    if not isinstance(t, _Tensor) or t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        _refuse(f"{name} must be a contiguous {dtype} tensor {tuple(shape)} on {device}")
 
 
 def _index(t, name, n, device):
-    if not isinstance(t, torch.Tensor) or t.dtype != torch.int32 or t.dim() != 1 or t.device != device or not t.is_contiguous() \
+    if not isinstance(t, _Tensor) or t.dtype != _I32 or t.dim() != 1 or t.device != device or not t.is_contiguous() \
             or t.shape[0] != n and (n or t.shape[0] != 1):              # (a plan without rows has arrays of one entry)
         _refuse(f"{name} must be a contiguous int32 tensor [{n}] on {device}")
 
 
-@contextlib.contextmanager
-def _elsewhere(device, stream):
-    with torch.cuda.device(device):
-        if stream is None:
-            yield
-        else:
-            with torch.cuda.stream(stream):
-                yield
-
-
-_here = contextlib.nullcontext()
-
-
-def _on(device, stream):
-    """The device current and `stream` its current stream: outputs are allocated there and the kernel is enqueued there."""
-    if stream is None and device.index == torch.cuda.current_device():
-        return _here
+def _elsewhere(call, device, stream, *args):
+    """The same call with the device current and `stream` its current stream: outputs are allocated there and the kernel is enqueued there."""
     if stream is not None and stream.device != device:
         _refuse(f"the stream is on {stream.device}, the tensors are on {device}")
-    return _elsewhere(device, stream)
+    with torch.cuda.device(device), torch.cuda.stream(stream):          # (a stream of None changes nothing)
+        return call(*args)
 
 
-def _go(name, *args):
-    rc = getattr(moe._lib or moe.lib(), name)(*args, moe.Context._stream(None))
-    if rc:
-        raise moe.MoeError(rc, name)
+def _failed(rc, name):
+    raise moe.MoeError(rc, name)
 
 
 def sort_rows(x, sorted_to_flat, flat_to_sorted, top_k: int, stream=None):
     """x [T, H] -> [T*k, H], the tokens' rows by expert (bf16, fp16, fp32, or one-byte codes)."""
-    stride = _rows(x, "x", _SORTED_DTYPES)
-    (T, H), dev = x.shape, x.device
+    T, H, step = _rows(x, "x", _SORTED_DTYPES)
+    dev = x.device
+    if stream is not None or dev.index != _current_device():
+        return _elsewhere(sort_rows, dev, stream, x, sorted_to_flat, flat_to_sorted, top_k)
     _index(sorted_to_flat, "sorted_to_flat", T * top_k, dev)
     _index(flat_to_sorted, "flat_to_sorted", T * top_k, dev)
-    with _on(dev, stream):
-        xs = torch.empty((T * top_k, H), dtype=x.dtype, device=dev)
-        _go("moe_sort_rows", x.data_ptr(), stride, _SORTED_DTYPES[x.dtype], T, top_k, H, sorted_to_flat.data_ptr(),
-            flat_to_sorted.data_ptr(), xs.data_ptr())
+    xs = x.new_empty(T * top_k, H)
+    rc = (moe._lib or moe.lib()).moe_sort_rows(x.data_ptr(), step, _SORTED_DTYPES[x.dtype], T, top_k, H, sorted_to_flat.data_ptr(),
+                                               flat_to_sorted.data_ptr(), xs.data_ptr(), _stream(None))
+    if rc:
+        _failed(rc, "moe_sort_rows")
     return xs
 
 
 def sort_rows_grad(dxs, flat_to_sorted, top_k: int, stream=None):
     """dxs [T*k, H], the gradient of sort_rows' result -> that of x [T, H]."""
-    stride = _rows(dxs, "dxs", _DTYPES)
-    (R, H), dev = dxs.shape, dxs.device
+    R, H, step = _rows(dxs, "dxs", _DTYPES)
+    dev = dxs.device
+    if stream is not None or dev.index != _current_device():
+        return _elsewhere(sort_rows_grad, dev, stream, dxs, flat_to_sorted, top_k)
     if top_k < 1 or R % top_k:
         _refuse("dxs must have top_k rows for every token")
     _index(flat_to_sorted, "flat_to_sorted", R, dev)
-    with _on(dev, stream):
-        dx = torch.empty((R // top_k, H), dtype=dxs.dtype, device=dev)
-        _go("moe_sort_rows_grad", dxs.data_ptr(), stride, _DTYPES[dxs.dtype], R // top_k, top_k, H, flat_to_sorted.data_ptr(), dx.data_ptr())
+    T = R // top_k
+    dx = dxs.new_empty(T, H)
+    rc = (moe._lib or moe.lib()).moe_sort_rows_grad(dxs.data_ptr(), step, _DTYPES[dxs.dtype], T, top_k, H, flat_to_sorted.data_ptr(),
+                                                    dx.data_ptr(), _stream(None))
+    if rc:
+        _failed(rc, "moe_sort_rows_grad")
     return dx
 
 
 def _weights(topk_w, R, dev):
-    if not isinstance(topk_w, torch.Tensor) or topk_w.dim() != 2 or topk_w.numel() != R:
-        _refuse("topk_w must be fp32 [T, k], a weight for every row")
-    _plain(topk_w, "topk_w", torch.float32, tuple(topk_w.shape), dev)
+    if not isinstance(topk_w, _Tensor) or topk_w.dtype != _FP32 or topk_w.dim() != 2 or topk_w.numel() != R or topk_w.device != dev \
+            or not topk_w.is_contiguous():
+        _refuse(f"topk_w must be a contiguous fp32 tensor [T, k] on {dev}, a weight for each of the {R} rows")
     return topk_w.shape
 
 
 def merge_rows(rows, flat_to_sorted, topk_w, stream=None):
     """rows [T*k, H] by expert -> y [T, H], the tokens' rows added up with their router weights."""
-    stride = _rows(rows, "rows", _DTYPES)
-    (R, H), dev = rows.shape, rows.device
+    R, H, step = _rows(rows, "rows", _DTYPES)
+    dev = rows.device
+    if stream is not None or dev.index != _current_device():
+        return _elsewhere(merge_rows, dev, stream, rows, flat_to_sorted, topk_w)
     T, k = _weights(topk_w, R, dev)
     _index(flat_to_sorted, "flat_to_sorted", R, dev)
-    with _on(dev, stream):
-        y = torch.empty((T, H), dtype=rows.dtype, device=dev)
-        _go("moe_merge_rows", rows.data_ptr(), stride, _DTYPES[rows.dtype], topk_w.data_ptr(), T, k, H, flat_to_sorted.data_ptr(), y.data_ptr())
+    y = rows.new_empty(T, H)
+    rc = (moe._lib or moe.lib()).moe_merge_rows(rows.data_ptr(), step, _DTYPES[rows.dtype], topk_w.data_ptr(), T, k, H,
+                                                flat_to_sorted.data_ptr(), y.data_ptr(), _stream(None))
+    if rc:
+        _failed(rc, "moe_merge_rows")
     return y
 
 
 def merge_rows_grad(dy, rows, sorted_to_flat, flat_to_sorted, topk_w, stream=None):
     """dy [T, H], the gradient of merge_rows' result -> (that of rows [T*k, H], that of topk_w [T, k] fp32)."""
-    stride = _rows(rows, "rows", _DTYPES)
-    (R, H), dev = rows.shape, rows.device
-    dy_stride = _rows(dy, "dy", _DTYPES, dev, rows.dtype)
+    R, H, step = _rows(rows, "rows", _DTYPES)
+    dev = rows.device
+    if stream is not None or dev.index != _current_device():
+        return _elsewhere(merge_rows_grad, dev, stream, dy, rows, sorted_to_flat, flat_to_sorted, topk_w)
     T, k = _weights(topk_w, R, dev)
-    if tuple(dy.shape) != (T, H):
-        _refuse(f"dy must be [{T}, {H}]")
+    dT, dH, dy_step = _rows(dy, "dy", _DTYPES)
+    if dT != T or dH != H or dy.dtype != rows.dtype or dy.device != dev:
+        _refuse(f"dy must be a {rows.dtype} tensor [{T}, {H}] on {dev}")
     _index(sorted_to_flat, "sorted_to_flat", R, dev)
     _index(flat_to_sorted, "flat_to_sorted", R, dev)
-    with _on(dev, stream):
-        drows = torch.empty((R, H), dtype=rows.dtype, device=dev)
-        dw = torch.empty((T, k), dtype=torch.float32, device=dev)
-        _go("moe_merge_rows_grad", dy.data_ptr(), dy_stride, rows.data_ptr(), stride, _DTYPES[rows.dtype], topk_w.data_ptr(), T, k, H,
-            sorted_to_flat.data_ptr(), flat_to_sorted.data_ptr(), drows.data_ptr(), dw.data_ptr())
+    drows, dw = rows.new_empty(R, H), topk_w.new_empty(T, k)
+    rc = (moe._lib or moe.lib()).moe_merge_rows_grad(dy.data_ptr(), dy_step, rows.data_ptr(), step, _DTYPES[rows.dtype], topk_w.data_ptr(), T, k, H,
+                                                     sorted_to_flat.data_ptr(), flat_to_sorted.data_ptr(), drows.data_ptr(), dw.data_ptr(),
+                                                     _stream(None))
+    if rc:
+        _failed(rc, "moe_merge_rows_grad")
     return drows, dw
 
 
 def route_grad(topk_ids, topk_w, d_topk_w, n_experts: int, stream=None):
     """The gradient of route's weights, fp32 [T, k] -> that of the logits, fp32 [T, E]."""
-    if not isinstance(topk_ids, torch.Tensor) or not topk_ids.is_cuda or topk_ids.dim() != 2:
+    if not isinstance(topk_ids, _Tensor) or not topk_ids.is_cuda or topk_ids.dim() != 2:
         _refuse("topk_ids must be a CUDA int32 tensor [T, k]")
-    shape, dev = tuple(topk_ids.shape), topk_ids.device
-    _plain(topk_ids, "topk_ids", torch.int32, shape, dev)
-    _plain(topk_w, "topk_w", torch.float32, shape, dev)
-    _plain(d_topk_w, "d_topk_w", torch.float32, shape, dev)
-    with _on(dev, stream):
-        dz = torch.empty((shape[0], n_experts), dtype=torch.float32, device=dev)
-        _go("moe_route_grad", topk_ids.data_ptr(), topk_w.data_ptr(), d_topk_w.data_ptr(), shape[0], n_experts, shape[1], dz.data_ptr())
+    shape, dev = topk_ids.shape, topk_ids.device
+    if stream is not None or dev.index != _current_device():
+        return _elsewhere(route_grad, dev, stream, topk_ids, topk_w, d_topk_w, n_experts)
+    _plain(topk_ids, "topk_ids", _I32, shape, dev)
+    _plain(topk_w, "topk_w", _FP32, shape, dev)
+    _plain(d_topk_w, "d_topk_w", _FP32, shape, dev)
+    T, k = shape
+    dz = topk_w.new_empty(T, n_experts)
+    rc = (moe._lib or moe.lib()).moe_route_grad(topk_ids.data_ptr(), topk_w.data_ptr(), d_topk_w.data_ptr(), T, n_experts, k, dz.data_ptr(),
+                                                _stream(None))
+    if rc:
+        _failed(rc, "moe_route_grad")
     return dz
 
 
 def mx_quantize(x, sorted_to_flat=None, flat_to_sorted=None, top_k: int = 1, stream=None):
     """x [..., K] -> codes uint8 [..., K/2], scales uint8 [..., K/32]; with a permutation x [T, K] -> the T*k rows by expert."""
-    lead = None
-    if isinstance(x, torch.Tensor) and x.dim() > 2 and x.is_contiguous() and sorted_to_flat is None and flat_to_sorted is None:
-        lead, x = x.shape[:-1], x.view(-1, x.shape[-1])
-    stride = _rows(x, "x", _DTYPES)
-    (T, K), dev = x.shape, x.device
+    if isinstance(x, _Tensor) and x.dim() > 2 and x.is_contiguous() and sorted_to_flat is None and flat_to_sorted is None:
+        codes, scales = mx_quantize(x.view(-1, x.shape[-1]), None, None, top_k, stream)
+        return codes.view(*x.shape[:-1], -1), scales.view(*x.shape[:-1], -1)
+    T, K, step = _rows(x, "x", _DTYPES)
+    dev = x.device
+    if stream is not None or dev.index != _current_device():
+        return _elsewhere(mx_quantize, dev, stream, x, sorted_to_flat, flat_to_sorted, top_k)
     if K % 32:
         _refuse("x must have a multiple of 32 columns")
+    R = T * top_k
     s2f = f2s = None
     if sorted_to_flat is not None or flat_to_sorted is not None:
-        _index(sorted_to_flat, "sorted_to_flat", T * top_k, dev)
-        _index(flat_to_sorted, "flat_to_sorted", T * top_k, dev)
+        _index(sorted_to_flat, "sorted_to_flat", R, dev)
+        _index(flat_to_sorted, "flat_to_sorted", R, dev)
         s2f, f2s = sorted_to_flat.data_ptr(), flat_to_sorted.data_ptr()
     elif top_k != 1:
         _refuse("top_k needs a permutation")
-    with _on(dev, stream):
-        codes = torch.empty((T * top_k, K // 2), dtype=torch.uint8, device=dev)
-        scales = torch.empty((T * top_k, K // 32), dtype=torch.uint8, device=dev)
-        _go("moe_mx_quantize", x.data_ptr(), stride, _DTYPES[x.dtype], T, top_k, K, s2f, f2s, codes.data_ptr(), scales.data_ptr())
-    return (codes, scales) if lead is None else (codes.view(*lead, -1), scales.view(*lead, -1))
+    codes, scales = x.new_empty((R, K // 2), dtype=_U8), x.new_empty((R, K // 32), dtype=_U8)
+    rc = (moe._lib or moe.lib()).moe_mx_quantize(x.data_ptr(), step, _DTYPES[x.dtype], T, top_k, K, s2f, f2s, codes.data_ptr(),
+                                                 scales.data_ptr(), _stream(None))
+    if rc:
+        _failed(rc, "moe_mx_quantize")
+    return codes, scales
 
 
-def _mx(codes, scales, names, dims, device=None):
-    """codes [..., K/2] and scales [..., K/32] -> K."""
-    if not isinstance(codes, torch.Tensor) or codes.dtype != torch.uint8 or not codes.is_cuda or not codes.is_contiguous() \
-            or (dims and codes.dim() != dims) or codes.dim() < 1 or codes.shape[-1] % 16 or (device is not None and codes.device != device):
-        _refuse(f"{names[0]} must be a contiguous CUDA uint8 tensor of {dims or 'some'} dimensions, a multiple of 16 bytes wide")
-    _plain(scales, names[1], torch.uint8, (*codes.shape[:-1], codes.shape[-1] // 16), codes.device)
+def _codes(codes, scales, what, dims):
+    """Codes [..., K/2] and scales [..., K/32] of so many dimensions (0: any) -> K."""
+    if not isinstance(codes, _Tensor) or codes.dtype != _U8 or not codes.is_cuda or not codes.is_contiguous() \
+            or (codes.dim() != dims if dims else codes.dim() < 1) or codes.shape[-1] % 16 \
+            or not isinstance(scales, _Tensor) or scales.dtype != _U8 or scales.device != codes.device or not scales.is_contiguous() \
+            or scales.shape[:-1] != codes.shape[:-1] or scales.shape[-1] * 16 != codes.shape[-1]:
+        _refuse(f"the codes and scales of {what} must be contiguous uint8 tensors of {dims or 'some'} dimensions on one GPU, a scale for 16 bytes of codes")
     return codes.shape[-1] * 2
 
 
-def mx_dequantize(codes, scales, dtype=torch.bfloat16, stream=None):
+def mx_dequantize(codes, scales, dtype=_BF16, stream=None):
     """The values [..., K] that codes [..., K/2] with scales [..., K/32] stand for."""
     if dtype not in _DTYPES:
         _refuse(f"dtype must be one of {sorted(map(str, _DTYPES))}")
-    K = _mx(codes, scales, ("codes", "scales"), 0)
-    with _on(codes.device, stream):
-        out = torch.empty((*codes.shape[:-1], K), dtype=dtype, device=codes.device)
-        if K:
-            _go("moe_mx_dequantize", codes.data_ptr(), scales.data_ptr(), out.numel() // K, K, _DTYPES[dtype], out.data_ptr())
+    K = _codes(codes, scales, "the rows", 0)
+    dev = codes.device
+    if stream is not None or dev.index != _current_device():
+        return _elsewhere(mx_dequantize, dev, stream, codes, scales, dtype)
+    out = codes.new_empty((*codes.shape[:-1], K), dtype=dtype)
+    if K:
+        rc = (moe._lib or moe.lib()).moe_mx_dequantize(codes.data_ptr(), scales.data_ptr(), out.numel() // K, K, _DTYPES[dtype], out.data_ptr(),
+                                                       _stream(None))
+        if rc:
+            _failed(rc, "moe_mx_dequantize")
     return out
 
 
-def _operands(codes, scales, w_codes, w_scales, offsets):
-    K = _mx(codes, scales, ("codes", "scales"), 2)
-    dev = codes.device
-    if _mx(w_codes, w_scales, ("w_codes", "w_scales"), 3, dev) != K:
-        _refuse("w_codes must be as wide as codes")
+def _operands(codes, scales, w_codes, w_scales, offsets, dev):
+    K = _codes(codes, scales, "the rows", 2)
+    if _codes(w_codes, w_scales, "the weights", 3) != K or w_codes.device != dev:
+        _refuse(f"the weights must have {K} columns and be on {dev}, as the rows")
     E, n, _ = w_codes.shape
     _index(offsets, "offsets", E + 1, dev)
     return codes.shape[0], E, n, K
@@ -217,22 +231,29 @@ def _operands(codes, scales, w_codes, w_scales, offsets):
 
 def mx_product(codes, scales, w_codes, w_scales, offsets, stream=None):
     """Sorted 4-bit rows [R, K] times the experts' matrices [E, n, K] -> bf16 [R, n]."""
-    R, E, n, K = _operands(codes, scales, w_codes, w_scales, offsets)
-    with _on(codes.device, stream):
-        out = torch.empty((R, n), dtype=torch.bfloat16, device=codes.device)
-        _go("moe_mx_product", codes.data_ptr(), scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), offsets.data_ptr(), R, E, n, K,
-            out.data_ptr())
+    dev = getattr(codes, "device", None)
+    R, E, n, K = _operands(codes, scales, w_codes, w_scales, offsets, dev)
+    if stream is not None or dev.index != _current_device():
+        return _elsewhere(mx_product, dev, stream, codes, scales, w_codes, w_scales, offsets)
+    out = codes.new_empty((R, n), dtype=_BF16)
+    rc = (moe._lib or moe.lib()).moe_mx_product(codes.data_ptr(), scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), offsets.data_ptr(), R, E,
+                                                n, K, out.data_ptr(), _stream(None))
+    if rc:
+        _failed(rc, "moe_mx_product")
     return out
 
 
 def mx_swiglu(codes, scales, w_codes, w_scales, offsets, stream=None):
     """Sorted 4-bit rows [R, K] times gate and up matrices [E, 2 I, K], silu(gate) * up -> codes [R, I/2], scales [R, I/32]."""
-    R, E, n, K = _operands(codes, scales, w_codes, w_scales, offsets)
+    dev = getattr(codes, "device", None)
+    R, E, n, K = _operands(codes, scales, w_codes, w_scales, offsets, dev)
     if n % 64:
-        _refuse("w_codes must have gate and up rows, a multiple of 32 each")
-    with _on(codes.device, stream):
-        out = torch.empty((R, n // 4), dtype=torch.uint8, device=codes.device)
-        out_scales = torch.empty((R, n // 64), dtype=torch.uint8, device=codes.device)
-        _go("moe_mx_swiglu", codes.data_ptr(), scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), offsets.data_ptr(), R, E, n // 2, K,
-            out.data_ptr(), out_scales.data_ptr())
+        _refuse("the weights must have gate and up rows, a multiple of 32 each")
+    if stream is not None or dev.index != _current_device():
+        return _elsewhere(mx_swiglu, dev, stream, codes, scales, w_codes, w_scales, offsets)
+    out, out_scales = codes.new_empty(R, n // 4), codes.new_empty(R, n // 64)
+    rc = (moe._lib or moe.lib()).moe_mx_swiglu(codes.data_ptr(), scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), offsets.data_ptr(), R, E,
+                                               n // 2, K, out.data_ptr(), out_scales.data_ptr(), _stream(None))
+    if rc:
+        _failed(rc, "moe_mx_swiglu")
     return out, out_scales

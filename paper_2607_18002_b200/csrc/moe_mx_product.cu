@@ -11,8 +11,8 @@
 // neighbouring columns of a row at a time, and for swiglu those 32 are one block of the result, its largest magnitude one warp-wide maximum.
 //
 // One persistent CTA per SM walks the tiles (rows of an expert innermost: neighbours share a weight tile in L2).  Roles: one thread issues TMA
-// (a stage is 256 columns of K: 128-byte rows, swizzled), four warps bring the stage's scale bytes (4-byte cp.async into the 512-byte
-// form that tcgen05.cp copies to TMEM: 128 rows x 4 blocks), one thread copies them and issues the MMAs, eight warps are the epilogue.
+// (a stage is 256 columns of K: 128-byte rows, swizzled), two warps bring the stage's scale bytes through registers into the 512-byte
+// form that tcgen05.cp copies to TMEM (128 rows x 4 blocks), one thread copies them and issues the MMAs, eight warps are the epilogue.
 // Every wait is bounded; where one runs out the launch ends and what it has not computed is NaN.
 #include "moe_dev.cuh"
 #include "moe_mx.cuh"
@@ -21,14 +21,14 @@
 namespace moe {
 namespace {
 
-constexpr int kMxThreads = 448;                 // warps 0-7 epilogue, 8 TMA, 9 MMA, 10-13 scales
-constexpr int kTmaWarp = 8, kMmaWarp = 9, kScaleWarp = 10, kScaleThreads = 128;
+// Warps 0-7 epilogue, 8 TMA, 9 MMA, 10 and 11 scales.  Three warps a quarter of the SM leave a thread 168 registers, four would leave 128.
+constexpr int kMxThreads = 384;
+constexpr int kTmaWarp = 8, kMmaWarp = 9, kScaleWarp = 10, kScaleWarps = 2;
 constexpr int kStageK = 256;                    // columns of K in a stage
 constexpr int kGroupK = 128;                    // ... in one 512-byte block of scales (4 a row)
 constexpr int kHalfRows = 128;                  // weight rows of an accumulator
 constexpr int kScaleBlock = 512;
 constexpr int kBoxRows = 32;                    // rows of a TMA box of activations
-constexpr int kLandDelay = 2;                   // stages of scale copies in flight
 constexpr unsigned long long kWaitNs = 2000000000ull;
 
 struct MxShared {
@@ -50,11 +50,12 @@ struct Shape {
   static constexpr int kWBytes = 2 * kHalfRows * 128, kXBytes = kRows * 128;
   static constexpr int kStageBytes = kWBytes + kXBytes + kScaleBytes;
   static constexpr int kScaleCols = 2 * (2 + kRowBlocks) * 4;                 // TMEM columns of a stage's scales
+  static constexpr int kLate = kRows / 16 < 6 ? kRows / 16 : 6;               // groups of 16 columns that the epilogue takes to registers
   static constexpr int kAccBufs = kRows <= 96 ? 2 : 1;
   static constexpr int kScaleCol0 = kAccBufs * 2 * kRows;
   static constexpr int kFitSmem = (227 * 1024 - 1024 - (int)sizeof(MxShared)) / kStageBytes, kFitTmem = (512 - kScaleCol0) / kScaleCols;
   static constexpr int kStages = kFitSmem < kFitTmem ? kFitSmem : kFitTmem;
-  static_assert(kStages > kLandDelay, "a stage's scales arrive kLandDelay stages late");
+  static_assert(kStages >= 2, "stages");
   static_assert(kStages <= 8, "barriers");
   static_assert(kScaleCol0 + kStages * kScaleCols <= 512, "TMEM");
 };
@@ -128,6 +129,30 @@ __device__ __forceinline__ void tc_ld16(unsigned taddr, unsigned (&r)[16]) {
       : "memory");
 }
 
+// 16 bytes of a row's scales, `left` of which are there (the others are not used), by loads of vec bytes
+__device__ __forceinline__ uint4 load_scales(const unsigned char* p, int left, int vec) {
+  uint4 v = make_uint4(0u, 0u, 0u, 0u);
+  if (vec == 16) return __ldg(reinterpret_cast<const uint4*>(p));
+  if (vec == 8) {
+    const uint2 lo = __ldg(reinterpret_cast<const uint2*>(p));
+    v.x = lo.x;
+    v.y = lo.y;
+    if (left > 8) {
+      const uint2 hi = __ldg(reinterpret_cast<const uint2*>(p) + 1);
+      v.z = hi.x;
+      v.w = hi.y;
+    }
+    return v;
+  }
+  const unsigned* w = reinterpret_cast<const unsigned*>(p);
+  v.x = __ldg(w);
+  if (left > 4) v.y = __ldg(w + 1);
+  if (left > 8) v.z = __ldg(w + 2);
+  if (left > 12) v.w = __ldg(w + 3);
+  return v;
+}
+__device__ __forceinline__ void st_word(unsigned saddr, unsigned v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(saddr), "r"(v) : "memory"); }
+
 struct Tile {
   int expert, row0, rows, n0;    // n0: first weight row (swiglu: first gate row)
 };
@@ -143,6 +168,11 @@ __device__ __forceinline__ Tile tile_at(const MxShared& s, int E, int t, int n_s
   return Tile{lo, s.first_row[lo] + m * kRows, min(kRows, rows - m * kRows), n * n_step};
 }
 
+__device__ __forceinline__ float rcp_approx(float v) {      // to one step
+  float r;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
 // 8 x 8 four-bit values over eight neighbouring lanes: lane i gives value j of word i, gets value i of word j
 __device__ __forceinline__ unsigned transpose_nibbles(unsigned v, int lane) {
 #pragma unroll
@@ -167,7 +197,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
   if (tid == 0) {
     for (int i = 0; i < S::kStages; ++i) {
       mbar_init(&s.full[i], 1);
-      mbar_init(&s.landed[i], kScaleThreads / 32);
+      mbar_init(&s.landed[i], kScaleWarps);
       mbar_init(&s.empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -274,45 +304,79 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
     }
     __syncwarp();
   } else if (warp >= kScaleWarp) {
-    // Two lanes a row: one for each group of 128 columns of the stage.  The four bytes of row r go to 16 (r % 32) + 4 (r / 32 % 4) of the
-    // group's block for 128 rows.
-    const int me = tid - kScaleWarp * 32, g = me & 1, r0 = me >> 1;
-    const int per_row = a.K / kMxBlock;
-    unsigned n = 0;
-    const auto hand_over = [&](unsigned m) {
-      fence_async_proxy_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&s.landed[m % S::kStages]);
+    // A thread has two rows of every 128-row block, in the order that spreads a warp's stores over all banks: their four bytes of a group of
+    // 128 columns go to 16 (r % 32) + 4 (r / 32) of the group's block.  16 bytes of a row are two stages; those of the next two are on their
+    // way to registers meanwhile, whether or not their stages are free.
+    const int r0 = 32 * (lane & 3) + 8 * (warp - kScaleWarp) + (lane >> 2);      // and r0 + 16
+    const unsigned spot = (unsigned)(r0 & 31) * 16 + (unsigned)(r0 >> 5) * 4;
+    const int per_row = a.K / kMxBlock, n_pairs = (n_stages + 1) / 2;
+    const int vec = per_row % 16 == 0 ? 16 : per_row % 8 == 0 ? 8 : 4;
+    const bool vec_w = ((size_t)a.w_scales & (vec - 1)) == 0, vec_x = ((size_t)a.x_scales & (vec - 1)) == 0;
+    constexpr int kBlocks = 2 + S::kRowBlocks;
+    struct Pair {
+      uint4 b[kBlocks][2];
+      int stages;                // 1 or 2; 0: there is no more
     };
-    bool ok = true;
-    for (int t = blockIdx.x; t < n_tiles && ok; t += gridDim.x) {
-      const Tile at = tile_at<S::kRows>(s, a.E, t, kStep);
-      const unsigned char* w_row = a.w_scales + (size_t)at.expert * a.N * per_row;
-      for (int i = 0; i < n_stages; ++i, ++n) {
-        const unsigned slot = n % S::kStages, round = n / S::kStages;
-        if (round) ok = __all_sync(0xffffffffu, wait(&s.empty[slot], (round - 1) & 1, &s.dead));
-        if (!ok) break;
-        const unsigned sc = smem_u32(stages + slot * S::kStageBytes) + S::kWBytes + S::kXBytes + g * (2 + S::kRowBlocks) * kScaleBlock;
-        const int at_k = i * (kStageK / kMxBlock) + g * (kGroupK / kMxBlock);
-        if (at_k < per_row) {
-          // a weight row behind the last one: any other's scales (its products are not stored)
+    int t = blockIdx.x, pair = 0;
+    const unsigned char* from[kBlocks][2];
+    unsigned n = 0;
+    const auto fetch = [&](Pair& p) {
+      p.stages = 0;
+      if (t >= n_tiles) return;
+      if (pair == 0) {
+        const Tile at = tile_at<S::kRows>(s, a.E, t, kStep);
 #pragma unroll
-          for (int r = r0; r < 2 * kHalfRows; r += kScaleThreads / 2) {
-            const int row = kSwiglu ? min(at.n0 + (r & 127), a.I - 1) + (r >> 7) * a.I : min(at.n0 + r, a.N - 1);
-            cp_async_4(sc + (r >> 7) * kScaleBlock + (r & 31) * 16 + (r >> 5 & 3) * 4, w_row + (size_t)row * per_row + at_k);
+        for (int q = 0; q < 2; ++q) {
+          const int r = r0 + 16 * q;
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {    // a weight row behind the last one: any other's scales (its products are not stored)
+            const int row = kSwiglu ? min(at.n0 + r, a.I - 1) + b * a.I : min(at.n0 + b * kHalfRows + r, a.N - 1);
+            from[b][q] = a.w_scales + ((size_t)at.expert * a.N + row) * per_row;
           }
-          for (int r = r0; r < at.rows; r += kScaleThreads / 2)
-            cp_async_4(sc + (2 + (r >> 7)) * kScaleBlock + (r & 31) * 16 + (r >> 5 & 3) * 4, a.x_scales + (size_t)(at.row0 + r) * per_row + at_k);
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-        if (n >= kLandDelay) {
-          asm volatile("cp.async.wait_group %0;" ::"n"(kLandDelay) : "memory");
-          hand_over(n - kLandDelay);
+#pragma unroll
+          for (int b = 0; b < S::kRowBlocks; ++b) from[2 + b][q] = a.x_scales + (size_t)(at.row0 + min(b * 128 + r, at.rows - 1)) * per_row;
         }
       }
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) p.b[b][q] = load_scales(from[b][q] + pair * 16, per_row - pair * 16, (b < 2 ? vec_w : vec_x) ? vec : 4);
+      p.stages = min(2, n_stages - 2 * pair);
+      if (++pair == n_pairs) {
+        pair = 0;
+        t += gridDim.x;
+      }
+    };
+    const auto put = [&](const Pair& p) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (h >= p.stages) break;
+        const unsigned slot = n % S::kStages, round = n / S::kStages;
+        if (round && !__all_sync(0xffffffffu, wait(&s.empty[slot], (round - 1) & 1, &s.dead))) return false;
+        const unsigned to = smem_u32(stages + slot * S::kStageBytes) + S::kWBytes + S::kXBytes + spot;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            const uint4& v = p.b[b][q];
+            st_word(to + b * kScaleBlock + 256 * q, h ? v.z : v.x);
+            st_word(to + (kBlocks + b) * kScaleBlock + 256 * q, h ? v.w : v.y);
+          }
+        fence_async_proxy_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&s.landed[slot]);
+        ++n;
+      }
+      return true;
+    };
+    Pair even, odd;
+    fetch(even);
+    while (even.stages) {
+      fetch(odd);
+      if (!put(even) || !odd.stages) break;
+      fetch(even);
+      if (!put(odd)) break;
     }
-    cp_async_wait_all();
-    for (unsigned m = n > kLandDelay ? n - kLandDelay : 0; m < n; ++m) hand_over(m);
   } else {
     const int quad = warp & 3, half = warp >> 2;
     unsigned k = 0;
@@ -323,26 +387,43 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
       if (ok) ok = __all_sync(0xffffffffu, wait(&s.acc_full[buf], use & 1, &s.dead));
       tc_fence_after();
       const unsigned acc = tmem + buf * 2 * S::kRows + ((unsigned)quad << 21);      // this warp's 32 lanes
+      // The last columns of the accumulator go to registers all at once and are worked off after it has been handed back, while the next
+      // tile's MMAs run.
+      const auto hand_back = [&] {
+        tc_wait_ld();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&s.acc_empty[buf]);
+      };
+      const int groups = (at.rows + 15) / 16;
       if (!kSwiglu) {            // warps 0-3 have the first accumulator, 4-7 the second
+        const unsigned mine = acc + half * S::kRows;
         const int col = at.n0 + half * kHalfRows + quad * 32 + lane;
         __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + (size_t)at.row0 * a.N + col;
-        for (int c = 0; c < at.rows; c += 16) {
-          unsigned v[16];
-          tc_ld16(acc + half * S::kRows + c, v);
-          tc_wait_ld();
+        const auto store = [&](const unsigned (&v)[16], int c) {
 #pragma unroll
           for (int j = 0; j < 16; ++j)
             if (c + j < at.rows && col < a.N)
               out[(size_t)(c + j) * a.N] = __float2bfloat16_rn(ok ? __uint_as_float(v[j]) : __uint_as_float(0x7fffffffu));
+        };
+        const int direct = max(groups - S::kLate, 0);
+        for (int g = 0; g < direct; ++g) {
+          unsigned v[16];
+          tc_ld16(mine + 16 * g, v);
+          tc_wait_ld();
+          store(v, 16 * g);
         }
+        unsigned v[S::kLate][16];
+#pragma unroll
+        for (int i = 0; i < S::kLate; ++i)
+          if (direct + i < groups) tc_ld16(mine + 16 * (direct + i), v[i]);
+        hand_back();
+#pragma unroll
+        for (int i = 0; i < S::kLate; ++i)
+          if (direct + i < groups) store(v[i], 16 * (direct + i));
       } else {                   // warps 0-3 and 4-7 take turns at groups of 16 rows
         const int col = at.n0 + quad * 32, per_row = a.I / kMxBlock;
-        unsigned char* codes = static_cast<unsigned char*>(a.out);
-        for (int c = half * 16; c < at.rows; c += 32) {
-          unsigned gate[16], up[16];
-          tc_ld16(acc + c, gate);
-          tc_ld16(acc + S::kRows + c, up);
-          tc_wait_ld();
+        const auto store = [&](const unsigned (&gate)[16], const unsigned (&up)[16], int c) {
 #pragma unroll
           for (int j0 = 0; j0 < 16; j0 += 8) {
             unsigned word = 0u, mine = 0u;
@@ -352,11 +433,10 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
 #pragma unroll
               for (int i = 0; i < 2; ++i) {
                 const float gv = __uint_as_float(gate[j0 + j + i]), uv = __uint_as_float(up[j0 + j + i]);
-                float v = __fdividef(gv, 1.f + __expf(-gv)) * uv;
-                if (!ok) v = __uint_as_float(0x7fffffffu);
-                const unsigned byte = mx_scale_byte(__reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7fffffffu));
-                if ((lane & 7) == j + i) mine = byte;
-                q[i] = v * mx_inverse(byte);
+                const float v = gv * rcp_approx(1.f + __expf(-gv)) * uv;
+                const unsigned top = __reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7f800000u);
+                if ((lane & 7) == j + i) mine = top;
+                q[i] = v * __uint_as_float(min(0x80000000u - top, 0x7f000000u));     // 2^(127 - scale byte)
               }
               word |= mx_codes2(q[0], q[1]) << (4 * j);
             }
@@ -364,15 +444,32 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
             const int row = c + j0 + (lane & 7);
             if (row < at.rows && col < a.I) {
               const size_t p = (size_t)(at.row0 + row);
-              *reinterpret_cast<unsigned*>(codes + p * (a.I / 2) + col / 2 + (lane >> 3) * 4) = word;
-              if (lane < 8) a.out_scales[p * per_row + col / kMxBlock] = (unsigned char)mine;
+              *reinterpret_cast<unsigned*>(static_cast<unsigned char*>(a.out) + p * (a.I / 2) + col / 2 + (lane >> 3) * 4) = word;
+              if (lane < 8) a.out_scales[p * per_row + col / kMxBlock] = (unsigned char)(ok ? mx_scale_byte(mine) : 255u);
             }
           }
+        };
+        constexpr int kLate = (S::kLate + 1) / 2;
+        const int my_groups = (groups - half + 1) / 2, direct = max(my_groups - kLate, 0);
+        for (int g = 0; g < direct; ++g) {
+          unsigned gate[16], up[16];
+          tc_ld16(acc + 16 * (half + 2 * g), gate);
+          tc_ld16(acc + S::kRows + 16 * (half + 2 * g), up);
+          tc_wait_ld();
+          store(gate, up, 16 * (half + 2 * g));
         }
+        unsigned gate[kLate][16], up[kLate][16];
+#pragma unroll
+        for (int i = 0; i < kLate; ++i)
+          if (direct + i < my_groups) {
+            tc_ld16(acc + 16 * (half + 2 * (direct + i)), gate[i]);
+            tc_ld16(acc + S::kRows + 16 * (half + 2 * (direct + i)), up[i]);
+          }
+        hand_back();
+#pragma unroll
+        for (int i = 0; i < kLate; ++i)
+          if (direct + i < my_groups) store(gate[i], up[i], 16 * (half + 2 * (direct + i)));
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&s.acc_empty[buf]);
     }
     // rows that belong to no expert: zeros, by the epilogue warps of the whole grid
     const size_t width = kSwiglu ? (size_t)a.I / 32 * 17 : (size_t)a.N;

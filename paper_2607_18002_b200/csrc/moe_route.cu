@@ -83,23 +83,23 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_kernel(const float* __
 
 // moe_route_grad: the gradient of the router weights carried on to the logits.  w = softmax over the chosen k logits, so
 //     dz[t, e] = sum_{j: ids[t,j] = e} w_j (dw_j - sum_i w_i dw_i),   0 for an expert that was not chosen.
-// One warp per token, lane j has slot j.  The row is put together in shared memory -- zeros, then the chosen entries -- and written once: bound by
-// its T*E*4 bytes.
+// One warp per token, lane j has slot j; the row is written as zeros and the chosen entries over them by the same warp, in that order.  Bound by
+// the T*E*4 bytes that it writes.
 __global__ void __launch_bounds__(kRouteWarps * 32) route_grad_kernel(const int* __restrict__ ids, const float* __restrict__ w,
                                                                       const float* __restrict__ dw, int T, int E, int k, bool vec,
                                                                       float* __restrict__ dz) {
-  extern __shared__ float4 route_rows[];
   const int lane = threadIdx.x & 31;
   const int t = blockIdx.x * kRouteWarps + (threadIdx.x >> 5);
-  const int quads = (E + 3) / 4;
-  float4* row4 = route_rows + (threadIdx.x >> 5) * quads;
-  float* row = reinterpret_cast<float*>(row4);
-  for (int q = lane; q < quads; q += 32) row4[q] = make_float4(0.f, 0.f, 0.f, 0.f);
   grid_dep_wait();
   if (t >= T) return;
+  float* row = dz + (size_t)t * E;
   const int id = lane < k ? ids[(size_t)t * k + lane] : -1;
   const bool on = (unsigned)id < (unsigned)E;
   const float wj = on ? w[(size_t)t * k + lane] : 0.f, dj = on ? dw[(size_t)t * k + lane] : 0.f;
+  if (vec)
+    for (int e = 4 * lane; e < E; e += 128) *reinterpret_cast<float4*>(row + e) = make_float4(0.f, 0.f, 0.f, 0.f);
+  else
+    for (int e = lane; e < E; e += 32) row[e] = 0.f;
   float mean = wj * dj;
 #pragma unroll
   for (int b = 16; b >= 1; b >>= 1) mean += __shfl_xor_sync(0xffffffffu, mean, b);
@@ -117,12 +117,6 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_grad_kernel(const int*
   }
   __syncwarp();
   if (on && first) row[id] = mine;
-  __syncwarp();
-  float* to = dz + (size_t)t * E;
-  if (vec)
-    for (int q = lane; q < quads; q += 32) reinterpret_cast<float4*>(to)[q] = row4[q];
-  else
-    for (int e = lane; e < E; e += 32) to[e] = row[e];
 }
 
 }  // namespace moe
@@ -136,8 +130,7 @@ extern "C" int moe_route_grad(const int32_t* topk_ids, const float* topk_w, cons
   if (!topk_ids || !topk_w || !d_topk_w || !d_logits) return MOE_EINVAL;
   const int blocks = (n_tokens + kRouteWarps - 1) / kRouteWarps;
   const bool vec = n_experts % 4 == 0 && (reinterpret_cast<uintptr_t>(d_logits) & 15) == 0;
-  const size_t smem = (size_t)kRouteWarps * ((n_experts + 3) / 4) * sizeof(float4);      // at most 32 KB
-  return launch_after(route_grad_kernel, blocks, kRouteWarps * 32, smem, static_cast<cudaStream_t>(stream), topk_ids, topk_w, d_topk_w, n_tokens,
+  return launch_after(route_grad_kernel, blocks, kRouteWarps * 32, 0, static_cast<cudaStream_t>(stream), topk_ids, topk_w, d_topk_w, n_tokens,
                       n_experts, top_k, vec, d_logits) == cudaSuccess ? MOE_OK : MOE_ECUDA;
 }
 

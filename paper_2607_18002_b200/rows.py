@@ -25,7 +25,7 @@ import paper_2607_18002_b200 as moe
 _BF16, _FP32, _I32, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
 _DTYPES = {_BF16: moe.MOE_DTYPE_BF16, torch.float16: moe.MOE_DTYPE_FP16, _FP32: moe.MOE_DTYPE_FP32}
 _SORTED_DTYPES = {**_DTYPES, torch.float8_e4m3fn: moe.MOE_DTYPE_FP8_E4M3, _U8: moe.MOE_DTYPE_FP8_E4M3}
-_Tensor = torch.Tensor
+_Tensor, _empty = torch.Tensor, torch.empty
 _current_device = torch.cuda.current_device
 _stream = moe.Context._stream
 
@@ -185,7 +185,8 @@ def mx_quantize(x, sorted_to_flat=None, flat_to_sorted=None, top_k: int = 1, str
         s2f, f2s = sorted_to_flat.data_ptr(), flat_to_sorted.data_ptr()
     elif top_k != 1:
         _refuse("top_k needs a permutation")
-    codes, scales = x.new_empty((R, K // 2), dtype=_U8), x.new_empty((R, K // 32), dtype=_U8)
+    codes = _empty(R, K // 2, dtype=_U8, device=dev)
+    scales = codes.new_empty(R, K // 32)
     rc = (moe._lib or moe.lib()).moe_mx_quantize(x.data_ptr(), step, _DTYPES[x.dtype], T, top_k, K, s2f, f2s, codes.data_ptr(),
                                                  scales.data_ptr(), _stream(None))
     if rc:
@@ -194,24 +195,26 @@ def mx_quantize(x, sorted_to_flat=None, flat_to_sorted=None, top_k: int = 1, str
 
 
 def _codes(codes, scales, what, dims):
-    """Codes [..., K/2] and scales [..., K/32] of so many dimensions (0: any) -> K."""
-    if not isinstance(codes, _Tensor) or codes.dtype != _U8 or not codes.is_cuda or not codes.is_contiguous() \
-            or (codes.dim() != dims if dims else codes.dim() < 1) or codes.shape[-1] % 16 \
-            or not isinstance(scales, _Tensor) or scales.dtype != _U8 or scales.device != codes.device or not scales.is_contiguous() \
-            or scales.shape[:-1] != codes.shape[:-1] or scales.shape[-1] * 16 != codes.shape[-1]:
+    """Codes [..., K/2] and scales [..., K/32] of so many dimensions (0: any) -> the shape of the codes."""
+    if not isinstance(codes, _Tensor) or not isinstance(scales, _Tensor):
+        _refuse(f"the codes and scales of {what} must be tensors")
+    shape, width = codes.shape, scales.shape
+    if codes.dtype != _U8 or scales.dtype != _U8 or not codes.is_cuda or codes.device != scales.device or not codes.is_contiguous() \
+            or not scales.is_contiguous() or (len(shape) != dims if dims else not shape) or not width or shape[-1] != 16 * width[-1] \
+            or shape[:-1] != width[:-1]:
         _refuse(f"the codes and scales of {what} must be contiguous uint8 tensors of {dims or 'some'} dimensions on one GPU, a scale for 16 bytes of codes")
-    return codes.shape[-1] * 2
+    return shape
 
 
 def mx_dequantize(codes, scales, dtype=_BF16, stream=None):
     """The values [..., K] that codes [..., K/2] with scales [..., K/32] stand for."""
     if dtype not in _DTYPES:
         _refuse(f"dtype must be one of {sorted(map(str, _DTYPES))}")
-    K = _codes(codes, scales, "the rows", 0)
-    dev = codes.device
+    *lead, half = _codes(codes, scales, "the rows", 0)
+    dev, K = codes.device, 2 * half
     if stream is not None or dev.index != _current_device():
         return _elsewhere(mx_dequantize, dev, stream, codes, scales, dtype)
-    out = codes.new_empty((*codes.shape[:-1], K), dtype=dtype)
+    out = _empty(*lead, K, dtype=dtype, device=dev)
     if K:
         rc = (moe._lib or moe.lib()).moe_mx_dequantize(codes.data_ptr(), scales.data_ptr(), out.numel() // K, K, _DTYPES[dtype], out.data_ptr(),
                                                        _stream(None))
@@ -220,22 +223,23 @@ def mx_dequantize(codes, scales, dtype=_BF16, stream=None):
     return out
 
 
-def _operands(codes, scales, w_codes, w_scales, offsets, dev):
-    K = _codes(codes, scales, "the rows", 2)
-    if _codes(w_codes, w_scales, "the weights", 3) != K or w_codes.device != dev:
-        _refuse(f"the weights must have {K} columns and be on {dev}, as the rows")
-    E, n, _ = w_codes.shape
+def _operands(codes, scales, w_codes, w_scales, offsets):
+    """-> device, R, E, n, K"""
+    R, half = _codes(codes, scales, "the rows", 2)
+    E, n, w_half = _codes(w_codes, w_scales, "the weights", 3)
+    dev = codes.device
+    if w_half != half or w_codes.device != dev:
+        _refuse(f"the weights must have {2 * half} columns and be on {dev}, as the rows")
     _index(offsets, "offsets", E + 1, dev)
-    return codes.shape[0], E, n, K
+    return dev, R, E, n, 2 * half
 
 
 def mx_product(codes, scales, w_codes, w_scales, offsets, stream=None):
     """Sorted 4-bit rows [R, K] times the experts' matrices [E, n, K] -> bf16 [R, n]."""
-    dev = getattr(codes, "device", None)
-    R, E, n, K = _operands(codes, scales, w_codes, w_scales, offsets, dev)
+    dev, R, E, n, K = _operands(codes, scales, w_codes, w_scales, offsets)
     if stream is not None or dev.index != _current_device():
         return _elsewhere(mx_product, dev, stream, codes, scales, w_codes, w_scales, offsets)
-    out = codes.new_empty((R, n), dtype=_BF16)
+    out = _empty(R, n, dtype=_BF16, device=dev)
     rc = (moe._lib or moe.lib()).moe_mx_product(codes.data_ptr(), scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), offsets.data_ptr(), R, E,
                                                 n, K, out.data_ptr(), _stream(None))
     if rc:
@@ -245,8 +249,7 @@ def mx_product(codes, scales, w_codes, w_scales, offsets, stream=None):
 
 def mx_swiglu(codes, scales, w_codes, w_scales, offsets, stream=None):
     """Sorted 4-bit rows [R, K] times gate and up matrices [E, 2 I, K], silu(gate) * up -> codes [R, I/2], scales [R, I/32]."""
-    dev = getattr(codes, "device", None)
-    R, E, n, K = _operands(codes, scales, w_codes, w_scales, offsets, dev)
+    dev, R, E, n, K = _operands(codes, scales, w_codes, w_scales, offsets)
     if n % 64:
         _refuse("the weights must have gate and up rows, a multiple of 32 each")
     if stream is not None or dev.index != _current_device():

@@ -21,7 +21,8 @@
 namespace moe {
 namespace {
 
-// Warps 0-7 epilogue, 8 TMA, 9 MMA, 10 and 11 scales.  Three warps a quarter of the SM leave a thread 168 registers, four would leave 128.
+// Warps 0-7 epilogue, 8 TMA, 9 MMA, 10 and 11 scales.  Three warps a quarter of the SM leave a thread 168 registers, four would leave 128; the
+// epilogue's two warpgroups then take 200 and the third keeps 104 (2 x 200 + 104 = 3 x 168).
 constexpr int kMxThreads = 384;
 constexpr int kTmaWarp = 8, kMmaWarp = 9, kScaleWarp = 10, kScaleWarps = 2;
 constexpr int kStageK = 256;                    // columns of K in a stage
@@ -42,15 +43,15 @@ struct MxShared {
 
 // What depends on the rows of a tile.  Shared memory: stages of 32 KB weights, kRows * 128 bytes of rows and the scale blocks of both; TMEM: the
 // accumulators (two buffers of them where they fit) from column 0, the stages' scales behind.
-template <int kRows_>
+template <int kRows_, bool kPair>
 struct Shape {
   static constexpr int kRows = kRows_;
   static constexpr int kRowBlocks = (kRows + 127) / 128;                      // 128-row blocks of row scales
   static constexpr int kScaleBytes = 2 * (2 + kRowBlocks) * kScaleBlock;
-  static constexpr int kWBytes = 2 * kHalfRows * 128, kXBytes = kRows * 128;
+  static constexpr int kWBytes = 2 * kHalfRows * 128, kXBytes = (kPair ? kRows / 2 : kRows) * 128;
   static constexpr int kStageBytes = kWBytes + kXBytes + kScaleBytes;
   static constexpr int kScaleCols = 2 * (2 + kRowBlocks) * 4;                 // TMEM columns of a stage's scales
-  static constexpr int kLate = kRows / 16 < 6 ? kRows / 16 : 6;               // groups of 16 columns that the epilogue takes to registers
+  static constexpr int kGroups = kRows / 16;                                  // groups of 16 columns, as the epilogue takes them
   static constexpr int kAccBufs = kRows <= 96 ? 2 : 1;
   static constexpr int kScaleCol0 = kAccBufs * 2 * kRows;
   static constexpr int kFitSmem = (227 * 1024 - 1024 - (int)sizeof(MxShared)) / kStageBytes, kFitTmem = (512 - kScaleCol0) / kScaleCols;
@@ -71,12 +72,14 @@ struct MxArgs {
   int wide;                      // rows of out are 16-byte aligned
 };
 
-// false: gave up, or somebody has
-__device__ __noinline__ bool wait_slow(unsigned long long* bar, unsigned parity, volatile int* dead) {
+// false: gave up, or somebody of this block has.  kTry: mbar_try, or mbar_try_cluster where the other CTA of a pair hands something over
+template <bool (*kTry)(void*, unsigned) = mbar_try>
+__device__ __forceinline__ bool wait(unsigned long long* bar, unsigned parity, volatile int* dead) {
+  if (kTry(bar, parity)) return true;
   const unsigned long long start = gtime_ns();
   for (;;) {
     for (int i = 0; i < 64; ++i)
-      if (mbar_try(bar, parity)) return true;
+      if (kTry(bar, parity)) return true;
     if (*dead) return false;
     if (gtime_ns() - start > kWaitNs) {
       *dead = 1;
@@ -84,42 +87,64 @@ __device__ __noinline__ bool wait_slow(unsigned long long* bar, unsigned parity,
     }
   }
 }
-__device__ __forceinline__ bool wait(unsigned long long* bar, unsigned parity, volatile int* dead) {
-  return mbar_try(bar, parity) || wait_slow(bar, parity, dead);
-}
 
 // shared-memory descriptor of a scale block: 32 rows of 16 bytes, unswizzled, 8-row groups 128 bytes apart
 __device__ __forceinline__ unsigned long long scale_desc(unsigned saddr) {
   return (unsigned long long)((saddr & 0x3ffffu) >> 4) | 8ull << 16 | 8ull << 32 | 1ull << 46;
 }
+// (of a pair: in both CTAs, each from its own shared memory into its own TMEM)
+template <bool kPair>
 __device__ __forceinline__ void copy_scales(unsigned tmem, unsigned saddr) {
-  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(scale_desc(saddr)) : "memory");
+  if (kPair) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(scale_desc(saddr)) : "memory");
+  else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(scale_desc(saddr)) : "memory");
 }
+template <bool kPair>
 __device__ __forceinline__ void mma_mxf4(unsigned d, unsigned long long a, unsigned long long b, unsigned idesc, unsigned sfa, unsigned sfb,
                                          unsigned accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %6, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
-      : "memory");
+  if (kPair)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
+        : "memory");
 }
-// e2m1 operands, both K-major, power-of-two scales, M = 128, N columns; half: which two of a block's four scales a row (K = 64 takes two)
-__device__ __forceinline__ unsigned mx_idesc(unsigned n, unsigned half) {
-  return 1u << 7 | 1u << 10 | (n >> 3) << 17 | 1u << 23 | (128u >> 4) << 24 | (2u * half) << 4 | (2u * half) << 29;
+// e2m1 operands, both K-major, power-of-two scales, M rows, N columns; half: which two of a block's four scales a row (K = 64 takes two)
+__device__ __forceinline__ unsigned mx_idesc(unsigned m, unsigned n, unsigned half) {
+  return 1u << 7 | 1u << 10 | (n >> 3) << 17 | 1u << 23 | (m >> 4) << 24 | (2u * half) << 4 | (2u * half) << 29;
 }
-__device__ __forceinline__ void tma_2d(unsigned dst, const CUtensorMap* m, int x, int y, void* bar) {
-  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-               "l"(reinterpret_cast<unsigned long long>(m)), "r"(x), "r"(y), "r"(smem_u32(bar))
-               : "memory");
+// bar: shared::cluster address of the barrier (of a pair: the leader's)
+template <bool kPair>
+__device__ __forceinline__ void tma_2d(unsigned dst, const CUtensorMap* m, int x, int y, unsigned bar) {
+  if (kPair)
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+                 "l"(reinterpret_cast<unsigned long long>(m)), "r"(x), "r"(y), "r"(bar)
+                 : "memory");
+  else
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+                 "l"(reinterpret_cast<unsigned long long>(m)), "r"(x), "r"(y), "r"(bar)
+                 : "memory");
 }
-__device__ __forceinline__ void tma_3d(unsigned dst, const CUtensorMap* m, int x, int y, int z, void* bar) {
-  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
-               "l"(reinterpret_cast<unsigned long long>(m)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
-               : "memory");
+template <bool kPair>
+__device__ __forceinline__ void tma_3d(unsigned dst, const CUtensorMap* m, int x, int y, int z, unsigned bar) {
+  if (kPair)
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+                 "l"(reinterpret_cast<unsigned long long>(m)), "r"(x), "r"(y), "r"(z), "r"(bar)
+                 : "memory");
+  else
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+                 "l"(reinterpret_cast<unsigned long long>(m)), "r"(x), "r"(y), "r"(z), "r"(bar)
+                 : "memory");
 }
-__device__ __forceinline__ void expect_tx(void* bar, unsigned bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
+__device__ __forceinline__ void expect_tx(unsigned bar, unsigned bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void tc_ld16(unsigned taddr, unsigned (&r)[16]) {
   asm volatile(
@@ -189,13 +214,13 @@ __device__ __forceinline__ unsigned pack_bf16(unsigned lo, unsigned hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(lo), __uint_as_float(hi));
   return *reinterpret_cast<const unsigned*>(&v);
 }
-// 8 x 8 fp32 values over eight neighbouring lanes, lane i with value j of column i: lane j gets row j as eight bf16.  Lane bit 0 changes places with
-// row bit 0 inside the packed pairs, then bits 1 and 2 with whole words.
+// 8 x 8 bf16 values over eight neighbouring lanes, lane i with column i as four pairs of rows: lane j gets row j.  Lane bit 0 changes places with
+// row bit 0 inside the pairs, then bits 1 and 2 with whole words.
 __device__ __forceinline__ uint4 transpose_bf16(const unsigned* v, int lane) {
   unsigned q[4], lo[2], hi[2];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const unsigned own = pack_bf16(v[2 * i], v[2 * i + 1]), other = __shfl_xor_sync(0xffffffffu, own, 1);
+    const unsigned own = v[i], other = __shfl_xor_sync(0xffffffffu, own, 1);
     q[i] = __byte_perm(own, other, lane & 1 ? 0x3276u : 0x5410u);
   }
 #pragma unroll
@@ -210,25 +235,28 @@ __device__ __forceinline__ uint4 transpose_bf16(const unsigned* v, int lane) {
   return lane & 4 ? make_uint4(other0, other1, own0, own1) : make_uint4(own0, own1, other0, other1);
 }
 
-template <int kRows_, bool kSwiglu>
+template <int kRows_, bool kSwiglu, bool kPair>
 __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_constant__ MxArgs a) {
-  using S = Shape<kRows_>;
+  using S = Shape<kRows_, kPair>;
   extern __shared__ unsigned char raw[];
   unsigned char* stages = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   MxShared& s = *reinterpret_cast<MxShared*>(stages + S::kStages * S::kStageBytes);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  constexpr int kStep = kSwiglu ? kHalfRows : 2 * kHalfRows;       // output columns of a tile
+  constexpr int kCtas = kPair ? 2 : 1;
+  constexpr int kStep = (kSwiglu ? 1 : 2) * kHalfRows * kCtas;     // output columns of a tile
+  const unsigned rank = kPair ? cluster_ctarank() : 0u;            // weight rows of an accumulator: this CTA has the rank-th 128
+  const int unit = (int)blockIdx.x / kCtas, n_units = (int)gridDim.x / kCtas;
   const int n_blocks = ((kSwiglu ? a.I : a.N) + kStep - 1) / kStep;
 
   if (tid == 0) {
     for (int i = 0; i < S::kStages; ++i) {
-      mbar_init(&s.full[i], 1);
-      mbar_init(&s.landed[i], kScaleWarps);
+      mbar_init(&s.full[i], kCtas);
+      mbar_init(&s.landed[i], kScaleWarps * kCtas);
       mbar_init(&s.empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&s.acc_full[i], 1);
-      mbar_init(&s.acc_empty[i], 8);
+      mbar_init(&s.acc_empty[i], 8 * kCtas);
     }
     mbar_init(&s.drained, 1);
     s.dead = 0;
@@ -236,8 +264,13 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
     fence_async_proxy_smem();
   }
   if (warp == kMmaWarp) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s.tmem)) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    if (kPair) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s.tmem)) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s.tmem)) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
   }
   grid_dep_wait();
   for (int e = tid; e <= a.E; e += kMxThreads) s.first_row[e] = min(max(a.offsets[e], 0), a.R);
@@ -260,209 +293,70 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
     if (lane == 0) s.first_tile[a.E] = before;
   }
   __syncthreads();
+  if (kPair) cluster_sync_all();          // the other CTA's barriers exist before anything arrives on them
   const unsigned tmem = s.tmem;
   const int n_tiles = s.first_tile[a.E];
   const int n_stages = (a.K + kStageK - 1) / kStageK;
 
-  if (warp == kTmaWarp) {
-    if (elect_one()) {
-      unsigned n = 0;            // stages so far
-      for (int t = blockIdx.x; t < n_tiles && !s.dead; t += gridDim.x) {
-        const Tile at = tile_at<S::kRows>(s, a.E, t, kStep);
-        const int boxes = (at.rows + kBoxRows - 1) / kBoxRows;
-        for (int i = 0; i < n_stages; ++i, ++n) {
-          const unsigned slot = n % S::kStages, round = n / S::kStages;
-          if (round && !wait(&s.empty[slot], (round - 1) & 1, &s.dead)) break;
-          const unsigned to = smem_u32(stages + slot * S::kStageBytes);
-          expect_tx(&s.full[slot], S::kWBytes + boxes * kBoxRows * 128);
-          tma_3d(to, &a.tm_w, i * 128, at.n0, at.expert, &s.full[slot]);
-          tma_3d(to + kHalfRows * 128, &a.tm_w, i * 128, (kSwiglu ? a.I : kHalfRows) + at.n0, at.expert, &s.full[slot]);
-          for (int b = 0; b < boxes; ++b) tma_2d(to + S::kWBytes + b * kBoxRows * 128, &a.tm_x, i * 128, at.row0 + b * kBoxRows, &s.full[slot]);
-        }
-      }
-      // copies that nobody has waited for (after a wait that ran out): the block's shared memory is theirs until they have landed
-      for (unsigned m = n > S::kStages ? n - S::kStages : 0; s.dead && m < n; ++m) {
-        const unsigned long long start = gtime_ns();
-        while (!mbar_try(&s.full[m % S::kStages], (m / S::kStages) & 1) && gtime_ns() - start < kWaitNs) {}
-      }
-    }
-    __syncwarp();
-  } else if (warp == kMmaWarp) {
-    if (elect_one()) {
-      unsigned n = 0, k = 0;     // stages, tiles so far
-      bool ok = true;
-      for (int t = blockIdx.x; t < n_tiles && ok; t += gridDim.x, ++k) {
-        const Tile at = tile_at<S::kRows>(s, a.E, t, kStep);
-        const unsigned buf = k % S::kAccBufs, use = k / S::kAccBufs;
-        if (use) ok = wait(&s.acc_empty[buf], (use - 1) & 1, &s.dead);
-        if (!ok) break;
-        tc_fence_after();
-        const unsigned cols = (unsigned)(at.rows + 15) & ~15u;
-        const unsigned acc = tmem + buf * 2 * S::kRows;
-        for (int i = 0; i < n_stages; ++i, ++n) {
-          const unsigned slot = n % S::kStages, round = n / S::kStages;
-          ok = wait(&s.full[slot], round & 1, &s.dead) && wait(&s.landed[slot], round & 1, &s.dead);
-          if (!ok) break;
-          tc_fence_after();
-          const unsigned st = smem_u32(stages + slot * S::kStageBytes);
-          const unsigned sc = st + S::kWBytes + S::kXBytes, tsc = tmem + S::kScaleCol0 + slot * S::kScaleCols;
-          const int groups = min(2, (a.K - i * kStageK) / kGroupK);
-          for (int g = 0; g < groups; ++g) {
-            const unsigned from = sc + g * (2 + S::kRowBlocks) * kScaleBlock, to = tsc + g * (2 + S::kRowBlocks) * 4;
-#pragma unroll
-            for (int b = 0; b < 2 + S::kRowBlocks; ++b) copy_scales(to + 4 * b, from + b * kScaleBlock);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const unsigned step = (2 * g + h) * 32;       // 64 columns, 32 bytes
-              const unsigned long long xd = umma_desc(st + S::kWBytes + step, 128);
-              const unsigned idesc = mx_idesc(cols, h), first = (i | g | h) != 0;
-              mma_mxf4(acc, umma_desc(st + step, 128), xd, idesc, to, to + 8, first);
-              mma_mxf4(acc + S::kRows, umma_desc(st + kHalfRows * 128 + step, 128), xd, idesc, to + 4, to + 8, first);
-            }
-          }
-          tc_commit(&s.empty[slot]);
-        }
-        if (ok) tc_commit(&s.acc_full[buf]);
-      }
-      tc_commit(&s.drained);     // nothing of this block's is left in the tensor core when it frees its TMEM
-      const unsigned long long start = gtime_ns();
-      while (!mbar_try(&s.drained, 0) && gtime_ns() - start < kWaitNs) {}
-    }
-    __syncwarp();
-  } else if (warp >= kScaleWarp) {
-    // A thread has two rows of every 128-row block, in the order that spreads a warp's stores over all banks: their four bytes of a group of
-    // 128 columns go to 16 (r % 32) + 4 (r / 32) of the group's block.  16 bytes of a row are two stages; those of the next two are on their
-    // way to registers meanwhile, whether or not their stages are free.
-    const int r0 = 32 * (lane & 3) + 8 * (warp - kScaleWarp) + (lane >> 2);      // and r0 + 16
-    const unsigned spot = (unsigned)(r0 & 31) * 16 + (unsigned)(r0 >> 5) * 4;
-    const int per_row = a.K / kMxBlock, n_pairs = (n_stages + 1) / 2;
-    const int vec = per_row % 16 == 0 ? 16 : per_row % 8 == 0 ? 8 : 4;
-    const bool vec_w = ((size_t)a.w_scales & (vec - 1)) == 0, vec_x = ((size_t)a.x_scales & (vec - 1)) == 0;
-    constexpr int kBlocks = 2 + S::kRowBlocks;
-    struct Pair {
-      uint4 b[kBlocks][2];
-      int stages;                // 1 or 2; 0: there is no more
-    };
-    int t = blockIdx.x, pair = 0;
-    const unsigned char* from[kBlocks][2];
-    unsigned n = 0;
-    const auto fetch = [&](Pair& p) {
-      p.stages = 0;
-      if (t >= n_tiles) return;
-      if (pair == 0) {
-        const Tile at = tile_at<S::kRows>(s, a.E, t, kStep);
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          const int r = r0 + 16 * q;
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {    // a weight row behind the last one: any other's scales (its products are not stored)
-            const int row = kSwiglu ? min(at.n0 + r, a.I - 1) + b * a.I : min(at.n0 + b * kHalfRows + r, a.N - 1);
-            from[b][q] = a.w_scales + ((size_t)at.expert * a.N + row) * per_row;
-          }
-#pragma unroll
-          for (int b = 0; b < S::kRowBlocks; ++b) from[2 + b][q] = a.x_scales + (size_t)(at.row0 + min(b * 128 + r, at.rows - 1)) * per_row;
-        }
-      }
-#pragma unroll
-      for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-        for (int q = 0; q < 2; ++q) p.b[b][q] = load_scales(from[b][q] + pair * 16, per_row - pair * 16, (b < 2 ? vec_w : vec_x) ? vec : 4);
-      p.stages = min(2, n_stages - 2 * pair);
-      if (++pair == n_pairs) {
-        pair = 0;
-        t += gridDim.x;
-      }
-    };
-    const auto put = [&](const Pair& p) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if (h >= p.stages) break;
-        const unsigned slot = n % S::kStages, round = n / S::kStages;
-        if (round && !__all_sync(0xffffffffu, wait(&s.empty[slot], (round - 1) & 1, &s.dead))) return false;
-        const unsigned to = smem_u32(stages + slot * S::kStageBytes) + S::kWBytes + S::kXBytes + spot;
-#pragma unroll
-        for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            const uint4& v = p.b[b][q];
-            st_word(to + b * kScaleBlock + 256 * q, h ? v.z : v.x);
-            st_word(to + (kBlocks + b) * kScaleBlock + 256 * q, h ? v.w : v.y);
-          }
-        fence_async_proxy_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&s.landed[slot]);
-        ++n;
-      }
-      return true;
-    };
-    Pair even, odd;
-    fetch(even);
-    while (even.stages) {
-      fetch(odd);
-      if (!put(even) || !odd.stages) break;
-      fetch(even);
-      if (!put(odd)) break;
-    }
-  } else {
+  if (warp < kTmaWarp) {
+    if (S::kRows > 96) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
     const int quad = warp & 3, half = warp >> 2;
     unsigned k = 0;
     bool ok = true;
-    for (int t = blockIdx.x; t < n_tiles; t += gridDim.x, ++k) {
+    for (int t = unit; t < n_tiles; t += n_units, ++k) {
       const Tile at = tile_at<S::kRows>(s, a.E, t, kStep);
       const unsigned buf = k % S::kAccBufs, use = k / S::kAccBufs;
       if (ok) ok = __all_sync(0xffffffffu, wait(&s.acc_full[buf], use & 1, &s.dead));
       tc_fence_after();
       const unsigned acc = tmem + buf * 2 * S::kRows + ((unsigned)quad << 21);      // this warp's 32 lanes
-      // The last columns of the accumulator go to registers all at once and are worked off after it has been handed back, while the next
-      // tile's MMAs run.
+      // Everything that is in the accumulator goes to registers first -- as bf16 for the plain product, for swiglu half of the rows as they
+      // are and half as silu(gate) up -- and the accumulator is handed back: rounding, quantising and storing run beside the next tile's MMAs.
       const auto hand_back = [&] {
         tc_wait_ld();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&s.acc_empty[buf]);
+        if (lane == 0) {
+          if (kPair) mbar_arrive_cluster(map_to_cta(&s.acc_empty[buf], 0));
+          else mbar_arrive(&s.acc_empty[buf]);
+        }
       };
       const int groups = (at.rows + 15) / 16;
       if (!kSwiglu) {            // warps 0-3 have the first accumulator, 4-7 the second
         const unsigned mine = acc + half * S::kRows;
-        const int col = at.n0 + half * kHalfRows + quad * 32 + lane;
-        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + (size_t)at.row0 * a.N + col;
-        const auto store = [&](unsigned (&v)[16], int c) {
-          if (!ok) {
+        const int col = at.n0 + (half * kCtas + (int)rank) * kHalfRows + quad * 32 + lane, col8 = col - lane + (lane >> 3) * 8;
+        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + (size_t)at.row0 * a.N;
+        unsigned v[S::kGroups][8];
 #pragma unroll
-            for (int j = 0; j < 16; ++j) v[j] = 0x7fffffffu;
-          }
-          if (a.wide) {          // eight neighbouring columns of a row a lane, 16 bytes: stores of 2 bytes took the down product 1.4 times as long
-#pragma unroll
-            for (int j0 = 0; j0 < 16; j0 += 8) {
-              const uint4 w = transpose_bf16(v + j0, lane);
-              const int row = c + j0 + (lane & 7), col8 = col - lane + (lane >> 3) * 8;
-              if (row < at.rows && col8 < a.N)
-                *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.out) + (size_t)(at.row0 + row) * a.N + col8) = w;
-            }
-          } else {
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-              if (c + j < at.rows && col < a.N) out[(size_t)(c + j) * a.N] = __float2bfloat16_rn(__uint_as_float(v[j]));
-          }
-        };
-        const int direct = max(groups - S::kLate, 0);
-        for (int g = 0; g < direct; ++g) {
-          unsigned v[16];
-          tc_ld16(mine + 16 * g, v);
+        for (int g = 0; g < S::kGroups; ++g) {
+          if (g >= groups) break;
+          unsigned raw[16];
+          tc_ld16(mine + 16 * g, raw);
           tc_wait_ld();
-          store(v, 16 * g);
-        }
-        unsigned v[S::kLate][16];
 #pragma unroll
-        for (int i = 0; i < S::kLate; ++i)
-          if (direct + i < groups) tc_ld16(mine + 16 * (direct + i), v[i]);
+          for (int j = 0; j < 8; ++j) v[g][j] = ok ? pack_bf16(raw[2 * j], raw[2 * j + 1]) : 0x7fff7fffu;
+        }
         hand_back();
 #pragma unroll
-        for (int i = 0; i < S::kLate; ++i)
-          if (direct + i < groups) store(v[i], 16 * (direct + i));
+        for (int g = 0; g < S::kGroups; ++g) {
+          if (g >= groups) break;
+#pragma unroll
+          for (int j0 = 0; j0 < 16; j0 += 8) {
+            const int c = 16 * g + j0;
+            if (a.wide) {        // eight neighbouring columns of a row a lane: stores of 2 bytes took the down product 1.3 times as long
+              const uint4 w = transpose_bf16(&v[g][j0 / 2], lane);
+              const int row = c + (lane & 7);
+              if (row < at.rows && col8 < a.N) *reinterpret_cast<uint4*>(out + (size_t)row * a.N + col8) = w;
+            } else {
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                if (c + j < at.rows && col < a.N)
+                  reinterpret_cast<unsigned short*>(out)[(size_t)(c + j) * a.N + col] = (unsigned short)(v[g][(j0 + j) / 2] >> (16 * (j & 1)));
+            }
+          }
+        }
       } else {                   // warps 0-3 and 4-7 take turns at groups of 16 rows
-        const int col = at.n0 + quad * 32, per_row = a.I / kMxBlock;
-        const auto store = [&](const unsigned (&gate)[16], const unsigned (&up)[16], int c) {
+        const int col = at.n0 + (int)rank * kHalfRows + quad * 32, per_row = a.I / kMxBlock;
+        const auto store = [&](const float (&v)[16], int c) {
 #pragma unroll
           for (int j0 = 0; j0 < 16; j0 += 8) {
             unsigned word = 0u, mine = 0u;
@@ -471,11 +365,9 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
               float q[2];
 #pragma unroll
               for (int i = 0; i < 2; ++i) {
-                const float gv = __uint_as_float(gate[j0 + j + i]), uv = __uint_as_float(up[j0 + j + i]);
-                const float v = gv * rcp_approx(1.f + __expf(-gv)) * uv;
-                const unsigned top = __reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7f800000u);
+                const unsigned top = __reduce_max_sync(0xffffffffu, __float_as_uint(v[j0 + j + i]) & 0x7f800000u);
                 if ((lane & 7) == j + i) mine = top;
-                q[i] = v * __uint_as_float(min(0x80000000u - top, 0x7f000000u));     // 2^(127 - scale byte)
+                q[i] = v[j0 + j + i] * __uint_as_float(min(0x80000000u - top, 0x7f000000u));     // 2^(127 - scale byte)
               }
               word |= mx_codes2(q[0], q[1]) << (4 * j);
             }
@@ -488,26 +380,43 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
             }
           }
         };
-        constexpr int kLate = (S::kLate + 1) / 2;
-        const int my_groups = (groups - half + 1) / 2, direct = max(my_groups - kLate, 0);
-        for (int g = 0; g < direct; ++g) {
-          unsigned gate[16], up[16];
-          tc_ld16(acc + 16 * (half + 2 * g), gate);
-          tc_ld16(acc + S::kRows + 16 * (half + 2 * g), up);
-          tc_wait_ld();
-          store(gate, up, 16 * (half + 2 * g));
-        }
-        unsigned gate[kLate][16], up[kLate][16];
+        constexpr int kMine = (S::kGroups + 1) / 2, kAsTheyAre = (kMine + 1) / 2, kFirst = kMine - kAsTheyAre;
+        const int my_groups = (groups - half + 1) / 2;
+        float v[kFirst > 0 ? kFirst : 1][16];
+        unsigned gate[kAsTheyAre][16], up[kAsTheyAre][16];
+        const auto load = [&](unsigned (&g)[16], unsigned (&u)[16], int i) {
+          tc_ld16(acc + 16 * (half + 2 * i), g);
+          tc_ld16(acc + S::kRows + 16 * (half + 2 * i), u);
+        };
+        const auto activate = [&](const unsigned (&g)[16], const unsigned (&u)[16], float (&to)[16]) {
 #pragma unroll
-        for (int i = 0; i < kLate; ++i)
-          if (direct + i < my_groups) {
-            tc_ld16(acc + 16 * (half + 2 * (direct + i)), gate[i]);
-            tc_ld16(acc + S::kRows + 16 * (half + 2 * (direct + i)), up[i]);
+          for (int j = 0; j < 16; ++j) {
+            const float gv = __uint_as_float(g[j]);
+            to[j] = gv * rcp_approx(1.f + __expf(-gv)) * __uint_as_float(u[j]);
           }
+        };
+#pragma unroll
+        for (int i = 0; i < kFirst; ++i)
+          if (i < my_groups) {
+            unsigned g[16], u[16];
+            load(g, u, i);
+            tc_wait_ld();
+            activate(g, u, v[i]);
+          }
+#pragma unroll
+        for (int i = 0; i < kAsTheyAre; ++i)
+          if (kFirst + i < my_groups) load(gate[i], up[i], kFirst + i);
         hand_back();
 #pragma unroll
-        for (int i = 0; i < kLate; ++i)
-          if (direct + i < my_groups) store(gate[i], up[i], 16 * (half + 2 * (direct + i)));
+        for (int i = 0; i < kFirst; ++i)
+          if (i < my_groups) store(v[i], 16 * (half + 2 * i));
+#pragma unroll
+        for (int i = 0; i < kAsTheyAre; ++i)
+          if (kFirst + i < my_groups) {
+            float w[16];
+            activate(gate[i], up[i], w);
+            store(w, 16 * (half + 2 * (kFirst + i)));
+          }
       }
     }
     // rows that belong to no expert: zeros, by the epilogue warps of the whole grid
@@ -521,13 +430,168 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
         else a.out_scales[p * (a.I / 32) + (c - a.I / 2)] = 0;
       }
     }
+  } else {
+    if (S::kRows > 96) asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+    if (warp == kTmaWarp) {
+      if (elect_one()) {
+        unsigned n = 0;            // stages so far
+        for (int t = unit; t < n_tiles && !s.dead; t += n_units) {
+          const Tile at = tile_at<S::kRows>(s, a.E, t, kStep);
+          // of a pair each CTA has half of the rows
+          const int mine = kPair ? (at.rows + 31) / 32 * 16 : at.rows, row0 = at.row0 + (int)rank * mine, boxes = (mine + kBoxRows - 1) / kBoxRows;
+          const bool second = kSwiglu || at.n0 + kHalfRows * kCtas < a.N;
+          const int n0 = at.n0 + (int)rank * kHalfRows;
+          for (int i = 0; i < n_stages; ++i, ++n) {
+            const unsigned slot = n % S::kStages, round = n / S::kStages;
+            if (round && !wait(&s.empty[slot], (round - 1) & 1, &s.dead)) break;
+            const unsigned to = smem_u32(stages + slot * S::kStageBytes);
+            const unsigned bar = kPair ? map_to_cta(&s.full[slot], 0) : smem_u32(&s.full[slot]);
+            expect_tx(bar, (second ? S::kWBytes : S::kWBytes / 2) + boxes * kBoxRows * 128);
+            tma_3d<kPair>(to, &a.tm_w, i * 128, n0, at.expert, bar);
+            if (second) tma_3d<kPair>(to + kHalfRows * 128, &a.tm_w, i * 128, n0 + (kSwiglu ? a.I : kHalfRows * kCtas), at.expert, bar);
+            for (int b = 0; b < boxes; ++b) tma_2d<kPair>(to + S::kWBytes + b * kBoxRows * 128, &a.tm_x, i * 128, row0 + b * kBoxRows, bar);
+          }
+        }
+        // copies that nobody has waited for (after a wait that ran out): the block's shared memory is theirs until they have landed
+        for (unsigned m = n > S::kStages ? n - S::kStages : 0; s.dead && m < n; ++m) {
+          const unsigned long long start = gtime_ns();
+          while (!(rank ? mbar_try(&s.empty[m % S::kStages], (m / S::kStages) & 1) : mbar_try(&s.full[m % S::kStages], (m / S::kStages) & 1)) &&
+                 gtime_ns() - start < kWaitNs) {}
+        }
+      }
+      __syncwarp();
+    } else if (warp == kMmaWarp) {
+      if (rank == 0 && elect_one()) {
+        const auto commit = [](unsigned long long* bar) {
+          if (kPair) tc_commit_pair(bar);
+          else tc_commit(bar);
+        };
+        unsigned n = 0, k = 0;     // stages, tiles so far
+        bool ok = true;
+        for (int t = unit; t < n_tiles && ok; t += n_units, ++k) {
+          const Tile at = tile_at<S::kRows>(s, a.E, t, kStep);
+          const unsigned buf = k % S::kAccBufs, use = k / S::kAccBufs;
+          if (use) ok = wait<kPair ? mbar_try_cluster : mbar_try>(&s.acc_empty[buf], (use - 1) & 1, &s.dead);
+          if (!ok) break;
+          tc_fence_after();
+          const unsigned cols = kPair ? (unsigned)(at.rows + 31) & ~31u : (unsigned)(at.rows + 15) & ~15u;
+          const bool second = kSwiglu || at.n0 + kHalfRows * kCtas < a.N;
+          const unsigned acc = tmem + buf * 2 * S::kRows;
+          for (int i = 0; i < n_stages; ++i, ++n) {
+            const unsigned slot = n % S::kStages, round = n / S::kStages;
+            ok = wait(&s.full[slot], round & 1, &s.dead) && wait(&s.landed[slot], round & 1, &s.dead);
+            if (!ok) break;
+            tc_fence_after();
+            const unsigned st = smem_u32(stages + slot * S::kStageBytes);
+            const unsigned sc = st + S::kWBytes + S::kXBytes, tsc = tmem + S::kScaleCol0 + slot * S::kScaleCols;
+            const int groups = min(2, (a.K - i * kStageK) / kGroupK);
+            for (int g = 0; g < groups; ++g) {
+              const unsigned from = sc + g * (2 + S::kRowBlocks) * kScaleBlock, to = tsc + g * (2 + S::kRowBlocks) * 4;
+#pragma unroll
+              for (int b = 0; b < 2 + S::kRowBlocks; ++b) copy_scales<kPair>(to + 4 * b, from + b * kScaleBlock);
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                const unsigned step = (2 * g + h) * 32;       // 64 columns, 32 bytes
+                const unsigned long long xd = umma_desc(st + S::kWBytes + step, 128);
+                const unsigned idesc = mx_idesc(kHalfRows * kCtas, cols, h), first = (i | g | h) != 0;
+                mma_mxf4<kPair>(acc, umma_desc(st + step, 128), xd, idesc, to, to + 8, first);
+                if (second) mma_mxf4<kPair>(acc + S::kRows, umma_desc(st + kHalfRows * 128 + step, 128), xd, idesc, to + 4, to + 8, first);
+              }
+            }
+            commit(&s.empty[slot]);
+          }
+          if (ok) commit(&s.acc_full[buf]);
+        }
+        commit(&s.drained);     // nothing of this block's is left in the tensor core when it frees its TMEM
+        const unsigned long long start = gtime_ns();
+        while (!mbar_try(&s.drained, 0) && gtime_ns() - start < kWaitNs) {}
+      }
+      __syncwarp();
+    } else if (warp >= kScaleWarp) {
+      // A thread has two rows of every 128-row block, in the order that spreads a warp's stores over all banks: their four bytes of a group of
+      // 128 columns go to 16 (r % 32) + 4 (r / 32) of the group's block.  16 bytes of a row are two stages; those of the next two are on their
+      // way to registers meanwhile, whether or not their stages are free.
+      const int r0 = 32 * (lane & 3) + 8 * (warp - kScaleWarp) + (lane >> 2);      // and r0 + 16
+      const unsigned spot = (unsigned)(r0 & 31) * 16 + (unsigned)(r0 >> 5) * 4;
+      const int per_row = a.K / kMxBlock, n_pairs = (n_stages + 1) / 2;
+      const int vec = per_row % 16 == 0 ? 16 : per_row % 8 == 0 ? 8 : 4;
+      const int vec_w = (size_t)a.w_scales & (vec - 1) ? 4 : vec, vec_x = (size_t)a.x_scales & (vec - 1) ? 4 : vec;
+      constexpr int kBlocks = 2 + S::kRowBlocks;
+      struct Pair {
+        uint4 b[kBlocks][2];
+        int stages;                // 1 or 2; 0: there is no more
+      };
+      int t = unit, pair = 0;
+      Tile at{};
+      unsigned n = 0;
+      const auto fetch = [&](Pair& p) {
+        p.stages = 0;
+        if (t >= n_tiles) return;
+        if (pair == 0) at = tile_at<S::kRows>(s, a.E, t, kStep);
+        const unsigned char* w = a.w_scales + (size_t)at.expert * a.N * per_row + pair * 16;
+        const unsigned char* x = a.x_scales + (size_t)at.row0 * per_row + pair * 16;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const int r = r0 + 16 * q;
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {      // a weight row behind the last one: any other's scales (its products are not stored)
+            const int row = kSwiglu ? min(at.n0 + (int)rank * kHalfRows + r, a.I - 1) + b * a.I
+                                    : min(at.n0 + (b * kCtas + (int)rank) * kHalfRows + r, a.N - 1);
+            p.b[b][q] = load_scales(w + (size_t)row * per_row, per_row - pair * 16, vec_w);
+          }
+#pragma unroll
+          for (int b = 0; b < S::kRowBlocks; ++b)
+            p.b[2 + b][q] = load_scales(x + (size_t)min(b * 128 + r, at.rows - 1) * per_row, per_row - pair * 16, vec_x);
+        }
+        p.stages = min(2, n_stages - 2 * pair);
+        if (++pair == n_pairs) {
+          pair = 0;
+          t += n_units;
+        }
+      };
+      const auto put = [&](const Pair& p) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (h >= p.stages) break;
+          const unsigned slot = n % S::kStages, round = n / S::kStages;
+          if (round && !__all_sync(0xffffffffu, wait(&s.empty[slot], (round - 1) & 1, &s.dead))) return false;
+          const unsigned to = smem_u32(stages + slot * S::kStageBytes) + S::kWBytes + S::kXBytes + spot;
+#pragma unroll
+          for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+              const uint4& v = p.b[b][q];
+              st_word(to + b * kScaleBlock + 256 * q, h ? v.z : v.x);
+              st_word(to + (kBlocks + b) * kScaleBlock + 256 * q, h ? v.w : v.y);
+            }
+          fence_async_proxy_smem();
+          __syncwarp();
+          if (lane == 0) {
+            if (kPair) mbar_arrive_remote(map_to_cta(&s.landed[slot], 0));
+            else mbar_arrive(&s.landed[slot]);
+          }
+          ++n;
+        }
+        return true;
+      };
+      Pair even, odd;
+      fetch(even);
+      while (even.stages) {
+        fetch(odd);
+        if (!put(even) || !odd.stages) break;
+        fetch(even);
+        if (!put(odd)) break;
+      }
+    }
   }
   __syncwarp();
   tc_fence_before();
   __syncthreads();
+  if (kPair) cluster_sync_all();          // no CTA leaves while the other may still signal its barriers, or read its shared memory
   if (warp == kMmaWarp) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    if (kPair) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
   }
 }
 
@@ -556,21 +620,38 @@ bool encode_codes(CUtensorMap* out, const void* base, int bytes, int rows, int p
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int kRows, bool kSwiglu>
+template <int kRows, bool kSwiglu, bool kPair>
 cudaError_t product_launch(const MxArgs& a, cudaStream_t stream) {
-  using S = Shape<kRows>;
+  using S = Shape<kRows, kPair>;
   constexpr size_t smem = 1024 + (size_t)S::kStages * S::kStageBytes + sizeof(MxShared);
   static_assert(smem <= 227 * 1024, "shared memory");
+  constexpr int kCtas = kPair ? 2 : 1;
+  auto* kernel = mx_product_kernel<kRows, kSwiglu, kPair>;
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(mx_product_kernel<kRows, kSwiglu>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   // most tiles that the rows can make
-  const int step = kSwiglu ? kHalfRows : 2 * kHalfRows;
+  const int step = (kSwiglu ? 1 : 2) * kHalfRows * kCtas;
   const long long m_tiles = a.R / kRows + (a.R < a.E ? a.R : a.E), tiles = m_tiles * (((kSwiglu ? a.I : a.N) + step - 1) / step);
   if (tiles > 0x3fffffffll) return cudaErrorInvalidValue;
-  return launch_after(mx_product_kernel<kRows, kSwiglu>, tiles < sms ? (int)tiles : sms, kMxThreads, smem, stream, a);
+  const int units = tiles < sms / kCtas ? (int)tiles : sms / kCtas;
+  if (!kPair) return launch_after(kernel, units, kMxThreads, smem, stream, a);
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 2;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)units * 2);
+  cfg.blockDim = dim3((unsigned)kMxThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
 template <bool kSwiglu>
@@ -592,9 +673,9 @@ int product(const void* codes, const void* scales, const void* w_codes, const vo
   a.R = n_rows; a.E = n_experts; a.N = n; a.K = K; a.I = n / 2;
   a.wide = n % 8 == 0 && (reinterpret_cast<uintptr_t>(out) & 15) == 0;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const int rows = n_rows <= 24ll * n_experts ? 32 : n_rows <= 64ll * n_experts ? 64 : 192;
-  const cudaError_t e = rows == 32 ? product_launch<32, kSwiglu>(a, st) : rows == 64 ? product_launch<64, kSwiglu>(a, st)
-                                                                                     : product_launch<192, kSwiglu>(a, st);
+  const cudaError_t e = n_rows <= 24ll * n_experts   ? product_launch<32, kSwiglu, false>(a, st)
+                        : n_rows <= 64ll * n_experts ? product_launch<64, kSwiglu, false>(a, st)
+                                                     : product_launch<192, kSwiglu, true>(a, st);
   return e == cudaSuccess ? MOE_OK : MOE_ECUDA;
 }
 

@@ -11,7 +11,7 @@
 // neighbouring columns of a row at a time, and for swiglu those 32 are one block of the result, its largest magnitude one warp-wide maximum.
 //
 // One persistent CTA per SM walks the tiles (rows of an expert innermost: neighbours share a weight tile in L2).  Roles: one thread issues TMA
-// (a stage is 256 columns of K: 128-byte rows, swizzled), two warps bring the stage's scale bytes through registers into the 512-byte
+// (a stage is 256 columns of K: 128-byte rows, swizzled), four warps bring the stage's scale bytes through registers into the 512-byte
 // form that tcgen05.cp copies to TMEM (128 rows x 4 blocks), one thread copies them and issues the MMAs, eight warps are the epilogue.
 // Every wait is bounded; where one runs out the launch ends and what it has not computed is NaN.
 #include "moe_dev.cuh"
@@ -21,10 +21,10 @@
 namespace moe {
 namespace {
 
-// Warps 0-7 epilogue, 8 TMA, 9 MMA, 10 and 11 scales.  Three warps a quarter of the SM leave a thread 168 registers, four would leave 128; the
-// epilogue's two warpgroups then take 200 and the third keeps 104 (2 x 200 + 104 = 3 x 168).
-constexpr int kMxThreads = 384;
-constexpr int kTmaWarp = 8, kMmaWarp = 9, kScaleWarp = 10, kScaleWarps = 2;
+// Warps 0-7 epilogue, 8 TMA, 9 MMA, 12-15 scales (10 and 11 fill up a warpgroup).  A thread is launched with 128 registers; where tiles have many rows
+// the epilogue's two warpgroups take 168, that of TMA and MMA keeps 72, the scales' 104 (2 x 168 + 72 + 104 = 4 x 128).
+constexpr int kMxThreads = 512;
+constexpr int kTmaWarp = 8, kMmaWarp = 9, kScaleWarp = 12, kScaleWarps = 4;
 constexpr int kStageK = 256;                    // columns of K in a stage
 constexpr int kGroupK = 128;                    // ... in one 512-byte block of scales (4 a row)
 constexpr int kHalfRows = 128;                  // weight rows of an accumulator
@@ -155,26 +155,31 @@ __device__ __forceinline__ void tc_ld16(unsigned taddr, unsigned (&r)[16]) {
       : "memory");
 }
 
-// 16 bytes of a row's scales, `left` of which are there (the others are not used), by loads of vec bytes
-__device__ __forceinline__ uint4 load_scales(const unsigned char* p, int left, int vec) {
-  uint4 v = make_uint4(0u, 0u, 0u, 0u);
-  if (vec == 16) return __ldg(reinterpret_cast<const uint4*>(p));
-  if (vec == 8) {
-    const uint2 lo = __ldg(reinterpret_cast<const uint2*>(p));
-    v.x = lo.x;
-    v.y = lo.y;
-    if (left > 8) {
-      const uint2 hi = __ldg(reinterpret_cast<const uint2*>(p) + 1);
-      v.z = hi.x;
-      v.w = hi.y;
-    }
-    return v;
+// 32 bytes of a row's scales, `left` of which are there (the others are not used), by loads of vec bytes
+struct RowScales {
+  unsigned w[8];
+};
+__device__ __forceinline__ RowScales load_scales(const unsigned char* p, int left, int vec) {
+  RowScales v;
+  if (vec == 16) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (left > 16 * i) {
+        const uint4 q = __ldg(reinterpret_cast<const uint4*>(p) + i);
+        v.w[4 * i] = q.x; v.w[4 * i + 1] = q.y; v.w[4 * i + 2] = q.z; v.w[4 * i + 3] = q.w;
+      }
+  } else if (vec == 8) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (left > 8 * i) {
+        const uint2 q = __ldg(reinterpret_cast<const uint2*>(p) + i);
+        v.w[2 * i] = q.x; v.w[2 * i + 1] = q.y;
+      }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (left > 4 * i) v.w[i] = __ldg(reinterpret_cast<const unsigned*>(p) + i);
   }
-  const unsigned* w = reinterpret_cast<const unsigned*>(p);
-  v.x = __ldg(w);
-  if (left > 4) v.y = __ldg(w + 1);
-  if (left > 8) v.z = __ldg(w + 2);
-  if (left > 12) v.w = __ldg(w + 3);
   return v;
 }
 __device__ __forceinline__ void st_word(unsigned saddr, unsigned v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(saddr), "r"(v) : "memory"); }
@@ -299,7 +304,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
   const int n_stages = (a.K + kStageK - 1) / kStageK;
 
   if (warp < kTmaWarp) {
-    if (S::kRows > 96) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+    if (S::kRows > 96) asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
     const int quad = warp & 3, half = warp >> 2;
     unsigned k = 0;
     bool ok = true;
@@ -309,8 +314,8 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
       if (ok) ok = __all_sync(0xffffffffu, wait(&s.acc_full[buf], use & 1, &s.dead));
       tc_fence_after();
       const unsigned acc = tmem + buf * 2 * S::kRows + ((unsigned)quad << 21);      // this warp's 32 lanes
-      // Everything that is in the accumulator goes to registers first -- as bf16 for the plain product, for swiglu half of the rows as they
-      // are and half as silu(gate) up -- and the accumulator is handed back: rounding, quantising and storing run beside the next tile's MMAs.
+      // Everything that is in the accumulator goes to registers first -- as bf16 for the plain product, for swiglu the last rows as they
+      // are and the others as silu(gate) up -- and the accumulator is handed back: rounding, quantising and storing run beside the next tile's MMAs.
       const auto hand_back = [&] {
         tc_wait_ld();
         tc_fence_before();
@@ -380,7 +385,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
             }
           }
         };
-        constexpr int kMine = (S::kGroups + 1) / 2, kAsTheyAre = (kMine + 1) / 2, kFirst = kMine - kAsTheyAre;
+        constexpr int kMine = (S::kGroups + 1) / 2, kAsTheyAre = kMine < 3 ? 1 : 2, kFirst = kMine - kAsTheyAre;
         const int my_groups = (groups - half + 1) / 2;
         float v[kFirst > 0 ? kFirst : 1][16];
         unsigned gate[kAsTheyAre][16], up[kAsTheyAre][16];
@@ -430,8 +435,8 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
         else a.out_scales[p * (a.I / 32) + (c - a.I / 2)] = 0;
       }
     }
-  } else {
-    if (S::kRows > 96) asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+  } else if (warp < kScaleWarp) {
+    if (S::kRows > 96) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == kTmaWarp) {
       if (elect_one()) {
         unsigned n = 0;            // stages so far
@@ -507,81 +512,75 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
         while (!mbar_try(&s.drained, 0) && gtime_ns() - start < kWaitNs) {}
       }
       __syncwarp();
-    } else if (warp >= kScaleWarp) {
-      // A thread has two rows of every 128-row block, in the order that spreads a warp's stores over all banks: their four bytes of a group of
-      // 128 columns go to 16 (r % 32) + 4 (r / 32) of the group's block.  16 bytes of a row are two stages; those of the next two are on their
-      // way to registers meanwhile, whether or not their stages are free.
-      const int r0 = 32 * (lane & 3) + 8 * (warp - kScaleWarp) + (lane >> 2);      // and r0 + 16
-      const unsigned spot = (unsigned)(r0 & 31) * 16 + (unsigned)(r0 >> 5) * 4;
-      const int per_row = a.K / kMxBlock, n_pairs = (n_stages + 1) / 2;
-      const int vec = per_row % 16 == 0 ? 16 : per_row % 8 == 0 ? 8 : 4;
-      const int vec_w = (size_t)a.w_scales & (vec - 1) ? 4 : vec, vec_x = (size_t)a.x_scales & (vec - 1) ? 4 : vec;
-      constexpr int kBlocks = 2 + S::kRowBlocks;
-      struct Pair {
-        uint4 b[kBlocks][2];
-        int stages;                // 1 or 2; 0: there is no more
-      };
-      int t = unit, pair = 0;
-      Tile at{};
-      unsigned n = 0;
-      const auto fetch = [&](Pair& p) {
-        p.stages = 0;
-        if (t >= n_tiles) return;
-        if (pair == 0) at = tile_at<S::kRows>(s, a.E, t, kStep);
-        const unsigned char* w = a.w_scales + (size_t)at.expert * a.N * per_row + pair * 16;
-        const unsigned char* x = a.x_scales + (size_t)at.row0 * per_row + pair * 16;
+    }
+  } else {
+    if (S::kRows > 96) asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+    // A thread has one row of every 128-row block, in the order that spreads a warp's stores over all banks: its four bytes of a group of 128
+    // columns go to 16 (r % 32) + 4 (r / 32) of the group's block.  It loads a sector of 32 bytes, four stages, at a time; the next one
+    // is on its way to registers meanwhile, whether or not its stages are free.
+    const int r = 32 * (lane & 3) + 8 * (warp - kScaleWarp) + (lane >> 2);
+    const unsigned spot = (unsigned)(r & 31) * 16 + (unsigned)(r >> 5) * 4;
+    const int per_row = a.K / kMxBlock, n_quads = (n_stages + 3) / 4;
+    const int vec = per_row % 16 == 0 ? 16 : per_row % 8 == 0 ? 8 : 4;
+    const int vec_w = (size_t)a.w_scales & (vec - 1) ? 4 : vec, vec_x = (size_t)a.x_scales & (vec - 1) ? 4 : vec;
+    constexpr int kBlocks = 2 + S::kRowBlocks;
+    struct Quad {
+      RowScales b[kBlocks];
+      int stages;                // 1 to 4; 0: there is no more
+    };
+    int t = unit, quad = 0;
+    Tile at{};
+    unsigned n = 0;
+    const auto fetch = [&](Quad& p) {
+      p.stages = 0;
+      if (t >= n_tiles) return;
+      if (quad == 0) at = tile_at<S::kRows>(s, a.E, t, kStep);
+      const int left = per_row - quad * 32;
+      const unsigned char* w = a.w_scales + (size_t)at.expert * a.N * per_row + quad * 32;
+      const unsigned char* x = a.x_scales + (size_t)at.row0 * per_row + quad * 32;
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          const int r = r0 + 16 * q;
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {      // a weight row behind the last one: any other's scales (its products are not stored)
-            const int row = kSwiglu ? min(at.n0 + (int)rank * kHalfRows + r, a.I - 1) + b * a.I
-                                    : min(at.n0 + (b * kCtas + (int)rank) * kHalfRows + r, a.N - 1);
-            p.b[b][q] = load_scales(w + (size_t)row * per_row, per_row - pair * 16, vec_w);
-          }
-#pragma unroll
-          for (int b = 0; b < S::kRowBlocks; ++b)
-            p.b[2 + b][q] = load_scales(x + (size_t)min(b * 128 + r, at.rows - 1) * per_row, per_row - pair * 16, vec_x);
-        }
-        p.stages = min(2, n_stages - 2 * pair);
-        if (++pair == n_pairs) {
-          pair = 0;
-          t += n_units;
-        }
-      };
-      const auto put = [&](const Pair& p) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (h >= p.stages) break;
-          const unsigned slot = n % S::kStages, round = n / S::kStages;
-          if (round && !__all_sync(0xffffffffu, wait(&s.empty[slot], (round - 1) & 1, &s.dead))) return false;
-          const unsigned to = smem_u32(stages + slot * S::kStageBytes) + S::kWBytes + S::kXBytes + spot;
-#pragma unroll
-          for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-              const uint4& v = p.b[b][q];
-              st_word(to + b * kScaleBlock + 256 * q, h ? v.z : v.x);
-              st_word(to + (kBlocks + b) * kScaleBlock + 256 * q, h ? v.w : v.y);
-            }
-          fence_async_proxy_smem();
-          __syncwarp();
-          if (lane == 0) {
-            if (kPair) mbar_arrive_remote(map_to_cta(&s.landed[slot], 0));
-            else mbar_arrive(&s.landed[slot]);
-          }
-          ++n;
-        }
-        return true;
-      };
-      Pair even, odd;
-      fetch(even);
-      while (even.stages) {
-        fetch(odd);
-        if (!put(even) || !odd.stages) break;
-        fetch(even);
-        if (!put(odd)) break;
+      for (int b = 0; b < 2; ++b) {        // a weight row behind the last one: any other's scales (its products are not stored)
+        const int row = kSwiglu ? min(at.n0 + (int)rank * kHalfRows + r, a.I - 1) + b * a.I
+                                : min(at.n0 + (b * kCtas + (int)rank) * kHalfRows + r, a.N - 1);
+        p.b[b] = load_scales(w + (size_t)row * per_row, left, vec_w);
       }
+#pragma unroll
+      for (int b = 0; b < S::kRowBlocks; ++b) p.b[2 + b] = load_scales(x + (size_t)min(b * 128 + r, at.rows - 1) * per_row, left, vec_x);
+      p.stages = min(4, n_stages - 4 * quad);
+      if (++quad == n_quads) {
+        quad = 0;
+        t += n_units;
+      }
+    };
+    const auto put = [&](const Quad& p) {
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        if (h >= p.stages) break;
+        const unsigned slot = n % S::kStages, round = n / S::kStages;
+        if (round && !__all_sync(0xffffffffu, wait(&s.empty[slot], (round - 1) & 1, &s.dead))) return false;
+        const unsigned to = smem_u32(stages + slot * S::kStageBytes) + S::kWBytes + S::kXBytes + spot;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) {
+          st_word(to + b * kScaleBlock, p.b[b].w[2 * h]);
+          st_word(to + (kBlocks + b) * kScaleBlock, p.b[b].w[2 * h + 1]);
+        }
+        fence_async_proxy_smem();
+        __syncwarp();
+        if (lane == 0) {
+          if (kPair) mbar_arrive_remote(map_to_cta(&s.landed[slot], 0));
+          else mbar_arrive(&s.landed[slot]);
+        }
+        ++n;
+      }
+      return true;
+    };
+    Quad even, odd;
+    fetch(even);
+    while (even.stages) {
+      fetch(odd);
+      if (!put(even) || !odd.stages) break;
+      fetch(even);
+      if (!put(odd)) break;
     }
   }
   __syncwarp();

@@ -30,6 +30,8 @@ constexpr int kGroupK = 128;                    // ... in one 512-byte block of 
 constexpr int kHalfRows = 128;                  // weight rows of an accumulator
 constexpr int kScaleBlock = 512;
 constexpr int kBoxRows = 32;                    // rows of a TMA box of activations
+constexpr int kStorePitch = 2 * kHalfRows + 16;  // a row of 128 bf16 outputs on its way out; the 16 bytes spread eight rows over all banks
+constexpr int kStoreBuf = 16 * kStorePitch;
 constexpr unsigned long long kWaitNs = 2000000000ull;
 
 struct MxShared {
@@ -43,7 +45,7 @@ struct MxShared {
 
 // What depends on the rows of a tile.  Shared memory: stages of 32 KB weights, kRows * 128 bytes of rows and the scale blocks of both; TMEM: the
 // accumulators (two buffers of them where they fit) from column 0, the stages' scales behind.
-template <int kRows_, bool kPair>
+template <int kRows_, bool kSwiglu, bool kPair>
 struct Shape {
   static constexpr int kRows = kRows_;
   static constexpr int kRowBlocks = (kRows + 127) / 128;                      // 128-row blocks of row scales
@@ -54,7 +56,8 @@ struct Shape {
   static constexpr int kGroups = kRows / 16;                                  // groups of 16 columns, as the epilogue takes them
   static constexpr int kAccBufs = kRows <= 96 ? 2 : 1;
   static constexpr int kScaleCol0 = kAccBufs * 2 * kRows;
-  static constexpr int kFitSmem = (227 * 1024 - 1024 - (int)sizeof(MxShared)) / kStageBytes, kFitTmem = (512 - kScaleCol0) / kScaleCols;
+  static constexpr int kStoreBytes = kSwiglu ? 0 : 4 * kStoreBuf;
+  static constexpr int kFitSmem = (227 * 1024 - 1024 - (int)sizeof(MxShared) - kStoreBytes) / kStageBytes, kFitTmem = (512 - kScaleCol0) / kScaleCols;
   static constexpr int kStages = kFitSmem < kFitTmem ? kFitSmem : kFitTmem;
   static_assert(kStages >= 2, "stages");
   static_assert(kStages <= 8, "barriers");
@@ -219,33 +222,27 @@ __device__ __forceinline__ unsigned pack_bf16(unsigned lo, unsigned hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(lo), __uint_as_float(hi));
   return *reinterpret_cast<const unsigned*>(&v);
 }
-// 8 x 8 bf16 values over eight neighbouring lanes, lane i with column i as four pairs of rows: lane j gets row j.  Lane bit 0 changes places with
-// row bit 0 inside the pairs, then bits 1 and 2 with whole words.
-__device__ __forceinline__ uint4 transpose_bf16(const unsigned* v, int lane) {
-  unsigned q[4], lo[2], hi[2];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const unsigned own = v[i], other = __shfl_xor_sync(0xffffffffu, own, 1);
-    q[i] = __byte_perm(own, other, lane & 1 ? 0x3276u : 0x5410u);
-  }
-#pragma unroll
-  for (int m = 0; m < 2; ++m) {
-    const unsigned own = lane & 2 ? q[2 * m + 1] : q[2 * m];
-    const unsigned other = __shfl_xor_sync(0xffffffffu, lane & 2 ? q[2 * m] : q[2 * m + 1], 2);
-    lo[m] = lane & 2 ? other : own;
-    hi[m] = lane & 2 ? own : other;
-  }
-  const unsigned own0 = lane & 4 ? lo[1] : lo[0], own1 = lane & 4 ? hi[1] : hi[0];
-  const unsigned other0 = __shfl_xor_sync(0xffffffffu, lane & 4 ? lo[0] : lo[1], 4), other1 = __shfl_xor_sync(0xffffffffu, lane & 4 ? hi[0] : hi[1], 4);
-  return lane & 4 ? make_uint4(other0, other1, own0, own1) : make_uint4(own0, own1, other0, other1);
+// 16 TMEM lanes x 16 columns as fragments: for column group j (8 columns) thread i holds row i / 4, columns 8 j + 2 (i % 4) and + 1 in r[4 j],
+// r[4 j + 1], and the same columns of row i / 4 + 8 in r[4 j + 2], r[4 j + 3]
+__device__ __forceinline__ void tc_ld_frag16(unsigned taddr, unsigned (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr)
+               : "memory");
 }
+__device__ __forceinline__ void bulk_store(void* to, unsigned from, int bytes) {
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(to), "r"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 
 template <int kRows_, bool kSwiglu, bool kPair>
 __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_constant__ MxArgs a) {
-  using S = Shape<kRows_, kPair>;
+  using S = Shape<kRows_, kSwiglu, kPair>;
   extern __shared__ unsigned char raw[];
   unsigned char* stages = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
-  MxShared& s = *reinterpret_cast<MxShared*>(stages + S::kStages * S::kStageBytes);
+  unsigned char* store_bufs = stages + S::kStages * S::kStageBytes;
+  MxShared& s = *reinterpret_cast<MxShared*>(store_bufs + S::kStoreBytes);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   constexpr int kCtas = kPair ? 2 : 1;
   constexpr int kStep = (kSwiglu ? 1 : 2) * kHalfRows * kCtas;     // output columns of a tile
@@ -306,7 +303,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
   if (warp < kTmaWarp) {
     if (S::kRows > 96) asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
     const int quad = warp & 3, half = warp >> 2;
-    unsigned k = 0;
+    unsigned k = 0, stored = 0;  // tiles, groups of outputs so far
     bool ok = true;
     for (int t = unit; t < n_tiles; t += n_units, ++k) {
       const Tile at = tile_at<S::kRows>(s, a.E, t, kStep);
@@ -328,34 +325,52 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
       const int groups = (at.rows + 15) / 16;
       if (!kSwiglu) {            // warps 0-3 have the first accumulator, 4-7 the second
         const unsigned mine = acc + half * S::kRows;
-        const int col = at.n0 + (half * kCtas + (int)rank) * kHalfRows + quad * 32 + lane, col8 = col - lane + (lane >> 3) * 8;
-        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + (size_t)at.row0 * a.N;
-        unsigned v[S::kGroups][8];
+        const int col0 = at.n0 + (half * kCtas + (int)rank) * kHalfRows;      // of these four warps' 128 output columns
+        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + (size_t)at.row0 * a.N + col0;
+        unsigned v[S::kGroups][8];   // a group as eight 8 x 8 fragments: [4 j + m] rows 8 j .. of the group, columns 8 m ..
 #pragma unroll
         for (int g = 0; g < S::kGroups; ++g) {
           if (g >= groups) break;
-          unsigned raw[16];
-          tc_ld16(mine + 16 * g, raw);
+          unsigned lo[8], hi[8];
+          tc_ld_frag16(mine + 16 * g, lo);
+          tc_ld_frag16(mine + 16 * g + (16u << 16), hi);
           tc_wait_ld();
 #pragma unroll
-          for (int j = 0; j < 8; ++j) v[g][j] = ok ? pack_bf16(raw[2 * j], raw[2 * j + 1]) : 0x7fff7fffu;
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+              v[g][4 * j + m] = ok ? pack_bf16(lo[4 * j + 2 * m], lo[4 * j + 2 * m + 1]) : 0x7fff7fffu;
+              v[g][4 * j + 2 + m] = ok ? pack_bf16(hi[4 * j + 2 * m], hi[4 * j + 2 * m + 1]) : 0x7fff7fffu;
+            }
         }
         hand_back();
+        if (a.wide) {            // transposed into shared memory, 16 rows of 256 bytes at a time, and out by bulk copies
+          const int bytes = min(2 * kHalfRows, 2 * (a.N - col0));
 #pragma unroll
-        for (int g = 0; g < S::kGroups; ++g) {
-          if (g >= groups) break;
+          for (int g = 0; g < S::kGroups; ++g) {
+            if (g >= groups) break;
+            const unsigned buf_at = smem_u32(store_bufs) + (2 * half + (stored & 1)) * kStoreBuf;
+            const unsigned to = buf_at + (lane & 7) * kStorePitch + quad * 64 + (lane >> 3) * 16;
 #pragma unroll
-          for (int j0 = 0; j0 < 16; j0 += 8) {
-            const int c = 16 * g + j0;
-            if (a.wide) {        // eight neighbouring columns of a row a lane: stores of 2 bytes took the down product 1.3 times as long
-              const uint4 w = transpose_bf16(&v[g][j0 / 2], lane);
-              const int row = c + (lane & 7);
-              if (row < at.rows && col8 < a.N) *reinterpret_cast<uint4*>(out + (size_t)row * a.N + col8) = w;
-            } else {
+            for (int j = 0; j < 2; ++j) st_matrix4_trans(to + 8 * j * kStorePitch, v[g][4 * j], v[g][4 * j + 1], v[g][4 * j + 2], v[g][4 * j + 3]);
+            fence_async_proxy_smem();
+            bulk_wait_read();    // the copies out of the other buffer, which the next group is written to, have read it
+            asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");
+            const int row = 4 * quad + lane;
+            if (lane < 4 && 16 * g + row < at.rows && bytes > 0) bulk_store(out + (size_t)(16 * g + row) * a.N, buf_at + row * kStorePitch, bytes);
+            bulk_commit();
+            ++stored;
+          }
+        } else {
 #pragma unroll
-              for (int j = 0; j < 8; ++j)
-                if (c + j < at.rows && col < a.N)
-                  reinterpret_cast<unsigned short*>(out)[(size_t)(c + j) * a.N + col] = (unsigned short)(v[g][(j0 + j) / 2] >> (16 * (j & 1)));
+          for (int g = 0; g < S::kGroups; ++g) {
+            if (g >= groups) break;
+#pragma unroll
+            for (int f = 0; f < 8; ++f) {
+              const int row = 16 * g + 8 * (f >> 2) + 2 * (lane & 3), c = quad * 32 + 8 * (f & 3) + (lane >> 2);
+              unsigned short* p = reinterpret_cast<unsigned short*>(out) + (size_t)row * a.N + c;
+              if (col0 + c < a.N && row < at.rows) *p = (unsigned short)v[g][f];
+              if (col0 + c < a.N && row + 1 < at.rows) p[a.N] = (unsigned short)(v[g][f] >> 16);
             }
           }
         }
@@ -424,6 +439,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
           }
       }
     }
+    asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     // rows that belong to no expert: zeros, by the epilogue warps of the whole grid
     const size_t width = kSwiglu ? (size_t)a.I / 32 * 17 : (size_t)a.N;
     const int lo = s.first_row[0], hi = max(s.first_row[a.E], lo), none = lo + (a.R - hi);
@@ -621,8 +637,8 @@ bool encode_codes(CUtensorMap* out, const void* base, int bytes, int rows, int p
 
 template <int kRows, bool kSwiglu, bool kPair>
 cudaError_t product_launch(const MxArgs& a, cudaStream_t stream) {
-  using S = Shape<kRows, kPair>;
-  constexpr size_t smem = 1024 + (size_t)S::kStages * S::kStageBytes + sizeof(MxShared);
+  using S = Shape<kRows, kSwiglu, kPair>;
+  constexpr size_t smem = 1024 + (size_t)S::kStages * S::kStageBytes + S::kStoreBytes + sizeof(MxShared);
   static_assert(smem <= 227 * 1024, "shared memory");
   constexpr int kCtas = kPair ? 2 : 1;
   auto* kernel = mx_product_kernel<kRows, kSwiglu, kPair>;

@@ -688,9 +688,19 @@ int product(const void* codes, const void* scales, const void* w_codes, const vo
   a.R = n_rows; a.E = n_experts; a.N = n; a.K = K; a.I = n / 2;
   a.wide = n % 8 == 0 && (reinterpret_cast<uintptr_t>(out) & 15) == 0;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = n_rows <= 24ll * n_experts   ? product_launch<32, kSwiglu, false>(a, st)
-                        : n_rows <= 64ll * n_experts ? product_launch<64, kSwiglu, false>(a, st)
-                                                     : product_launch<192, kSwiglu, true>(a, st);
+  // The tile's height goes by the rows that an expert gets on average (the host does not know more).  Two buffers of 64 or 96 columns let the epilogue of
+  // a tile run beside the next one's MMAs; 192 columns take the weights from L2 half as often.  us, 32 experts, K 4096, inter 1792 (gate/up, down):
+  //   rows an expert     32          64          128         256         512          1024         2048
+  //   64 rows            54.5, 28.4  57.3, 33.8  74.8, 43.3  122.6, 70.1
+  //   96 rows            54.3, 28.9  56.3, 31.2  72.2, 39.2  98.3, 55.3  186, 101     336, 184     652, 358
+  //   192 rows           58.6, 32.8  64.0, 35.6  71.4, 39.7  110, 60.2   156, 92.9    329, 168     552, 304
+  //   192 rows, pairs    61.2, 34.8  64.5, 36.9  72.7, 42.0  98.0, 63.2  148, 93.4    265, 175     473, 313
+  // 64 experts, K 2048, inter 768, uneven (Zipf 0.8), 64 and 96 rows: 24.3, 14.3 and 25.3, 16.1 for 32 rows an expert, 35.8, 23.3 and 29.9, 25.1 for 96.
+  // Tiles of 32 rows gained 2-8 % below 16 rows an expert, 0.2-0.5 us of a launch of 6-20, and are left out.
+  const bool few = n_rows <= 64ll * n_experts, many = n_rows > 256ll * n_experts;
+  const cudaError_t e = few    ? product_launch<64, kSwiglu, false>(a, st)
+                        : many ? product_launch<192, kSwiglu, kSwiglu>(a, st)
+                               : product_launch<96, kSwiglu, false>(a, st);
   return e == cudaSuccess ? MOE_OK : MOE_ECUDA;
 }
 

@@ -12,7 +12,8 @@
 // or written for it; a row whose entry of s2f is outside [0, R) belongs to no token and is set to zero where rows are the output.
 //
 // Device time, bf16, and the rate of the bytes that have to move (a plain copy runs at 6.5 TB/s): 8 192 tokens x 8 slots x 4 096 columns sort 98 us
-// (6.2 TB/s), its gradient 89 us (6.8); 4 096 x 8 x 6 144 merge 68 us (6.6), its gradient 133 us (6.4); one token 2.2-2.5 us, launch included.
+// (6.2 TB/s), its gradient 89 us (6.8); 4 096 x 8 x 6 144 merge 68 us (6.6), its gradient 136 us (6.3); 16 384 x 2 x 4 096 64 and 122 us; one token
+// 2.2-2.5 us, launch included.  8 192 x 8 rows of odd width (3 001) move at 2.3-4.4 TB/s: accesses of two bytes.
 #include <cuda_fp16.h>
 
 #include "moe_dev.cuh"
@@ -125,6 +126,25 @@ template <> struct Vec<__nv_bfloat16, 8> {
   static __device__ __forceinline__ void unpack(const Raw& r, float (&v)[8]) { two(r.x, v[0], v[1]); two(r.y, v[2], v[3]); two(r.z, v[4], v[5]); two(r.w, v[6], v[7]); }
   static __device__ __forceinline__ Raw pack(const float (&v)[8]) { return make_uint4(one(v[0], v[1]), one(v[2], v[3]), one(v[4], v[5]), one(v[6], v[7])); }
 };
+// two elements: rows that are aligned to two only
+template <> struct Vec<float, 2> {
+  using Raw = float2;
+  static __device__ __forceinline__ Raw zero() { return make_float2(0.f, 0.f); }
+  static __device__ __forceinline__ void unpack(const Raw& r, float (&v)[2]) { v[0] = r.x; v[1] = r.y; }
+  static __device__ __forceinline__ Raw pack(const float (&v)[2]) { return make_float2(v[0], v[1]); }
+};
+template <> struct Vec<__half, 2> {
+  using Raw = unsigned;
+  static __device__ __forceinline__ Raw zero() { return 0u; }
+  static __device__ __forceinline__ void unpack(Raw r, float (&v)[2]) { Vec<__half, 8>::two(r, v[0], v[1]); }
+  static __device__ __forceinline__ Raw pack(const float (&v)[2]) { return Vec<__half, 8>::one(v[0], v[1]); }
+};
+template <> struct Vec<__nv_bfloat16, 2> {
+  using Raw = unsigned;
+  static __device__ __forceinline__ Raw zero() { return 0u; }
+  static __device__ __forceinline__ void unpack(Raw r, float (&v)[2]) { Vec<__nv_bfloat16, 8>::two(r, v[0], v[1]); }
+  static __device__ __forceinline__ Raw pack(const float (&v)[2]) { return Vec<__nv_bfloat16, 8>::one(v[0], v[1]); }
+};
 template <> struct Vec<float, 1> {
   using Raw = float;
   static __device__ __forceinline__ Raw zero() { return 0.f; }
@@ -145,95 +165,114 @@ template <> struct Vec<__nv_bfloat16, 1> {
 };
 
 // ------------------------------------------------------------------ merge, and the gradient of sort (kWeights = false)
-// A thread owns kV columns of a token and has the rows of eight slots in flight; a slot without a row adds 0.
-template <class E, int kV, bool kWeights>
-__global__ void __launch_bounds__(kRowThreads, 4)
+// A thread owns kPer times kV columns of a token and has kSlots of its rows in flight at a time; a slot without a row adds 0.
+template <class E, int kV, int kSlots, int kPer, bool kWeights>
+__global__ void __launch_bounds__(kRowThreads, kPer > 1 && kV > 1 ? 3 : 4)
 merge_rows_kernel(const E* __restrict__ rows, long long stride, const float* __restrict__ w, const int* __restrict__ f2s,
                   E* __restrict__ y, int T, int k, int H, Walk walk) {
   grid_dep_wait();
   using V = Vec<E, kV>;
-  const int t = my_token(walk), c = my_column(walk, 1) * kV;
+  const int t = my_token(walk), c = my_column(walk, kPer) * kV, step = kV << walk.tpt_log2;
   if (t >= T || c >= H) return;
   const unsigned R = (unsigned)T * (unsigned)k;
   const E* from = rows + c;
-  float acc[kV];
+  float acc[kPer][kV];
 #pragma unroll
-  for (int i = 0; i < kV; ++i) acc[i] = 0.f;
-  for (int j0 = 0; j0 < k; j0 += 8) {
-    typename V::Raw d[8];
-    float wj[8];
+  for (int i = 0; i < kPer; ++i)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int j = j0 + i;
-      const unsigned p = j < k ? (unsigned)f2s[(size_t)t * k + j] : R;
-      d[i] = V::zero();
-      wj[i] = 0.f;
-      if (p < R) {
-        d[i] = *reinterpret_cast<const typename V::Raw*>(from + p * stride);
-        if (kWeights) wj[i] = w[(size_t)t * k + j];
+    for (int n = 0; n < kV; ++n) acc[i][n] = 0.f;
+  for (int j0 = 0; j0 < k; j0 += kSlots) {
+    typename V::Raw d[kSlots][kPer];
+    unsigned p[kSlots];
+    float wj[kSlots];
+#pragma unroll
+    for (int b = 0; b < kSlots; ++b) p[b] = j0 + b < k ? (unsigned)f2s[(size_t)t * k + j0 + b] : R;
+#pragma unroll
+    for (int b = 0; b < kSlots; ++b) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        d[b][i] = V::zero();
+        if (p[b] < R && c + i * step < H) d[b][i] = *reinterpret_cast<const typename V::Raw*>(from + p[b] * stride + i * step);
       }
+      wj[b] = 0.f;
+      if (kWeights && p[b] < R) wj[b] = w[(size_t)t * k + j0 + b];
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float v[kV];
-      V::unpack(d[i], v);
+    for (int b = 0; b < kSlots; ++b)
 #pragma unroll
-      for (int n = 0; n < kV; ++n) acc[n] = kWeights ? fmaf(wj[i], v[n], acc[n]) : acc[n] + v[n];
-    }
+      for (int i = 0; i < kPer; ++i) {
+        float v[kV];
+        V::unpack(d[b][i], v);
+#pragma unroll
+        for (int n = 0; n < kV; ++n) acc[i][n] = kWeights ? fmaf(wj[b], v[n], acc[i][n]) : acc[i][n] + v[n];
+      }
   }
-  *reinterpret_cast<typename V::Raw*>(y + (size_t)t * H + c) = V::pack(acc);
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+    if (c + i * step < H) *reinterpret_cast<typename V::Raw*>(y + (size_t)t * H + c + i * step) = V::pack(acc[i]);
 }
 
 // ------------------------------------------------------------------ gradient of merge
-// A block owns a token: its threads share the columns, every one of them keeps the partial dot products of eight slots, and the block adds
-// them up in a fixed order.  dy is read once for eight slots, each row of `rows` once, each row of drows written once.
-constexpr int kGradMaxThreads = 256;
-template <class E> constexpr int kGradBlocks = 2;                    // blocks an SM: the third would cost fp16 and fp32 spilled registers
-template <> constexpr int kGradBlocks<__nv_bfloat16> = 3;
-template <class E, int kV>
-__global__ void __launch_bounds__(kGradMaxThreads, kGradBlocks<E>)
+// A group of 32 to 256 threads owns a token: its threads share the columns, every one of them keeps the partial dot products of kSlots slots,
+// and the group adds them up in a fixed order.  Each row of `rows` is read once and each row of drows written once; dy is read once for kSlots
+// slots (from L1 again for the next ones).
+template <class E, int kV, int kSlots, int kPer>
+__global__ void __launch_bounds__(kRowThreads, 4)
 merge_grad_kernel(const E* __restrict__ dy, long long dy_stride, const E* __restrict__ rows, long long stride, const float* __restrict__ w,
-                  const int* __restrict__ s2f, const int* __restrict__ f2s, E* __restrict__ drows, float* __restrict__ dw, int k, int H) {
+                  const int* __restrict__ s2f, const int* __restrict__ f2s, E* __restrict__ drows, float* __restrict__ dw, int T, int k, int H,
+                  int group) {
   grid_dep_wait();
   using V = Vec<E, kV>;
   using Raw = typename V::Raw;
-  __shared__ float part[kGradMaxThreads / 32][8];
-  const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_warps = blockDim.x >> 5;
-  const unsigned R = gridDim.x * (unsigned)k;
-  for (int j0 = 0; j0 < k; j0 += 8) {
-    unsigned p[8];
-    float wj[8], dot[8];
+  __shared__ float part[kRowThreads / 32][kSlots];
+  const int groups = kRowThreads / group, tid = threadIdx.x & (group - 1), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int t = blockIdx.x * groups + (int)threadIdx.x / group, step = group * kV;
+  const bool on = t < T;                               // (a group without a token takes part in the barriers)
+  const unsigned R = (unsigned)T * (unsigned)k;
+  const E* g_row = dy + t * dy_stride;
+  for (int j0 = 0; j0 < k; j0 += kSlots) {
+    unsigned p[kSlots];
+    float wj[kSlots], dot[kSlots];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int j = j0 + i;
-      p[i] = j < k ? (unsigned)f2s[(size_t)t * k + j] : R;
-      wj[i] = p[i] < R ? w[(size_t)t * k + j] : 0.f;
-      dot[i] = 0.f;
+    for (int b = 0; b < kSlots; ++b) {
+      const int j = j0 + b;
+      p[b] = on && j < k ? (unsigned)f2s[(size_t)t * k + j] : R;
+      wj[b] = p[b] < R ? w[(size_t)t * k + j] : 0.f;
+      dot[b] = 0.f;
     }
-    for (int c = tid * kV; c < H; c += blockDim.x * kV) {
-      const Raw graw = *reinterpret_cast<const Raw*>(dy + t * dy_stride + c);
-      Raw d[8];
+    for (int c = tid * kV; on && c < H; c += kPer * step) {
+      Raw graw[kPer], d[kSlots][kPer];
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (p[i] < R) d[i] = *reinterpret_cast<const Raw*>(rows + p[i] * stride + c);
-      float g[kV];
-      V::unpack(graw, g);
+      for (int i = 0; i < kPer; ++i)
+        if (c + i * step < H) graw[i] = *reinterpret_cast<const Raw*>(g_row + c + i * step);
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (p[i] < R) {
-          float v[kV], out[kV];
-          V::unpack(d[i], v);
+      for (int b = 0; b < kSlots; ++b)
 #pragma unroll
-          for (int n = 0; n < kV; ++n) {
-            dot[i] = fmaf(g[n], v[n], dot[i]);
-            out[n] = wj[i] * g[n];
-          }
-          *reinterpret_cast<Raw*>(drows + (size_t)p[i] * H + c) = V::pack(out);
+        for (int i = 0; i < kPer; ++i)
+          if (p[b] < R && c + i * step < H) d[b][i] = *reinterpret_cast<const Raw*>(rows + p[b] * stride + c + i * step);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+        if (c + i * step < H) {
+          float g[kV];
+          V::unpack(graw[i], g);
+#pragma unroll
+          for (int b = 0; b < kSlots; ++b)
+            if (p[b] < R) {
+              float v[kV], out[kV];
+              V::unpack(d[b][i], v);
+#pragma unroll
+              for (int n = 0; n < kV; ++n) {
+                dot[b] = fmaf(g[n], v[n], dot[b]);
+                out[n] = wj[b] * g[n];
+              }
+              *reinterpret_cast<Raw*>(drows + (size_t)p[b] * H + c + i * step) = V::pack(out);
+            }
         }
     }
-    // eight sums over 32 lanes: lanes halve the set of slots that they keep while they add, nine exchanges instead of forty
+    // kSlots sums over 32 lanes: lanes halve the set of slots that they keep while they add
+    int b = 16;
 #pragma unroll
-    for (int s = 4, b = 16; s >= 1; s >>= 1, b >>= 1) {
+    for (int s = kSlots / 2; s >= 1; s >>= 1, b >>= 1) {
       const bool high = lane & b;
 #pragma unroll
       for (int i = 0; i < s; ++i) {
@@ -241,20 +280,26 @@ merge_grad_kernel(const E* __restrict__ dy, long long dy_stride, const E* __rest
         dot[i] = keep + __shfl_xor_sync(0xffffffffu, give, b);
       }
     }
-    dot[0] += __shfl_xor_sync(0xffffffffu, dot[0], 2);
-    dot[0] += __shfl_xor_sync(0xffffffffu, dot[0], 1);
-    if (j0) __syncthreads();                          // the sums of the eight slots before have been read
-    if ((lane & 3) == 0) part[warp][lane >> 2] = dot[0];
+    constexpr int kSame = 32 / kSlots;                // neighbouring lanes that now have the same slot
+#pragma unroll
+    for (int m = kSame / 2; m >= 1; m >>= 1) dot[0] += __shfl_xor_sync(0xffffffffu, dot[0], m);
+    const bool first = (lane & (kSame - 1)) == 0;     // lane kSame * b has the sum of slot b
+    if (group == 32) {
+      if (on && first && j0 + lane / kSame < k) dw[(size_t)t * k + j0 + lane / kSame] = dot[0];      // 0 for a slot that names no row
+      continue;
+    }
+    if (j0) __syncthreads();                          // the sums of the slots before have been read
+    if (first) part[warp][lane / kSame] = dot[0];
     __syncthreads();
-    if (tid < 8 && j0 + tid < k) {
+    if (on && tid < kSlots && j0 + tid < k) {
       float sum = 0.f;
-      for (int i = 0; i < n_warps; ++i) sum += part[i][tid];
-      dw[(size_t)t * k + j0 + tid] = sum;             // 0 for a slot that names no row
+      for (int i = 0; i < group / 32; ++i) sum += part[warp + i][tid];    // (tid < 32: the group's first warp)
+      dw[(size_t)t * k + j0 + tid] = sum;
     }
   }
-  for (int j = 0; j < k; ++j)                         // rows that belong to no token
+  for (int j = 0; on && j < k; ++j)                   // rows that belong to no token
     if ((unsigned)s2f[(size_t)t * k + j] >= R)
-      for (int c = tid * kV; c < H; c += blockDim.x * kV) *reinterpret_cast<Raw*>(drows + ((size_t)t * k + j) * H + c) = V::zero();
+      for (int c = tid * kV; c < H; c += step) *reinterpret_cast<Raw*>(drows + ((size_t)t * k + j) * H + c) = V::zero();
 }
 
 // ------------------------------------------------------------------ host
@@ -282,13 +327,15 @@ int widest(unsigned long long all) {
 }
 unsigned long long bits(const void* p) { return reinterpret_cast<uintptr_t>(p); }
 
+constexpr long long kFillThreads = 148ll * 2048 * 4;     // accesses that keep every thread of the GPU busy with four
+
 template <int kBytes>
 cudaError_t sort_launch(const void* x, long long x_stride_bytes, void* xs, const int* s2f, const int* f2s, int T, int k, long long row_bytes,
                         cudaStream_t stream) {
   using U = typename Unit<kBytes>::type;
   const long long units = row_bytes / kBytes;
   // Four accesses a thread where there are rows enough to fill the GPU, else one: shorter chains and more SMs at work.
-  const bool few = (long long)T * units < 148ll * 2048 * 4;
+  const bool few = (long long)T * units < kFillThreads;
   const Walk w = walk_of(units, few ? 1 : 4);
   const long long blocks = blocks_of(w, T);
   if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
@@ -296,28 +343,48 @@ cudaError_t sort_launch(const void* x, long long x_stride_bytes, void* xs, const
                       x_stride_bytes / kBytes, static_cast<U*>(xs), s2f, f2s, T, k, (int)units, w);
 }
 
+template <class E, int kV, int kSlots, int kPer, bool kWeights>
+cudaError_t merge_launch_as(const void* rows, long long stride, const float* w, const int* f2s, void* y, int T, int k, int H, cudaStream_t stream) {
+  const Walk walk = walk_of(H / kV, kPer);
+  const long long blocks = blocks_of(walk, T);
+  if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
+  return launch_after(merge_rows_kernel<E, kV, kSlots, kPer, kWeights>, (int)blocks, kRowThreads, 0, stream, static_cast<const E*>(rows), stride, w,
+                      f2s, static_cast<E*>(y), T, k, H, walk);
+}
 template <class E, bool kWeights>
 cudaError_t merge_launch(const void* rows, long long stride, const float* w, const int* f2s, void* y, int T, int k, int H, cudaStream_t stream) {
   constexpr int kV = 16 / sizeof(E);
-  const bool wide = widest(bits(rows) | bits(y) | (unsigned long long)stride * sizeof(E) | (unsigned long long)H * sizeof(E)) == 16;
-  const Walk walk = walk_of(wide ? H / kV : H, 1);
-  const long long blocks = blocks_of(walk, T);
-  if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
-  return launch_after(wide ? merge_rows_kernel<E, kV, kWeights> : merge_rows_kernel<E, 1, kWeights>, (int)blocks, kRowThreads, 0, stream,
-                      static_cast<const E*>(rows), stride, w, f2s, static_cast<E*>(y), T, k, H, walk);
+  const int access = widest(bits(rows) | bits(y) | (unsigned long long)stride * sizeof(E) | (unsigned long long)H * sizeof(E)) / (int)sizeof(E);
+  const int v = access >= kV ? kV : access >= 2 ? 2 : 1;
+  // Few columns: one access a slot and thread, so that more threads are at work.  Else about 8 rows' worth of 16 bytes in flight a thread, whatever k is and
+  // as near to it as narrow accesses come: 16 384 x 2 x 4 096 bf16 110 us with one access a slot, 67 with four.
+  const bool few = (long long)T * (H / v) < kFillThreads;
+  const auto launch = v == 1   ? (few ? merge_launch_as<E, 1, 8, 1, kWeights> : merge_launch_as<E, 1, 8, 4, kWeights>)
+                      : v == 2 ? (few ? merge_launch_as<E, 2, 8, 1, kWeights> : merge_launch_as<E, 2, 8, sizeof(E) == 4 ? 2 : 4, kWeights>)
+                      : few || k > 4 ? merge_launch_as<E, kV, 8, 1, kWeights>
+                      : k > 2        ? merge_launch_as<E, kV, 4, 2, kWeights>
+                                     : merge_launch_as<E, kV, 2, 4, kWeights>;
+  return launch(rows, stride, w, f2s, y, T, k, H, stream);
 }
 
+template <class E, int kV, int kSlots, int kPer>
+cudaError_t grad_launch_as(const void* dy, long long dy_stride, const void* rows, long long stride, const float* w, const int* s2f, const int* f2s,
+                           void* drows, float* dw, int T, int k, int H, cudaStream_t stream) {
+  int group = 32;
+  while (group < kRowThreads && group * kPer < H / kV) group *= 2;
+  const int groups = kRowThreads / group;
+  return launch_after(merge_grad_kernel<E, kV, kSlots, kPer>, (T + groups - 1) / groups, kRowThreads, 0, stream, static_cast<const E*>(dy), dy_stride,
+                      static_cast<const E*>(rows), stride, w, s2f, f2s, static_cast<E*>(drows), dw, T, k, H, group);
+}
 template <class E>
 cudaError_t grad_launch(const void* dy, long long dy_stride, const void* rows, long long stride, const float* w, const int* s2f, const int* f2s,
                         void* drows, float* dw, int T, int k, int H, cudaStream_t stream) {
   constexpr int kV = 16 / sizeof(E);
-  const bool wide = widest(bits(dy) | bits(rows) | bits(drows) | (unsigned long long)dy_stride * sizeof(E) |
-                           (unsigned long long)stride * sizeof(E) | (unsigned long long)H * sizeof(E)) == 16;
-  const int units = wide ? H / kV : H;
-  int threads = 32;
-  while (threads < kGradMaxThreads && threads < units) threads *= 2;
-  return launch_after(wide ? merge_grad_kernel<E, kV> : merge_grad_kernel<E, 1>, T, threads, 0, stream, static_cast<const E*>(dy), dy_stride,
-                      static_cast<const E*>(rows), stride, w, s2f, f2s, static_cast<E*>(drows), dw, k, H);
+  const int access = widest(bits(dy) | bits(rows) | bits(drows) | (unsigned long long)dy_stride * sizeof(E) | (unsigned long long)stride * sizeof(E) |
+                            (unsigned long long)H * sizeof(E)) / (int)sizeof(E);
+  const auto launch = access >= kV ? (k > 2 ? grad_launch_as<E, kV, 4, 1> : grad_launch_as<E, kV, 2, 2>)
+                      : access >= 2 ? grad_launch_as<E, 2, 4, 2> : grad_launch_as<E, 1, 4, 4>;
+  return launch(dy, dy_stride, rows, stride, w, s2f, f2s, drows, dw, T, k, H, stream);
 }
 
 template <bool kWeights>

@@ -230,14 +230,18 @@ merge_grad_kernel(const E* __restrict__ dy, long long dy_stride, const E* __rest
   const bool on = t < T;                               // (a group without a token takes part in the barriers)
   const unsigned R = (unsigned)T * (unsigned)k;
   const E* g_row = dy + t * dy_stride;
+  // lane j has slot j, and row t k + j of the result to look after
+  const size_t mine = (size_t)t * k + lane;
+  const unsigned my_row = on && lane < k ? (unsigned)f2s[mine] : R;
+  const float my_w = my_row < R ? w[mine] : 0.f;
+  unsigned lost = __ballot_sync(0xffffffffu, on && lane < k && (unsigned)s2f[mine] >= R);
   for (int j0 = 0; j0 < k; j0 += kSlots) {
     unsigned p[kSlots];
     float wj[kSlots], dot[kSlots];
 #pragma unroll
     for (int b = 0; b < kSlots; ++b) {
-      const int j = j0 + b;
-      p[b] = on && j < k ? (unsigned)f2s[(size_t)t * k + j] : R;
-      wj[b] = p[b] < R ? w[(size_t)t * k + j] : 0.f;
+      p[b] = __shfl_sync(0xffffffffu, my_row, j0 + b);          // (lanes from k on have none; j0 + b < 32)
+      wj[b] = __shfl_sync(0xffffffffu, my_w, j0 + b);
       dot[b] = 0.f;
     }
     for (int c = tid * kV; on && c < H; c += kPer * step) {
@@ -297,9 +301,8 @@ merge_grad_kernel(const E* __restrict__ dy, long long dy_stride, const E* __rest
       dw[(size_t)t * k + j0 + tid] = sum;
     }
   }
-  for (int j = 0; on && j < k; ++j)                   // rows that belong to no token
-    if ((unsigned)s2f[(size_t)t * k + j] >= R)
-      for (int c = tid * kV; c < H; c += step) *reinterpret_cast<Raw*>(drows + ((size_t)t * k + j) * H + c) = V::zero();
+  for (; lost; lost &= lost - 1)                      // rows that belong to no token
+    for (int c = tid * kV; c < H; c += step) *reinterpret_cast<Raw*>(drows + ((size_t)t * k + (__ffs(lost) - 1)) * H + c) = V::zero();
 }
 
 // ------------------------------------------------------------------ host

@@ -13,6 +13,8 @@
 // One persistent CTA per SM walks the tiles (rows of an expert innermost: neighbours share a weight tile in L2).  Roles: one thread issues TMA
 // (a stage is 256 columns of K: 128-byte rows, swizzled), four warps bring the stage's scale bytes through registers into the 512-byte
 // form that tcgen05.cp copies to TMEM (128 rows x 4 blocks), one thread copies them and issues the MMAs, eight warps are the epilogue.
+// Weights that one tile alone reads leave L2 first, and L2 fetches 256 bytes of a weight row at a time, two stages: 800 rows of 128 experts, the
+// weight stream, 166 -> 152 us (gate/up, K 4096) and 85 -> 75 (down, K 1792), 6.6 TB/s.
 // Every wait is bounded; where one runs out the launch ends and what it has not computed is NaN.
 #include "moe_dev.cuh"
 #include "moe_mx.cuh"
@@ -136,14 +138,14 @@ __device__ __forceinline__ void tma_2d(unsigned dst, const CUtensorMap* m, int x
                  : "memory");
 }
 template <bool kPair>
-__device__ __forceinline__ void tma_3d(unsigned dst, const CUtensorMap* m, int x, int y, int z, unsigned bar) {
+__device__ __forceinline__ void tma_3d(unsigned dst, const CUtensorMap* m, int x, int y, int z, unsigned bar, unsigned long long policy) {
   if (kPair)
-    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
-                 "l"(reinterpret_cast<unsigned long long>(m)), "r"(x), "r"(y), "r"(z), "r"(bar)
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4}], [%5], %6;"
+                 ::"r"(dst), "l"(reinterpret_cast<unsigned long long>(m)), "r"(x), "r"(y), "r"(z), "r"(bar), "l"(policy)
                  : "memory");
   else
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
-                 "l"(reinterpret_cast<unsigned long long>(m)), "r"(x), "r"(y), "r"(z), "r"(bar)
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4}], [%5], %6;"
+                 ::"r"(dst), "l"(reinterpret_cast<unsigned long long>(m)), "r"(x), "r"(y), "r"(z), "r"(bar), "l"(policy)
                  : "memory");
 }
 __device__ __forceinline__ void expect_tx(unsigned bar, unsigned bytes) {
@@ -189,6 +191,7 @@ __device__ __forceinline__ void st_word(unsigned saddr, unsigned v) { asm volati
 
 struct Tile {
   int expert, row0, rows, n0;    // n0: first weight row (swiglu: first gate row)
+  bool alone;                    // the expert's only tile of these weights
 };
 template <int kRows>
 __device__ __forceinline__ Tile tile_at(const MxShared& s, int E, int t, int n_step) {
@@ -199,7 +202,7 @@ __device__ __forceinline__ Tile tile_at(const MxShared& s, int E, int t, int n_s
   }
   const int rows = s.rows(lo), m_tiles = (rows + kRows - 1) / kRows, local = t - s.first_tile[lo];
   const int n = local / m_tiles, m = local - n * m_tiles;
-  return Tile{lo, s.first_row[lo] + m * kRows, min(kRows, rows - m * kRows), n * n_step};
+  return Tile{lo, s.first_row[lo] + m * kRows, min(kRows, rows - m * kRows), n * n_step, m_tiles == 1};
 }
 
 __device__ __forceinline__ float rcp_approx(float v) {      // to one step
@@ -461,6 +464,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
           // of a pair each CTA has half of the rows
           const int mine = kPair ? (at.rows + 31) / 32 * 16 : at.rows, row0 = at.row0 + (int)rank * mine, boxes = (mine + kBoxRows - 1) / kBoxRows;
           const bool second = kSwiglu || at.n0 + kHalfRows * kCtas < a.N;
+          const unsigned long long policy = at.alone ? l2_evict_first() : l2_evict_normal();
           const int n0 = at.n0 + (int)rank * kHalfRows;
           for (int i = 0; i < n_stages; ++i, ++n) {
             const unsigned slot = n % S::kStages, round = n / S::kStages;
@@ -468,8 +472,8 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
             const unsigned to = smem_u32(stages + slot * S::kStageBytes);
             const unsigned bar = kPair ? map_to_cta(&s.full[slot], 0) : smem_u32(&s.full[slot]);
             expect_tx(bar, (second ? S::kWBytes : S::kWBytes / 2) + boxes * kBoxRows * 128);
-            tma_3d<kPair>(to, &a.tm_w, i * 128, n0, at.expert, bar);
-            if (second) tma_3d<kPair>(to + kHalfRows * 128, &a.tm_w, i * 128, n0 + (kSwiglu ? a.I : kHalfRows * kCtas), at.expert, bar);
+            tma_3d<kPair>(to, &a.tm_w, i * 128, n0, at.expert, bar, policy);
+            if (second) tma_3d<kPair>(to + kHalfRows * 128, &a.tm_w, i * 128, n0 + (kSwiglu ? a.I : kHalfRows * kCtas), at.expert, bar, policy);
             for (int b = 0; b < boxes; ++b) tma_2d<kPair>(to + S::kWBytes + b * kBoxRows * 128, &a.tm_x, i * 128, row0 + b * kBoxRows, bar);
           }
         }
@@ -632,7 +636,7 @@ bool encode_codes(CUtensorMap* out, const void* base, int bytes, int rows, int p
   const cuuint64_t strides[2] = {(cuuint64_t)bytes, (cuuint64_t)bytes * rows};
   const cuuint32_t box[3] = {128u, (cuuint32_t)box_rows, 1u}, one[3] = {1u, 1u, 1u};
   return fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, planes ? 3 : 2, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+            CU_TENSOR_MAP_SWIZZLE_128B, planes ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int kRows, bool kSwiglu, bool kPair>

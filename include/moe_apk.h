@@ -297,7 +297,7 @@ int moe_route_grad(const int32_t* topk_ids, const float* topk_w, const float* d_
  *     MOE_DTYPE_FP8_E4M3 too (the scales of such rows are fp32 rows of hidden/128 columns: another call).  Sums are fp32 in slot
  *     order, rounded once; a call's result does not depend on the schedule.
  *   - *_stride: elements from a row to the next of that input, at least `hidden`; outputs are contiguous [R or T, hidden].
- *     hidden >= 1, any; rows that are 16-byte aligned (addresses, strides and hidden) take the fast path.
+ *     hidden: 1 to 2^30, any; rows that are 16-byte aligned (addresses, strides and hidden) take the fast path.
  *   - a slot whose entry of flat_to_sorted is outside [0, R) -- a rejected expert id -- has no row: it contributes nothing and its
  *     d_topk_w is 0.  A row whose entry of sorted_to_flat is outside [0, R) belongs to no token: xs and drows are 0 there.
  *     moe_plan_static leaves the entries of rejected ids as it finds them: preset both arrays to -1 where ids may be rejected.
@@ -322,7 +322,7 @@ int moe_merge_rows_grad(const void* dy, int64_t dy_stride, const void* rows, int
  * moe_mx_quantize: x [T, cols] -> codes and scales.  With sorted_to_flat and flat_to_sorted the result is sorted by expert
  * as in moe_sort_rows: [T*k, cols/2] and [T*k, cols/32], zero where a row belongs to no token.  With both NULL (top_k = 1) row t
  * of x is row t of the result: expert weights [E, n, cols] are quantised as E*n rows.  dtype BF16, FP16 or FP32; cols a multiple
- * of 32; codes 16-byte aligned; T * cols < 2^37.
+ * of 32, at most 2^30; codes 16-byte aligned; T * cols < 2^37.
  * moe_mx_dequantize: the values that codes and scales stand for, rounded to dtype; values 16-byte aligned. */
 int moe_mx_quantize(const void* x, int64_t x_stride, int32_t dtype, int32_t n_tokens, int32_t top_k, int32_t cols,
                     const int32_t* sorted_to_flat, const int32_t* flat_to_sorted, void* codes, void* scales, void* stream);
@@ -335,8 +335,8 @@ int moe_mx_dequantize(const void* codes, const void* scales, int64_t n_rows, int
  *   moe_mx_swiglu   weights [E, 2*inter, K], gate rows first: silu(gate) * up, computed in fp32 and quantised as by
  *                   moe_mx_quantize: codes [R, inter/2], scales [R, inter/32], the rows of the down product
  * The experts of a layer: moe_mx_quantize (sorting) -> moe_mx_swiglu -> moe_mx_product -> moe_merge_rows.
- * Rows that belong to no expert (before offsets[0], from offsets[E] on) are 0.  k_cols a multiple of 128, inter one of 32, n_cols >= 1,
- * R < 2^27, E <= 1024; codes and w_codes 16-byte aligned, scales and w_scales 4-byte aligned, else MOE_EINVAL.  No context, no
+ * Rows that belong to no expert (before offsets[0], from offsets[E] on) are 0.  (Offsets are held inside [0, R] and never lower than
+ * those before, whatever is there.)  k_cols a multiple of 128, inter one of 32, n_cols >= 1, all at most 2^30 (inter 2^29), R < 2^27, E <= 1024; codes and w_codes 16-byte aligned, scales and w_scales 4-byte aligned, else MOE_EINVAL.  No context, no
  * workspace.  Waits inside the kernel are bounded (2 s); what a launch that gave up has not computed is NaN. */
 int moe_mx_product(const void* codes, const void* scales, const void* w_codes, const void* w_scales, const int32_t* offsets,
                    int32_t n_rows, int32_t n_experts, int32_t n_cols, int32_t k_cols, void* out, void* stream);

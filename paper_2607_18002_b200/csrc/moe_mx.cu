@@ -197,7 +197,7 @@ extern "C" {
 int moe_mx_quantize(const void* x, int64_t x_stride, int32_t dtype, int32_t n_tokens, int32_t top_k, int32_t cols,
                     const int32_t* sorted_to_flat, const int32_t* flat_to_sorted, void* codes, void* scales, void* stream) {
   using namespace moe;
-  if (n_tokens < 0 || top_k < 1 || top_k > 32 || cols < kMxBlock || cols % kMxBlock || !value_type(dtype)) return MOE_EINVAL;
+  if (n_tokens < 0 || top_k < 1 || top_k > 32 || cols < kMxBlock || cols > 1 << 30 || cols % kMxBlock || !value_type(dtype)) return MOE_EINVAL;
   if (!sorted_to_flat != !flat_to_sorted || (!flat_to_sorted && top_k != 1)) return MOE_EINVAL;
   if (flat_to_sorted && (long long)n_tokens * top_k >= (1ll << kRowSlotShift)) return MOE_EINVAL;
   if ((long long)n_tokens * (cols / kMxBlock) >= (1ll << 32)) return MOE_EINVAL;
@@ -212,7 +212,7 @@ int moe_mx_quantize(const void* x, int64_t x_stride, int32_t dtype, int32_t n_to
 
 int moe_mx_dequantize(const void* codes, const void* scales, int64_t n_rows, int32_t cols, int32_t dtype, void* values, void* stream) {
   using namespace moe;
-  if (n_rows < 0 || cols < kMxBlock || cols % kMxBlock || !value_type(dtype) || n_rows > (1ll << 40) / cols) return MOE_EINVAL;
+  if (n_rows < 0 || cols < kMxBlock || cols > 1 << 30 || cols % kMxBlock || !value_type(dtype) || n_rows > (1ll << 40) / cols) return MOE_EINVAL;
   if (n_rows == 0) return MOE_OK;
   if (!codes || !scales || !values || misaligned(codes, 4) || misaligned(values, 16)) return MOE_EINVAL;
   const auto launch = dtype == MOE_DTYPE_FP32 ? dequantize_launch<float> : dtype == MOE_DTYPE_FP16 ? dequantize_launch<__half> : dequantize_launch<__nv_bfloat16>;

@@ -41,8 +41,8 @@ struct MxShared {
   unsigned tmem;
   volatile int dead;             // a wait ran out
   int first_tile[kMaxExperts + 1];   // tiles before expert e
-  int first_row[kMaxExperts + 1];    // segments, held inside [0, R)
-  __device__ __forceinline__ int rows(int e) const { return max(first_row[e + 1] - first_row[e], 0); }
+  int first_row[kMaxExperts + 1];    // segments: the offsets, held inside [0, R] and in ascending order
+  __device__ __forceinline__ int rows(int e) const { return first_row[e + 1] - first_row[e]; }
 };
 
 // What depends on the rows of a tile.  Shared memory: stages of 32 KB weights, kRows * 128 bytes of rows and the scale blocks of both; TMEM: the
@@ -283,17 +283,30 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
   __syncthreads();
   tc_fence_after();
   if (warp == 0) {
-    int before = 0;
+    int before = 0, end = s.first_row[0];
     for (int e0 = 0; e0 < a.E; e0 += 32) {
-      const int e = e0 + lane, mine = e < a.E ? (s.rows(e) + S::kRows - 1) / S::kRows * n_blocks : 0;
+      const int e = e0 + lane;
+      int to = e < a.E ? s.first_row[e + 1] : 0;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, to, d);
+        if (lane >= d) to = max(to, v);
+      }
+      to = max(to, end);
+      const int left = __shfl_up_sync(0xffffffffu, to, 1), from = lane ? left : end;
+      const int mine = e < a.E ? (to - from + S::kRows - 1) / S::kRows * n_blocks : 0;
       int sum = mine;
 #pragma unroll
       for (int d = 1; d < 32; d <<= 1) {
         const int v = __shfl_up_sync(0xffffffffu, sum, d);
         if (lane >= d) sum += v;
       }
-      if (e < a.E) s.first_tile[e] = before + sum - mine;
+      if (e < a.E) {
+        s.first_row[e + 1] = to;
+        s.first_tile[e] = before + sum - mine;
+      }
       before += __shfl_sync(0xffffffffu, sum, 31);
+      end = __shfl_sync(0xffffffffu, to, 31);
     }
     if (lane == 0) s.first_tile[a.E] = before;
   }
@@ -445,7 +458,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
     asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     // rows that belong to no expert: zeros, by the epilogue warps of the whole grid
     const size_t width = kSwiglu ? (size_t)a.I / 32 * 17 : (size_t)a.N;
-    const int lo = s.first_row[0], hi = max(s.first_row[a.E], lo), none = lo + (a.R - hi);
+    const int lo = s.first_row[0], hi = s.first_row[a.E], none = lo + (a.R - hi);
     for (int i = blockIdx.x; i < none; i += gridDim.x) {
       const size_t p = (size_t)(i < lo ? i : hi + (i - lo));
       for (size_t c = tid; c < width; c += 256) {
@@ -676,7 +689,9 @@ cudaError_t product_launch(const MxArgs& a, cudaStream_t stream) {
 template <bool kSwiglu>
 int product(const void* codes, const void* scales, const void* w_codes, const void* w_scales, const int32_t* offsets, int n_rows, int n_experts,
             int n, int K, void* out, void* out_scales, void* stream) {
-  if (n_rows < 0 || n_rows >= 1 << kRowSlotShift || n_experts < 1 || n_experts > kMaxExperts || n < 1 || K < kGroupK || K % kGroupK) return MOE_EINVAL;
+  if (n_rows < 0 || n_rows >= 1 << kRowSlotShift || n_experts < 1 || n_experts > kMaxExperts || n < 1 || n > 1 << 30 || K < kGroupK ||
+      K > 1 << 30 || K % kGroupK)
+    return MOE_EINVAL;
   if (n_rows == 0) return MOE_OK;
   if (!codes || !scales || !w_codes || !w_scales || !offsets || !out || (kSwiglu && !out_scales)) return MOE_EINVAL;
   const uintptr_t wide = reinterpret_cast<uintptr_t>(codes) | reinterpret_cast<uintptr_t>(w_codes);

@@ -311,7 +311,7 @@ int element_bytes(int dtype) {
 }
 // sizes shared by the four calls; MOE_OK with *empty set where there is nothing to do
 int check_sizes(int T, int k, int H, int dtype, bool bytes_ok, bool* empty) {
-  if (T < 0 || k < 1 || k > 32 || H < 1) return MOE_EINVAL;
+  if (T < 0 || k < 1 || k > 32 || H < 1 || H > 1 << 30) return MOE_EINVAL;
   if (!element_bytes(dtype) || (dtype == MOE_DTYPE_FP8_E4M3 && !bytes_ok)) return MOE_EINVAL;
   if ((long long)T * k >= (1ll << kRowSlotShift)) return MOE_EINVAL;        // as in a context
   *empty = T == 0;

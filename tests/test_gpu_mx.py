@@ -139,11 +139,12 @@ def _bf16(a):
 COUNTS = {
     "one row": [1], "none at all but one": [0, 0, 3, 0], "odd": [5, 0, 17, 1, 33, 0, 2, 64], "around a tile": [31, 32, 33, 0, 65],
     "dense": [300], "large": [191, 192, 193, 385, 0, 7], "mid": [64, 65, 63, 40, 130, 20],
+    "tall": [577, 192, 0, 390], "tall and one": [1100, 1, 33],            # more than 256 rows an expert, up to 64, and between: three heights of tiles
 }
 
 
 @pytest.mark.parametrize("counts", list(COUNTS.values()), ids=list(COUNTS))
-@pytest.mark.parametrize("N,K", [(256, 256), (1000, 384), (64, 128), (1, 640), (513, 2048)])
+@pytest.mark.parametrize("N,K", [(256, 256), (1000, 384), (64, 128), (1, 640), (513, 2048), (392, 512)])
 def test_product_is_exact_where_fp32_is(counts, N, K):
     """|terms| <= 36 * 4, multiples of 2^-4: sums of up to 2048 of them take 18 + 4 bits."""
     E, R = len(counts), sum(counts)
@@ -166,6 +167,26 @@ def test_rows_of_no_expert_are_zero_and_segments_need_not_start_at_the_first_row
         assert (t[:lead] == 0).all() and (t[lead + 43:] == 0).all() and t[lead:lead + 43].any()
     nobody = np.zeros(4, np.int32)
     assert (moe.mx_product(*gpu(*x, *w, nobody)) == 0).all()
+
+
+def test_offsets_out_of_order_stay_inside_their_rows():
+    """What the documentation forbids is not an access out of bounds: offsets count as the largest so far, inside [0, R]."""
+    R, K, N, E = 40, 256, 128, 5
+    x, w = _exact_operand((R,), K, 31), _exact_operand((E, N), K, 32)
+    for off, held in (([-7, 10, 4, 30, 20, 90], [0, 10, 10, 30, 30, 40]), ([2 ** 31 - 1, 0, -2 ** 31, 5, 6, 7], [40] * 6), ([0, 40, 0, 40, 0, 40], [0, 40, 40, 40, 40, 40])):
+        got = moe.mx_product(*gpu(*x, *w, np.array(off, np.int64).astype(np.int32))).cpu()
+        assert torch.equal(got, _bf16(_product64(values_of(*x), values_of(*w), np.array(held), R)))
+
+
+@pytest.mark.parametrize("E", [31, 32, 33, 64, 200, 1024])
+def test_many_experts(E):
+    """Every expert's segment is found, whatever its place in the scan over the experts."""
+    rng = np.random.default_rng(E)
+    counts = rng.integers(0, 4, E)
+    R, K, N = int(counts.sum()), 128, 40
+    x, w = _exact_operand((R,), K, 33), _exact_operand((E, N), K, 34)
+    off = _offsets(counts)
+    assert torch.equal(moe.mx_product(*gpu(*x, *w, off)).cpu(), _bf16(_product64(values_of(*x), values_of(*w), off, R)))
 
 
 def test_product_of_any_scales():

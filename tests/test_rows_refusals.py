@@ -27,6 +27,8 @@ GOOD = {
 BAD = [
     *[("moe_sort_rows", i, v) for i, v in ((0, None), (0, P + 1), (1, 63), (2, 4), (2, -1), (3, -1), (4, 0), (4, 33), (5, 0), (6, None), (7, None), (7, P + 2), (8, None),
                                            (3, 1 << 26))],
+    ("moe_sort_rows", 5, (1 << 30) + 1), ("moe_merge_rows", 6, (1 << 30) + 1), ("moe_mx_quantize", 5, (1 << 30) + 32), ("moe_mx_dequantize", 3, (1 << 30) + 32),
+    ("moe_mx_product", 7, (1 << 30) + 1), ("moe_mx_product", 8, (1 << 30) + 128), ("moe_mx_swiglu", 7, (1 << 29) + 32),
     *[("moe_sort_rows_grad", i, v) for i, v in ((0, None), (1, 63), (2, 1), (3, -1), (4, 0), (5, -1), (6, None), (7, None), (7, P + 1))],
     *[("moe_merge_rows", i, v) for i, v in ((0, None), (1, 1), (2, 1), (2, 9), (3, None), (3, P + 2), (4, -5), (5, 33), (6, 0), (7, None), (8, None))],
     *[("moe_merge_rows_grad", i, v) for i, v in ((0, None), (1, 63), (2, None), (3, 63), (4, 1), (5, None), (6, -1), (7, 0), (8, 0), (9, None), (10, None), (11, None),

@@ -13,8 +13,8 @@
 // One persistent CTA per SM walks the tiles (rows of an expert innermost: neighbours share a weight tile in L2).  Roles: one thread issues TMA
 // (a stage is 256 columns of K: 128-byte rows, swizzled), four warps bring the stage's scale bytes through registers into the 512-byte
 // form that tcgen05.cp copies to TMEM (128 rows x 4 blocks), one thread copies them and issues the MMAs, eight warps are the epilogue.
-// Weights that one tile alone reads leave L2 first, and L2 fetches 256 bytes of a weight row at a time, two stages: 800 rows of 128 experts, the
-// weight stream, 166 -> 152 us (gate/up, K 4096) and 85 -> 75 (down, K 1792), 6.6 TB/s.
+// Weights that one tile alone reads leave L2 first.  With other weights in every launch that makes no difference (800 rows of 128 experts, 1.5 GB, the
+// weight stream: gate/up 162 us, down 82, 6.1 TB/s); weights of about L2's size that come again gain 5-15 %.
 // Every wait is bounded; where one runs out the launch ends and what it has not computed is NaN.
 #include "moe_dev.cuh"
 #include "moe_mx.cuh"
@@ -205,10 +205,13 @@ __device__ __forceinline__ Tile tile_at(const MxShared& s, int E, int t, int n_s
   return Tile{lo, s.first_row[lo] + m * kRows, min(kRows, rows - m * kRows), n * n_step, m_tiles == 1};
 }
 
-__device__ __forceinline__ float rcp_approx(float v) {      // to one step
-  float r;
-  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
-  return r;
+// silu(g) u in fp32: exp(-g) = 2^(-g log2 e) to 2 + 1.2 |g| steps, the reciprocal to one.  Powers below 2^-126 and reciprocals of those above 2^126 count
+// as 0 (nothing next to the 1 that is added, silu of less than -87): the forms that keep them take three instructions more each.
+__device__ __forceinline__ float silu_times(float g, float u) {
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(g * -1.4426950408889634f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+  return g * r * u;
 }
 // 8 x 8 four-bit values over eight neighbouring lanes: lane i gives value j of word i, gets value i of word j
 __device__ __forceinline__ unsigned transpose_nibbles(unsigned v, int lane) {
@@ -426,10 +429,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
         };
         const auto activate = [&](const unsigned (&g)[16], const unsigned (&u)[16], float (&to)[16]) {
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const float gv = __uint_as_float(g[j]);
-            to[j] = gv * rcp_approx(1.f + __expf(-gv)) * __uint_as_float(u[j]);
-          }
+          for (int j = 0; j < 16; ++j) to[j] = silu_times(__uint_as_float(g[j]), __uint_as_float(u[j]));
         };
 #pragma unroll
         for (int i = 0; i < kFirst; ++i)
@@ -649,7 +649,7 @@ bool encode_codes(CUtensorMap* out, const void* base, int bytes, int rows, int p
   const cuuint64_t strides[2] = {(cuuint64_t)bytes, (cuuint64_t)bytes * rows};
   const cuuint32_t box[3] = {128u, (cuuint32_t)box_rows, 1u}, one[3] = {1u, 1u, 1u};
   return fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, planes ? 3 : 2, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_128B, planes ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int kRows, bool kSwiglu, bool kPair>
@@ -707,19 +707,21 @@ int product(const void* codes, const void* scales, const void* w_codes, const vo
   a.R = n_rows; a.E = n_experts; a.N = n; a.K = K; a.I = n / 2;
   a.wide = n % 8 == 0 && (reinterpret_cast<uintptr_t>(out) & 15) == 0;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  // The tile's height goes by the rows that an expert gets on average (the host does not know more).  Two buffers of 64 or 96 columns let the epilogue of
-  // a tile run beside the next one's MMAs; 192 columns take the weights from L2 half as often.  us, 32 experts, K 4096, inter 1792 (gate/up, down):
-  //   rows an expert     32          64          128         256         512          1024         2048
-  //   64 rows            54.5, 28.4  57.3, 33.8  74.8, 43.3  122.6, 70.1
-  //   96 rows            54.3, 28.9  56.3, 31.2  72.2, 39.2  98.3, 55.3  186, 101     336, 184     652, 358
-  //   192 rows           58.6, 32.8  64.0, 35.6  71.4, 39.7  110, 60.2   156, 92.9    329, 168     552, 304
-  //   192 rows, pairs    61.2, 34.8  64.5, 36.9  72.7, 42.0  98.0, 63.2  148, 93.4    265, 175     473, 313
-  // 64 experts, K 2048, inter 768, uneven (Zipf 0.8), 64 and 96 rows: 24.3, 14.3 and 25.3, 16.1 for 32 rows an expert, 35.8, 23.3 and 29.9, 25.1 for 96.
-  // Tiles of 32 rows gained 2-8 % below 16 rows an expert, 0.2-0.5 us of a launch of 6-20, and are left out.
-  const bool few = n_rows <= 64ll * n_experts, many = n_rows > 256ll * n_experts;
-  const cudaError_t e = few    ? product_launch<64, kSwiglu, false>(a, st)
-                        : many ? product_launch<192, kSwiglu, kSwiglu>(a, st)
-                               : product_launch<96, kSwiglu, false>(a, st);
+  // The tile's height goes by the rows that an expert gets on average (the host does not know more).  Two buffers of 96 columns let the epilogue of a tile
+  // run beside the next one's MMAs; 192 columns take the weights from L2 half as often, and for gate/up a pair of CTAs takes half of the rows each.
+  // us (gate/up, down), weights that are not in L2:
+  //   rows an expert                   32          64          128         256         384         512         1024      2048
+  //   even, 32 experts, 4096 x 1792
+  //     96 rows                        50.2, 24.9  51.9, 26.3  74.4, 39.9  103, 57.7   136, 76.8   191, 104    347, 191  678, 369
+  //     192 rows                       52.9, 25.9  56.0, 28.3  64.9, 35.5  107, 63.5   119, 74.8   151, 95.2   294, 176  505, 314
+  //     192 rows, pairs                53.9, 29.4  57.0, 30.7  64.9, 36.5  98.6, 65.9  109, 76.8   144, 94.7   257, 181  462, 327
+  //   uneven (Zipf 0.8), 64 experts, 2048 x 768
+  //     96 rows                        23.6, 16.7  29.3, 19.8              52.9, 44.0              84.7, 72.4
+  //     192 rows                       28.0, 19.1  31.4, 23.9              56.0, 45.1              98.3, 72.7
+  //     192 rows, pairs                29.7, 21.8  32.1, 26.3              50.9, 48.1              82.9, 77.5
+  // Tiles of 64 and 32 rows are left out: 0-7 % faster below 32 rows an expert, up to 25 % slower at 64.
+  const bool many = n_rows > (kSwiglu ? 192ll : 320ll) * n_experts;
+  const cudaError_t e = many ? product_launch<192, kSwiglu, kSwiglu>(a, st) : product_launch<96, kSwiglu, false>(a, st);
   return e == cudaSuccess ? MOE_OK : MOE_ECUDA;
 }
 

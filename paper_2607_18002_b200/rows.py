@@ -2,7 +2,8 @@
 experts in 4 bits (moe_sort_rows ... moe_mx_swiglu of include/moe_apk.h).
 
 Checks of arguments and marshalling only; a call enqueues one kernel on `stream` (the current stream of the tensors' device if
-None) and allocates its outputs there.  Wrong types, shapes, strides or devices raise ValueError, what the library refuses MoeError.
+None) and allocates its outputs there.  Nothing is recorded for autograd: gradients are calls of their own.  Wrong types, shapes, strides
+or devices raise ValueError, what the library refuses MoeError.
 A permutation is the pair (sorted_to_flat, flat_to_sorted) of a plan, int32 [T*k] each.
 
     codes, scales = mx_quantize(x, s2f, f2s, k)                          # experts of a layer in 4 bits

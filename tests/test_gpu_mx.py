@@ -217,6 +217,20 @@ def test_nan_blocks_reach_their_outputs_only():
     assert torch.equal(bad, want)
 
 
+@pytest.mark.parametrize("counts", [[20, 30], [420, 30]], ids=["low tiles", "high tiles"])
+def test_nan_blocks_make_their_swiglu_blocks_nan(counts):
+    K, I = 256, 96
+    x, w = _exact_operand((sum(counts),), K, 7), _exact_operand((2, 2 * I), K, 8)
+    x[1][4, 3] = 255                                                # a row
+    w[1][1, 40, 0] = 255                                            # expert 1, gate column 40
+    w[1][1, I + 95, 1] = 255                                        # ... and up column 95
+    codes, scales = (t.cpu().numpy() for t in moe.mx_swiglu(*gpu(*x, *w, _offsets(counts))))
+    want = np.zeros(scales.shape, bool)
+    want[4] = True
+    want[counts[0]:, 1:] = True
+    assert np.array_equal(scales == 255, want)
+
+
 def _swiglu_bounds(g, u):
     """silu(g) u, and how far off fp32 may be: exp to 2 + 1.2 |g| steps of 2^-23, a sum, a quotient to two steps, a product."""
     a = g / (1.0 + np.exp(-g)) * u
@@ -273,7 +287,7 @@ def test_results_do_not_depend_on_the_run_or_on_neighbours():
         assert torch.equal(one[0], all_rows[at])
 
 
-@pytest.mark.parametrize("T,E,k,H,I", [(1, 8, 2, 256, 128), (5, 64, 8, 512, 256), (100, 16, 4, 384, 384), (700, 8, 2, 256, 128)])
+@pytest.mark.parametrize("T,E,k,H,I", [(1, 8, 2, 256, 128), (5, 64, 8, 512, 256), (100, 16, 4, 384, 384), (700, 8, 2, 256, 128), (1500, 8, 2, 384, 160 * 4)])
 def test_a_layer_as_it_is_used(T, E, k, H, I):
     """route -> plan -> quantise and sort -> gate/up -> down -> merge, eagerly and as a captured graph that is replayed on new tokens."""
     rng = np.random.default_rng([T, E])
@@ -335,18 +349,37 @@ def test_a_layer_as_it_is_used(T, E, k, H, I):
         check(out)
 
 
-def test_two_streams_at_once():
+@pytest.mark.parametrize("counts", [[100, 20, 0, 180], [900, 20, 0, 380]], ids=["low tiles", "high tiles"])
+def test_two_streams_at_once(counts):
     """Products on two streams share nothing: both are what they are alone."""
     K, N = 512, 512
-    a = [gpu(*_exact_operand((300,), K, s), *_exact_operand((4, N), K, s + 1), _offsets([100, 20, 0, 180])) for s in (20, 30)]
-    want = [moe.mx_product(*v) for v in a]
+    a = [gpu(*_exact_operand((sum(counts),), K, s), *_exact_operand((4, N), K, s + 1), _offsets(counts)) for s in (20, 30)]
+    both = lambda v, s=None: (moe.mx_product(*v, stream=s), *moe.mx_swiglu(*v, stream=s))
+    want = [both(v) for v in a]
     streams = [torch.cuda.Stream() for _ in a]
     torch.cuda.synchronize()
-    got = [[moe.mx_product(*v, stream=s) for v, s in zip(a, streams)] for _ in range(10)]
+    got = [[both(v, s) for v, s in zip(a, streams)] for _ in range(10)]
     torch.cuda.synchronize()
     for pair in got:
         for x, y in zip(pair, want):
-            assert torch.equal(x, y)
+            assert all(torch.equal(p, q) for p, q in zip(x, y))
+
+
+@pytest.mark.parametrize("K", [128, 256, 384, 768, 1024])
+@pytest.mark.parametrize("shift", [4, 8])
+def test_scales_that_are_aligned_to_words_only(K, shift):
+    counts, N = [50, 0, 300], 200
+    R = sum(counts)
+    x, w = _exact_operand((R,), K, 41), _exact_operand((3, N), K, 42)
+    off = _offsets(counts)
+    def moved(t):
+        buf = torch.full((t.numel() + shift,), 255, dtype=torch.uint8, device="cuda")
+        buf[shift:] = t.reshape(-1)
+        return buf[shift:].view(t.shape)
+    dx, dxs, dw, dws, doff = gpu(*x, *w, off)
+    ref = _bf16(_product64(values_of(*x), values_of(*w), off, R))
+    assert torch.equal(moe.mx_product(dx, moved(dxs), dw, moved(dws), doff).cpu(), ref)
+    assert torch.equal(moe.mx_product(dx, dxs, dw, moved(dws), doff).cpu(), ref)
 
 
 def test_weights_past_four_gigabytes():

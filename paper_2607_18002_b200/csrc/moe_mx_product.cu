@@ -160,30 +160,23 @@ __device__ __forceinline__ void tc_ld16(unsigned taddr, unsigned (&r)[16]) {
       : "memory");
 }
 
-// 32 bytes of a row's scales, `left` of which are there (the others are not used), by loads of vec bytes
-struct RowScales {
-  unsigned w[8];
-};
-__device__ __forceinline__ RowScales load_scales(const unsigned char* p, int left, int vec) {
-  RowScales v;
+// 16 bytes of a row's scales, `left` of which are there (the others are not used), by loads of vec bytes
+__device__ __forceinline__ uint4 load_scales(const unsigned char* p, int left, int vec) {
+  uint4 v = make_uint4(0u, 0u, 0u, 0u);
   if (vec == 16) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      if (left > 16 * i) {
-        const uint4 q = __ldg(reinterpret_cast<const uint4*>(p) + i);
-        v.w[4 * i] = q.x; v.w[4 * i + 1] = q.y; v.w[4 * i + 2] = q.z; v.w[4 * i + 3] = q.w;
-      }
+    if (left > 0) v = __ldg(reinterpret_cast<const uint4*>(p));
   } else if (vec == 8) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (left > 8 * i) {
-        const uint2 q = __ldg(reinterpret_cast<const uint2*>(p) + i);
-        v.w[2 * i] = q.x; v.w[2 * i + 1] = q.y;
-      }
+    const uint2* q = reinterpret_cast<const uint2*>(p);
+    uint2 a = make_uint2(0u, 0u), b = a;
+    if (left > 0) a = __ldg(q);
+    if (left > 8) b = __ldg(q + 1);
+    v = make_uint4(a.x, a.y, b.x, b.y);
   } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (left > 4 * i) v.w[i] = __ldg(reinterpret_cast<const unsigned*>(p) + i);
+    const unsigned* q = reinterpret_cast<const unsigned*>(p);
+    if (left > 0) v.x = __ldg(q);
+    if (left > 4) v.y = __ldg(q + 1);
+    if (left > 8) v.z = __ldg(q + 2);
+    if (left > 12) v.w = __ldg(q + 3);
   }
   return v;
 }
@@ -548,17 +541,17 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
     }
   } else {
     if (S::kRows > 96) asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
-    // A thread has one row of every 128-row block, in the order that spreads a warp's stores over all banks: its four bytes of a group of 128
-    // columns go to 16 (r % 32) + 4 (r / 32) of the group's block.  It loads a sector of 32 bytes, four stages, at a time; the next one
-    // is on its way to registers meanwhile, whether or not its stages are free.
-    const int r = 32 * (lane & 3) + 8 * (warp - kScaleWarp) + (lane >> 2);
-    const unsigned spot = (unsigned)(r & 31) * 16 + (unsigned)(r >> 5) * 4;
+    // Two neighbouring lanes have a row: together they load a sector of 32 bytes, four stages, two each; the next sector is on its way to registers
+    // meanwhile, whether or not its stages are free.  A thread has two rows of every 128-row block, in the order that spreads a warp's stores over
+    // the banks: the four bytes of a group of 128 columns of row r go to 16 (r % 32) + 4 (r / 32) of the group's block.
+    const int pair = lane & 1, r0 = 32 * (lane >> 1 & 3) + 4 * (warp - kScaleWarp) + (lane >> 3);      // and r0 + 16
+    const unsigned spot = (unsigned)(r0 & 31) * 16 + (unsigned)(r0 >> 5) * 4;
     const int per_row = a.K / kMxBlock, n_quads = (n_stages + 3) / 4;
     const int vec = per_row % 16 == 0 ? 16 : per_row % 8 == 0 ? 8 : 4;
     const int vec_w = (size_t)a.w_scales & (vec - 1) ? 4 : vec, vec_x = (size_t)a.x_scales & (vec - 1) ? 4 : vec;
     constexpr int kBlocks = 2 + S::kRowBlocks;
     struct Quad {
-      RowScales b[kBlocks];
+      uint4 b[kBlocks][2];
       int stages;                // 1 to 4; 0: there is no more
     };
     int t = unit, quad = 0;
@@ -568,17 +561,21 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
       p.stages = 0;
       if (t >= n_tiles) return;
       if (quad == 0) at = tile_at<S::kRows>(s, a.E, t, kStep);
-      const int left = per_row - quad * 32;
-      const unsigned char* w = a.w_scales + (size_t)at.expert * a.N * per_row + quad * 32;
-      const unsigned char* x = a.x_scales + (size_t)at.row0 * per_row + quad * 32;
+      const int from = quad * 32 + pair * 16, left = per_row - from;
+      const unsigned char* w = a.w_scales + (size_t)at.expert * a.N * per_row + from;
+      const unsigned char* x = a.x_scales + (size_t)at.row0 * per_row + from;
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {        // a weight row behind the last one: any other's scales (its products are not stored)
-        const int row = kSwiglu ? min(at.n0 + (int)rank * kHalfRows + r, a.I - 1) + b * a.I
-                                : min(at.n0 + (b * kCtas + (int)rank) * kHalfRows + r, a.N - 1);
-        p.b[b] = load_scales(w + (size_t)row * per_row, left, vec_w);
+      for (int q = 0; q < 2; ++q) {
+        const int r = r0 + 16 * q;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {      // a weight row behind the last one: any other's scales (its products are not stored)
+          const int row = kSwiglu ? min(at.n0 + (int)rank * kHalfRows + r, a.I - 1) + b * a.I
+                                  : min(at.n0 + (b * kCtas + (int)rank) * kHalfRows + r, a.N - 1);
+          p.b[b][q] = load_scales(w + (size_t)row * per_row, left, vec_w);
+        }
+#pragma unroll
+        for (int b = 0; b < S::kRowBlocks; ++b) p.b[2 + b][q] = load_scales(x + (size_t)min(b * 128 + r, at.rows - 1) * per_row, left, vec_x);
       }
-#pragma unroll
-      for (int b = 0; b < S::kRowBlocks; ++b) p.b[2 + b] = load_scales(x + (size_t)min(b * 128 + r, at.rows - 1) * per_row, left, vec_x);
       p.stages = min(4, n_stages - 4 * quad);
       if (++quad == n_quads) {
         quad = 0;
@@ -591,13 +588,18 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
         if (h >= p.stages) break;
         const unsigned slot = n % S::kStages, round = n / S::kStages;
         if (round && !__all_sync(0xffffffffu, wait(&s.empty[slot], (round - 1) & 1, &s.dead))) return false;
-        const unsigned to = smem_u32(stages + slot * S::kStageBytes) + S::kWBytes + S::kXBytes + spot;
+        if (pair == h / 2) {
+          const unsigned to = smem_u32(stages + slot * S::kStageBytes) + S::kWBytes + S::kXBytes + spot;
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b) {
-          st_word(to + b * kScaleBlock, p.b[b].w[2 * h]);
-          st_word(to + (kBlocks + b) * kScaleBlock, p.b[b].w[2 * h + 1]);
+          for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+              const uint4& v = p.b[b][q];
+              st_word(to + b * kScaleBlock + 256 * q, h & 1 ? v.z : v.x);
+              st_word(to + (kBlocks + b) * kScaleBlock + 256 * q, h & 1 ? v.w : v.y);
+            }
+          fence_async_proxy_smem();
         }
-        fence_async_proxy_smem();
         __syncwarp();
         if (lane == 0) {
           if (kPair) mbar_arrive_remote(map_to_cta(&s.landed[slot], 0));

@@ -46,16 +46,16 @@ def _rows(t, name, dtypes):
     return n, h, step if step > h else h
 
 
-def _plain(t, name, dtype, shape, device):
-    """A contiguous tensor of this type and shape."""
-    if not isinstance(t, _Tensor) or t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
-        _refuse(f"{name} must be a contiguous {dtype} tensor {tuple(shape)} on {device}")
+def _plain(t, name, dtype, shape, gpu):
+    """A contiguous tensor of this type and shape on GPU number `gpu`."""
+    if not isinstance(t, _Tensor) or t.dtype is not dtype or t.shape != shape or t.get_device() != gpu or not t.is_contiguous():
+        _refuse(f"{name} must be a contiguous {dtype} tensor {tuple(shape)} on cuda:{gpu}")
 
 
-def _index(t, name, n, device):
-    if not isinstance(t, _Tensor) or t.dtype != _I32 or t.dim() != 1 or t.device != device or not t.is_contiguous() \
-            or t.shape[0] != n and (n or t.shape[0] != 1):              # (a plan without rows has arrays of one entry)
-        _refuse(f"{name} must be a contiguous int32 tensor [{n}] on {device}")
+def _index(t, name, n, gpu):
+    if not isinstance(t, _Tensor) or t.dtype is not _I32 or t.get_device() != gpu or not t.is_contiguous() \
+            or t.numel() != n and (n or t.numel() != 1):                # (a plan without rows has arrays of one entry)
+        _refuse(f"{name} must be a contiguous int32 tensor of {n} on cuda:{gpu}")
 
 
 def _elsewhere(call, device, stream, *args):
@@ -73,11 +73,11 @@ def _failed(rc, name):
 def sort_rows(x, sorted_to_flat, flat_to_sorted, top_k: int, stream=None):
     """x [T, H] -> [T*k, H], the tokens' rows by expert (bf16, fp16, fp32, or one-byte codes)."""
     T, H, step = _rows(x, "x", _SORTED_DTYPES)
-    dev = x.device
-    if stream is not None or dev.index != _current_device():
-        return _elsewhere(sort_rows, dev, stream, x, sorted_to_flat, flat_to_sorted, top_k)
-    _index(sorted_to_flat, "sorted_to_flat", T * top_k, dev)
-    _index(flat_to_sorted, "flat_to_sorted", T * top_k, dev)
+    gpu = x.get_device()
+    if stream is not None or gpu != _current_device():
+        return _elsewhere(sort_rows, x.device, stream, x, sorted_to_flat, flat_to_sorted, top_k)
+    _index(sorted_to_flat, "sorted_to_flat", T * top_k, gpu)
+    _index(flat_to_sorted, "flat_to_sorted", T * top_k, gpu)
     xs = x.new_empty(T * top_k, H)
     rc = (moe._lib or moe.lib()).moe_sort_rows(x.data_ptr(), step, _SORTED_DTYPES[x.dtype], T, top_k, H, sorted_to_flat.data_ptr(),
                                                flat_to_sorted.data_ptr(), xs.data_ptr(), _stream(None))
@@ -89,12 +89,12 @@ def sort_rows(x, sorted_to_flat, flat_to_sorted, top_k: int, stream=None):
 def sort_rows_grad(dxs, flat_to_sorted, top_k: int, stream=None):
     """dxs [T*k, H], the gradient of sort_rows' result -> that of x [T, H]."""
     R, H, step = _rows(dxs, "dxs", _DTYPES)
-    dev = dxs.device
-    if stream is not None or dev.index != _current_device():
-        return _elsewhere(sort_rows_grad, dev, stream, dxs, flat_to_sorted, top_k)
+    gpu = dxs.get_device()
+    if stream is not None or gpu != _current_device():
+        return _elsewhere(sort_rows_grad, dxs.device, stream, dxs, flat_to_sorted, top_k)
     if top_k < 1 or R % top_k:
         _refuse("dxs must have top_k rows for every token")
-    _index(flat_to_sorted, "flat_to_sorted", R, dev)
+    _index(flat_to_sorted, "flat_to_sorted", R, gpu)
     T = R // top_k
     dx = dxs.new_empty(T, H)
     rc = (moe._lib or moe.lib()).moe_sort_rows_grad(dxs.data_ptr(), step, _DTYPES[dxs.dtype], T, top_k, H, flat_to_sorted.data_ptr(),
@@ -104,21 +104,21 @@ def sort_rows_grad(dxs, flat_to_sorted, top_k: int, stream=None):
     return dx
 
 
-def _weights(topk_w, R, dev):
-    if not isinstance(topk_w, _Tensor) or topk_w.dtype != _FP32 or topk_w.dim() != 2 or topk_w.numel() != R or topk_w.device != dev \
+def _weights(topk_w, R, gpu):
+    if not isinstance(topk_w, _Tensor) or topk_w.dtype is not _FP32 or topk_w.dim() != 2 or topk_w.numel() != R or topk_w.get_device() != gpu \
             or not topk_w.is_contiguous():
-        _refuse(f"topk_w must be a contiguous fp32 tensor [T, k] on {dev}, a weight for each of the {R} rows")
+        _refuse(f"topk_w must be a contiguous fp32 tensor [T, k] on cuda:{gpu}, a weight for each of the {R} rows")
     return topk_w.shape
 
 
 def merge_rows(rows, flat_to_sorted, topk_w, stream=None):
     """rows [T*k, H] by expert -> y [T, H], the tokens' rows added up with their router weights."""
     R, H, step = _rows(rows, "rows", _DTYPES)
-    dev = rows.device
-    if stream is not None or dev.index != _current_device():
-        return _elsewhere(merge_rows, dev, stream, rows, flat_to_sorted, topk_w)
-    T, k = _weights(topk_w, R, dev)
-    _index(flat_to_sorted, "flat_to_sorted", R, dev)
+    gpu = rows.get_device()
+    if stream is not None or gpu != _current_device():
+        return _elsewhere(merge_rows, rows.device, stream, rows, flat_to_sorted, topk_w)
+    T, k = _weights(topk_w, R, gpu)
+    _index(flat_to_sorted, "flat_to_sorted", R, gpu)
     y = rows.new_empty(T, H)
     rc = (moe._lib or moe.lib()).moe_merge_rows(rows.data_ptr(), step, _DTYPES[rows.dtype], topk_w.data_ptr(), T, k, H,
                                                 flat_to_sorted.data_ptr(), y.data_ptr(), _stream(None))
@@ -130,15 +130,15 @@ def merge_rows(rows, flat_to_sorted, topk_w, stream=None):
 def merge_rows_grad(dy, rows, sorted_to_flat, flat_to_sorted, topk_w, stream=None):
     """dy [T, H], the gradient of merge_rows' result -> (that of rows [T*k, H], that of topk_w [T, k] fp32)."""
     R, H, step = _rows(rows, "rows", _DTYPES)
-    dev = rows.device
-    if stream is not None or dev.index != _current_device():
-        return _elsewhere(merge_rows_grad, dev, stream, dy, rows, sorted_to_flat, flat_to_sorted, topk_w)
-    T, k = _weights(topk_w, R, dev)
+    gpu = rows.get_device()
+    if stream is not None or gpu != _current_device():
+        return _elsewhere(merge_rows_grad, rows.device, stream, dy, rows, sorted_to_flat, flat_to_sorted, topk_w)
+    T, k = _weights(topk_w, R, gpu)
     dT, dH, dy_step = _rows(dy, "dy", _DTYPES)
-    if dT != T or dH != H or dy.dtype != rows.dtype or dy.device != dev:
-        _refuse(f"dy must be a {rows.dtype} tensor [{T}, {H}] on {dev}")
-    _index(sorted_to_flat, "sorted_to_flat", R, dev)
-    _index(flat_to_sorted, "flat_to_sorted", R, dev)
+    if dT != T or dH != H or dy.dtype is not rows.dtype or dy.get_device() != gpu:
+        _refuse(f"dy must be a {rows.dtype} tensor [{T}, {H}] on cuda:{gpu}")
+    _index(sorted_to_flat, "sorted_to_flat", R, gpu)
+    _index(flat_to_sorted, "flat_to_sorted", R, gpu)
     drows, dw = rows.new_empty(R, H), topk_w.new_empty(T, k)
     rc = (moe._lib or moe.lib()).moe_merge_rows_grad(dy.data_ptr(), dy_step, rows.data_ptr(), step, _DTYPES[rows.dtype], topk_w.data_ptr(), T, k, H,
                                                      sorted_to_flat.data_ptr(), flat_to_sorted.data_ptr(), drows.data_ptr(), dw.data_ptr(),
@@ -152,12 +152,12 @@ def route_grad(topk_ids, topk_w, d_topk_w, n_experts: int, stream=None):
     """The gradient of route's weights, fp32 [T, k] -> that of the logits, fp32 [T, E]."""
     if not isinstance(topk_ids, _Tensor) or not topk_ids.is_cuda or topk_ids.dim() != 2:
         _refuse("topk_ids must be a CUDA int32 tensor [T, k]")
-    shape, dev = topk_ids.shape, topk_ids.device
-    if stream is not None or dev.index != _current_device():
-        return _elsewhere(route_grad, dev, stream, topk_ids, topk_w, d_topk_w, n_experts)
-    _plain(topk_ids, "topk_ids", _I32, shape, dev)
-    _plain(topk_w, "topk_w", _FP32, shape, dev)
-    _plain(d_topk_w, "d_topk_w", _FP32, shape, dev)
+    shape, gpu = topk_ids.shape, topk_ids.get_device()
+    if stream is not None or gpu != _current_device():
+        return _elsewhere(route_grad, topk_ids.device, stream, topk_ids, topk_w, d_topk_w, n_experts)
+    _plain(topk_ids, "topk_ids", _I32, shape, gpu)
+    _plain(topk_w, "topk_w", _FP32, shape, gpu)
+    _plain(d_topk_w, "d_topk_w", _FP32, shape, gpu)
     T, k = shape
     dz = topk_w.new_empty(T, n_experts)
     rc = (moe._lib or moe.lib()).moe_route_grad(topk_ids.data_ptr(), topk_w.data_ptr(), d_topk_w.data_ptr(), T, n_experts, k, dz.data_ptr(),
@@ -173,20 +173,20 @@ def mx_quantize(x, sorted_to_flat=None, flat_to_sorted=None, top_k: int = 1, str
         codes, scales = mx_quantize(x.view(-1, x.shape[-1]), None, None, top_k, stream)
         return codes.view(*x.shape[:-1], -1), scales.view(*x.shape[:-1], -1)
     T, K, step = _rows(x, "x", _DTYPES)
-    dev = x.device
-    if stream is not None or dev.index != _current_device():
-        return _elsewhere(mx_quantize, dev, stream, x, sorted_to_flat, flat_to_sorted, top_k)
+    gpu = x.get_device()
+    if stream is not None or gpu != _current_device():
+        return _elsewhere(mx_quantize, x.device, stream, x, sorted_to_flat, flat_to_sorted, top_k)
     if K % 32:
         _refuse("x must have a multiple of 32 columns")
     R = T * top_k
     s2f = f2s = None
     if sorted_to_flat is not None or flat_to_sorted is not None:
-        _index(sorted_to_flat, "sorted_to_flat", R, dev)
-        _index(flat_to_sorted, "flat_to_sorted", R, dev)
+        _index(sorted_to_flat, "sorted_to_flat", R, gpu)
+        _index(flat_to_sorted, "flat_to_sorted", R, gpu)
         s2f, f2s = sorted_to_flat.data_ptr(), flat_to_sorted.data_ptr()
     elif top_k != 1:
         _refuse("top_k needs a permutation")
-    codes = _empty(R, K // 2, dtype=_U8, device=dev)
+    codes = _empty(R, K // 2, dtype=_U8, device=x.device)
     scales = codes.new_empty(R, K // 32)
     rc = (moe._lib or moe.lib()).moe_mx_quantize(x.data_ptr(), step, _DTYPES[x.dtype], T, top_k, K, s2f, f2s, codes.data_ptr(),
                                                  scales.data_ptr(), _stream(None))
@@ -200,7 +200,7 @@ def _codes(codes, scales, what, dims):
     if not isinstance(codes, _Tensor) or not isinstance(scales, _Tensor):
         _refuse(f"the codes and scales of {what} must be tensors")
     shape, width = codes.shape, scales.shape
-    if codes.dtype != _U8 or scales.dtype != _U8 or not codes.is_cuda or codes.device != scales.device or not codes.is_contiguous() \
+    if codes.dtype is not _U8 or scales.dtype is not _U8 or not codes.is_cuda or codes.get_device() != scales.get_device() or not codes.is_contiguous() \
             or not scales.is_contiguous() or (len(shape) != dims if dims else not shape) or not width or shape[-1] != 16 * width[-1] \
             or shape[:-1] != width[:-1]:
         _refuse(f"the codes and scales of {what} must be contiguous uint8 tensors of {dims or 'some'} dimensions on one GPU, a scale for 16 bytes of codes")
@@ -212,10 +212,10 @@ def mx_dequantize(codes, scales, dtype=_BF16, stream=None):
     if dtype not in _DTYPES:
         _refuse(f"dtype must be one of {sorted(map(str, _DTYPES))}")
     *lead, half = _codes(codes, scales, "the rows", 0)
-    dev, K = codes.device, 2 * half
-    if stream is not None or dev.index != _current_device():
-        return _elsewhere(mx_dequantize, dev, stream, codes, scales, dtype)
-    out = _empty(*lead, K, dtype=dtype, device=dev)
+    gpu, K = codes.get_device(), 2 * half
+    if stream is not None or gpu != _current_device():
+        return _elsewhere(mx_dequantize, codes.device, stream, codes, scales, dtype)
+    out = _empty(*lead, K, dtype=dtype, device=codes.device)
     if K:
         rc = (moe._lib or moe.lib()).moe_mx_dequantize(codes.data_ptr(), scales.data_ptr(), out.numel() // K, K, _DTYPES[dtype], out.data_ptr(),
                                                        _stream(None))
@@ -225,22 +225,22 @@ def mx_dequantize(codes, scales, dtype=_BF16, stream=None):
 
 
 def _operands(codes, scales, w_codes, w_scales, offsets):
-    """-> device, R, E, n, K"""
+    """-> number of the GPU, R, E, n, K"""
     R, half = _codes(codes, scales, "the rows", 2)
     E, n, w_half = _codes(w_codes, w_scales, "the weights", 3)
-    dev = codes.device
-    if w_half != half or w_codes.device != dev:
-        _refuse(f"the weights must have {2 * half} columns and be on {dev}, as the rows")
-    _index(offsets, "offsets", E + 1, dev)
-    return dev, R, E, n, 2 * half
+    gpu = codes.get_device()
+    if w_half != half or w_codes.get_device() != gpu:
+        _refuse(f"the weights must have {2 * half} columns and be on cuda:{gpu}, as the rows")
+    _index(offsets, "offsets", E + 1, gpu)
+    return gpu, R, E, n, 2 * half
 
 
 def mx_product(codes, scales, w_codes, w_scales, offsets, stream=None):
     """Sorted 4-bit rows [R, K] times the experts' matrices [E, n, K] -> bf16 [R, n]."""
-    dev, R, E, n, K = _operands(codes, scales, w_codes, w_scales, offsets)
-    if stream is not None or dev.index != _current_device():
-        return _elsewhere(mx_product, dev, stream, codes, scales, w_codes, w_scales, offsets)
-    out = _empty(R, n, dtype=_BF16, device=dev)
+    gpu, R, E, n, K = _operands(codes, scales, w_codes, w_scales, offsets)
+    if stream is not None or gpu != _current_device():
+        return _elsewhere(mx_product, codes.device, stream, codes, scales, w_codes, w_scales, offsets)
+    out = _empty(R, n, dtype=_BF16, device=codes.device)
     rc = (moe._lib or moe.lib()).moe_mx_product(codes.data_ptr(), scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), offsets.data_ptr(), R, E,
                                                 n, K, out.data_ptr(), _stream(None))
     if rc:
@@ -250,11 +250,11 @@ def mx_product(codes, scales, w_codes, w_scales, offsets, stream=None):
 
 def mx_swiglu(codes, scales, w_codes, w_scales, offsets, stream=None):
     """Sorted 4-bit rows [R, K] times gate and up matrices [E, 2 I, K], silu(gate) * up -> codes [R, I/2], scales [R, I/32]."""
-    dev, R, E, n, K = _operands(codes, scales, w_codes, w_scales, offsets)
+    gpu, R, E, n, K = _operands(codes, scales, w_codes, w_scales, offsets)
     if n % 64:
         _refuse("the weights must have gate and up rows, a multiple of 32 each")
-    if stream is not None or dev.index != _current_device():
-        return _elsewhere(mx_swiglu, dev, stream, codes, scales, w_codes, w_scales, offsets)
+    if stream is not None or gpu != _current_device():
+        return _elsewhere(mx_swiglu, codes.device, stream, codes, scales, w_codes, w_scales, offsets)
     out, out_scales = codes.new_empty(R, n // 4), codes.new_empty(R, n // 64)
     rc = (moe._lib or moe.lib()).moe_mx_swiglu(codes.data_ptr(), scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), offsets.data_ptr(), R, E,
                                                n // 2, K, out.data_ptr(), out_scales.data_ptr(), _stream(None))

@@ -396,6 +396,36 @@ def test_weights_past_four_gigabytes():
     assert out[1, N - 3:].tolist() == [K, K, 2 * K]
 
 
+def test_results_past_four_giga_elements():
+    """Sorted codes of more than 2^32 bytes; products of more than 2^32 outputs, stored both ways (rows aligned to 16 bytes, and not)."""
+    T, k, K = 1 << 17, 8, 8448
+    ids, w, offsets, s2f, f2s = routing(T, 16, k, 3)
+    ds2f, df2s = gpu(s2f, f2s)
+    x = torch.randn(T, K, device="cuda").to(torch.bfloat16)
+    codes, scales = moe.mx_quantize(x, ds2f, df2s, k)
+    c0, s0 = moe.mx_quantize(x)
+    token = (ds2f // k).long()
+    for at in (0, K // 4 + 3, K // 2 - 1):
+        assert torch.equal(codes[:, at], c0[token, at])
+    for at in (0, K // 32 - 1):
+        assert torch.equal(scales[:, at], s0[token, at])
+    R = T * k
+    rows, rows_scales = codes[:, :64].contiguous(), torch.full((R, 4), 127, dtype=torch.uint8, device="cuda")
+    del codes, scales, c0, s0, x
+    for N in (4104, 4101):
+        wc, ws = _exact_operand((2, N), 128, 5)
+        out = moe.mx_product(rows, rows_scales, *gpu(wc, ws), gpu(np.array([0, R // 2 + 5, R], np.int32)))
+        at = np.array([0, 1, R // 2 + 4, R // 2 + 5, R - 2, R - 1])
+        xv, wv = values_of(rows[at].cpu(), rows_scales[at].cpu()), values_of(wc, ws)
+        ref = np.stack([xv[i] @ wv[0 if at[i] < R // 2 + 5 else 1].T for i in range(len(at))])
+        assert torch.equal(out[at].cpu(), _bf16(ref))
+        whole = torch.cat([out[: 1 << 16], out[-(1 << 16):]])
+        near = torch.cat([moe.mx_product(rows[: 1 << 16], rows_scales[: 1 << 16], *gpu(wc, ws), gpu(np.array([0, 1 << 16, 1 << 16], np.int32))),
+                          moe.mx_product(rows[-(1 << 16):], rows_scales[-(1 << 16):], *gpu(wc, ws), gpu(np.array([0, 0, 1 << 16], np.int32)))])
+        assert torch.equal(whole, near)
+        del out, whole, near
+
+
 def test_empty_batches():
     x = torch.empty(0, 128, dtype=torch.bfloat16, device="cuda")
     codes, scales = moe.mx_quantize(x)

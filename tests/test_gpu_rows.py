@@ -8,6 +8,9 @@ import torch
 
 import paper_2607_18002_b200 as moe
 
+from gpu_util import assert_close, bind_ops, make_ctx, weights_to
+from workloads import synth
+
 from rows_util import EPS_FP32, gpu, half_step, plan, routing, tiny
 
 pytestmark = pytest.mark.gpu
@@ -146,6 +149,26 @@ def test_rows_far_into_a_large_buffer():
     assert torch.equal(moe.sort_rows(far, *args[:2], k), moe.sort_rows(dy, *args[:2], k))
 
 
+def test_results_of_more_than_four_giga_elements():
+    """R * H beyond 2^32: every row is where it belongs, checked on the GPU by two columns of every row and by sums."""
+    T, k, H, E = 8192, 32, 16512, 64
+    ids, w, offsets, s2f, f2s = routing(T, E, k, 6)
+    ds2f, df2s, dw = gpu(s2f, f2s, w)
+    x = torch.randint(-8, 9, (T, H), device="cuda", dtype=torch.int8).to(torch.bfloat16)
+    xs = moe.sort_rows(x, ds2f, df2s, k)
+    token = (ds2f // k).long()
+    for c in (0, H // 2 + 1, H - 1):
+        assert torch.equal(xs[:, c], x[token, c])
+    y = moe.merge_rows(xs, df2s, torch.ones_like(dw))              # whole numbers up to 256: exact
+    assert torch.equal(y.float(), (k * x.float()))
+    assert torch.equal(moe.sort_rows_grad(xs, df2s, k), y)
+    drows, dwt = moe.merge_rows_grad(x, xs, ds2f, df2s, torch.ones_like(dw))
+    for c in (0, H // 2 + 1, H - 1):
+        assert torch.equal(drows[:, c], x[token, c])
+    want = (x.float() ** 2).sum(1, keepdim=True).expand(T, k)      # whole numbers below 2^24: exact in any order
+    assert torch.equal(dwt, want)
+
+
 def test_results_do_not_depend_on_the_run():
     T, k, H = 700, 8, 2048
     ids, w, offsets, s2f, f2s = routing(T, 64, k, 9)
@@ -261,6 +284,26 @@ def test_with_the_librarys_own_route_and_plan():
     y = moe.merge_rows(xs, f2s, w)
     err = (y.double() - x.double()).abs()
     assert (err <= (half_step(torch.bfloat16) + (k + 8) * EPS_FP32) * x.double().abs() + tiny(torch.bfloat16)).all()
+
+
+def test_a_contexts_plan_with_experts_of_the_callers_own():
+    """The permutation of moe_plan serves both: experts computed here between sort and merge give what moe_run gives."""
+    spec = synth.Spec("rows", synth.Shape(8, 2, 512, 256), ((synth.PREFILL, 150),), "zipf", 1.0, 1.0, -1.0, 61)
+    W, (op,) = synth.make_weights(spec), synth.make_ops(spec)
+    ctx, Wd = make_ctx(spec), weights_to(W)
+    (b,) = bind_ops(ctx, [op], Wd)
+    ctx.plan(0, b)
+    ctx.run([0], fuse_combine=True)
+    ctx.check()
+    xs = moe.sort_rows(b.x, b.sorted_to_flat, b.flat_to_sorted, 2).float()
+    o = b.offsets.tolist()
+    rows = torch.empty(300, 512, dtype=torch.bfloat16, device="cuda")
+    for e in range(8):
+        h = xs[o[e]:o[e + 1]] @ Wd.w_gate_up[e].float().T
+        a = (torch.nn.functional.silu(h[:, :256]) * h[:, 256:]).to(torch.bfloat16).float()
+        rows[o[e]:o[e + 1]] = (a @ Wd.w_down[e].float().T).to(torch.bfloat16)
+    y = moe.merge_rows(rows, b.flat_to_sorted, b.topk_w)
+    assert_close(b.y.float().cpu().numpy(), y.float().cpu().numpy())
 
 
 def test_streams_graphs_and_several_batches():

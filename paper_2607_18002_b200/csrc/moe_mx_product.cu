@@ -182,6 +182,56 @@ __device__ __forceinline__ uint4 load_scales(const unsigned char* p, int left, i
 }
 __device__ __forceinline__ void st_word(unsigned saddr, unsigned v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(saddr), "r"(v) : "memory"); }
 
+// inclusive sum and maximum over the lanes
+__device__ __forceinline__ int scan_sum(int v, int lane) {
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int left = __shfl_up_sync(0xffffffffu, v, d);
+    if (lane >= d) v += left;
+  }
+  return v;
+}
+__device__ __forceinline__ int scan_max(int v, int lane) {
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int left = __shfl_up_sync(0xffffffffu, v, d);
+    if (lane >= d) v = max(v, left);
+  }
+  return v;
+}
+// Offsets -> ascending first rows, and the tiles before every expert; by one warp.  One expert a lane, or neighbouring ones: the maximum and the sum of
+// theirs are scanned, then they are gone through once more (256 experts: 1.3 us less than 32 at a time, 8 experts 0.3 us more than that).
+template <int kRows>
+__device__ __forceinline__ void list_tiles(MxShared& s, int E, int n_blocks, int lane) {
+  const int first = s.first_row[0];
+  if (E <= 32) {
+    const int to = max(scan_max(lane < E ? s.first_row[lane + 1] : 0, lane), first), left = __shfl_up_sync(0xffffffffu, to, 1);
+    const int mine = lane < E ? (to - (lane ? left : first) + kRows - 1) / kRows * n_blocks : 0, sum = scan_sum(mine, lane);
+    if (lane < E) {
+      s.first_row[lane + 1] = to;
+      s.first_tile[lane] = sum - mine;
+    }
+    if (lane == 31) s.first_tile[E] = sum;
+    return;
+  }
+  const int per = (E + 31) / 32, e0 = min(lane * per, E), e1 = min(e0 + per, E);
+  int top = first;
+  for (int e = e0; e < e1; ++e) top = max(top, s.first_row[e + 1]);
+  top = scan_max(top, lane);
+  int row = __shfl_up_sync(0xffffffffu, top, 1), tiles = 0;
+  if (lane == 0) row = first;
+  for (int e = e0; e < e1; ++e) {
+    const int to = max(row, s.first_row[e + 1]);
+    s.first_row[e + 1] = to;
+    s.first_tile[e] = tiles;
+    tiles += (to - row + kRows - 1) / kRows * n_blocks;
+    row = to;
+  }
+  const int sum = scan_sum(tiles, lane);
+  for (int e = e0; e < e1; ++e) s.first_tile[e] += sum - tiles;
+  if (lane == 31) s.first_tile[E] = sum;
+}
+
 struct Tile {
   int expert, row0, rows, n0;    // n0: first weight row (swiglu: first gate row)
   bool alone;                    // the expert's only tile of these weights
@@ -278,34 +328,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == 0) {
-    int before = 0, end = s.first_row[0];
-    for (int e0 = 0; e0 < a.E; e0 += 32) {
-      const int e = e0 + lane;
-      int to = e < a.E ? s.first_row[e + 1] : 0;
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, to, d);
-        if (lane >= d) to = max(to, v);
-      }
-      to = max(to, end);
-      const int left = __shfl_up_sync(0xffffffffu, to, 1), from = lane ? left : end;
-      const int mine = e < a.E ? (to - from + S::kRows - 1) / S::kRows * n_blocks : 0;
-      int sum = mine;
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, sum, d);
-        if (lane >= d) sum += v;
-      }
-      if (e < a.E) {
-        s.first_row[e + 1] = to;
-        s.first_tile[e] = before + sum - mine;
-      }
-      before += __shfl_sync(0xffffffffu, sum, 31);
-      end = __shfl_sync(0xffffffffu, to, 31);
-    }
-    if (lane == 0) s.first_tile[a.E] = before;
-  }
+  if (warp == 0) list_tiles<S::kRows>(s, a.E, n_blocks, lane);
   __syncthreads();
   if (kPair) cluster_sync_all();          // the other CTA's barriers exist before anything arrives on them
   const unsigned tmem = s.tmem;

@@ -196,23 +196,24 @@ def mx_quantize(x, sorted_to_flat=None, flat_to_sorted=None, top_k: int = 1, str
 
 
 def _codes(codes, scales, what, dims):
-    """Codes [..., K/2] and scales [..., K/32] of so many dimensions (0: any) -> the shape of the codes."""
+    """Codes [..., K/2] and scales [..., K/32] of so many dimensions (0: any) -> the shape of the codes and the number of their GPU."""
     if not isinstance(codes, _Tensor) or not isinstance(scales, _Tensor):
         _refuse(f"the codes and scales of {what} must be tensors")
-    shape, width = codes.shape, scales.shape
-    if codes.dtype is not _U8 or scales.dtype is not _U8 or not codes.is_cuda or codes.get_device() != scales.get_device() or not codes.is_contiguous() \
-            or not scales.is_contiguous() or (len(shape) != dims if dims else not shape) or not width or shape[-1] != 16 * width[-1] \
-            or shape[:-1] != width[:-1]:
+    shape, width, gpu = codes.shape, scales.shape, codes.get_device()
+    n = len(shape)
+    if codes.dtype is not _U8 or scales.dtype is not _U8 or not codes.is_cuda or gpu != scales.get_device() or not codes.is_contiguous() \
+            or not scales.is_contiguous() or (n != dims if dims else not n) or len(width) != n or shape[n - 1] != 16 * width[n - 1] \
+            or (shape[0] != width[0] and n > 1) or (n > 2 and shape[1:-1] != width[1:-1]):
         _refuse(f"the codes and scales of {what} must be contiguous uint8 tensors of {dims or 'some'} dimensions on one GPU, a scale for 16 bytes of codes")
-    return shape
+    return shape, gpu
 
 
 def mx_dequantize(codes, scales, dtype=_BF16, stream=None):
     """The values [..., K] that codes [..., K/2] with scales [..., K/32] stand for."""
     if dtype not in _DTYPES:
         _refuse(f"dtype must be one of {sorted(map(str, _DTYPES))}")
-    *lead, half = _codes(codes, scales, "the rows", 0)
-    gpu, K = codes.get_device(), 2 * half
+    (*lead, half), gpu = _codes(codes, scales, "the rows", 0)
+    K = 2 * half
     if stream is not None or gpu != _current_device():
         return _elsewhere(mx_dequantize, codes.device, stream, codes, scales, dtype)
     out = _empty(*lead, K, dtype=dtype, device=codes.device)
@@ -226,10 +227,9 @@ def mx_dequantize(codes, scales, dtype=_BF16, stream=None):
 
 def _operands(codes, scales, w_codes, w_scales, offsets):
     """-> number of the GPU, R, E, n, K"""
-    R, half = _codes(codes, scales, "the rows", 2)
-    E, n, w_half = _codes(w_codes, w_scales, "the weights", 3)
-    gpu = codes.get_device()
-    if w_half != half or w_codes.get_device() != gpu:
+    (R, half), gpu = _codes(codes, scales, "the rows", 2)
+    (E, n, w_half), w_gpu = _codes(w_codes, w_scales, "the weights", 3)
+    if w_half != half or w_gpu != gpu:
         _refuse(f"the weights must have {2 * half} columns and be on cuda:{gpu}, as the rows")
     _index(offsets, "offsets", E + 1, gpu)
     return gpu, R, E, n, 2 * half

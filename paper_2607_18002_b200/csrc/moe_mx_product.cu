@@ -7,12 +7,15 @@
 //
 // The weight rows are the M of the instruction (128 TMEM lanes), the tile's rows its N in steps of 16, so an expert with a few rows costs a few
 // columns.  A tile is 256 weight rows -- two accumulators; for swiglu 128 gate rows and the 128 up rows that go with them, so that a thread has
-// both factors of an output -- and up to kRows rows of one expert.  A thread of the epilogue has one weight row (one output column): a warp writes 32
-// neighbouring columns of a row at a time, and for swiglu those 32 are one block of the result, its largest magnitude one warp-wide maximum.
+// both factors of an output -- and up to kRows rows of one expert.  A pair of CTAs (cta_group::2) has twice the weight rows, M = 256, and each of the
+// two holds its own weight rows and half of the tile's rows in shared memory: swiglu with many rows an expert.
 //
-// One persistent CTA per SM walks the tiles (rows of an expert innermost: neighbours share a weight tile in L2).  Roles: one thread issues TMA
-// (a stage is 256 columns of K: 128-byte rows, swizzled), four warps bring the stage's scale bytes through registers into the 512-byte
-// form that tcgen05.cp copies to TMEM (128 rows x 4 blocks), one thread copies them and issues the MMAs, eight warps are the epilogue.
+// One persistent CTA (or pair) per SM walks the tiles (rows of an expert innermost: neighbours share a weight tile in L2).  Roles: one thread issues
+// TMA (a stage is 256 columns of K: 128-byte rows, swizzled), four warps bring the stage's scale bytes through registers into the 512-byte
+// form that tcgen05.cp copies to TMEM (128 rows x 4 blocks), one thread copies them and issues the MMAs, eight warps are the epilogue: for the plain
+// product through stmatrix and bulk copies, for swiglu a warp's 32 lanes have one 32-column block of the result, its largest magnitude one redux.
+// What bounds them: few rows, the weight stream; many, energy (65 536 rows of 64 experts, K 4096, inter 1792: gate/up 480-510 us, 3.8-4.0 PFLOP/s at 1 000 W;
+// down 340-360 us, 2.7 PFLOP/s and 537 MB of outputs).
 // Weights that one tile alone reads leave L2 first.  With other weights in every launch that makes no difference (800 rows of 128 experts, 1.5 GB, the
 // weight stream: gate/up 162 us, down 82, 6.1 TB/s); weights of about L2's size that come again gain 5-15 %.
 // Every wait is bounded; where one runs out the launch ends and what it has not computed is NaN.

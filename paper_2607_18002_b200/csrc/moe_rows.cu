@@ -12,8 +12,8 @@
 // or written for it; a row whose entry of s2f is outside [0, R) belongs to no token and is set to zero where rows are the output.
 //
 // Device time, bf16, and the rate of the bytes that have to move (a plain copy runs at 6.5 TB/s): 8 192 tokens x 8 slots x 4 096 columns sort 98 us
-// (6.2 TB/s), its gradient 89 us (6.8); 4 096 x 8 x 6 144 merge 68 us (6.6), its gradient 136 us (6.3); 16 384 x 2 x 4 096 64 and 122 us; one token
-// 2.2-2.5 us, launch included.  8 192 x 8 rows of odd width (3 001) move at 2.3-4.4 TB/s: accesses of two bytes.
+// (6.2 TB/s), its gradient 89 us (6.8); 4 096 x 8 x 6 144 merge 68 us (6.6), its gradient 134 us (6.4); 16 384 x 2 x 4 096 63 and 102 us; one token
+// 2.2-2.5 us, launch included.  8 192 x 8 rows of odd width (3 001) move at 2.6-4.4 TB/s: accesses of two bytes.
 #include <cuda_fp16.h>
 
 #include "moe_dev.cuh"
@@ -359,10 +359,10 @@ cudaError_t merge_launch(const void* rows, long long stride, const float* w, con
   constexpr int kV = 16 / sizeof(E);
   const int access = widest(bits(rows) | bits(y) | (unsigned long long)stride * sizeof(E) | (unsigned long long)H * sizeof(E)) / (int)sizeof(E);
   const int v = access >= kV ? kV : access >= 2 ? 2 : 1;
-  // Few columns: one access a slot and thread, so that more threads are at work.  Else about 8 rows' worth of 16 bytes in flight a thread, whatever k is and
+  // Few columns: one access a slot and thread (two of single elements), so that more threads are at work.  Else about 8 rows' worth of 16 bytes in flight a thread, whatever k is and
   // as near to it as narrow accesses come: 16 384 x 2 x 4 096 bf16 110 us with one access a slot, 67 with four.
   const bool few = (long long)T * (H / v) < kFillThreads;
-  const auto launch = v == 1   ? (few ? merge_launch_as<E, 1, 8, 1, kWeights> : merge_launch_as<E, 1, 8, 4, kWeights>)
+  const auto launch = v == 1   ? (few ? merge_launch_as<E, 1, 8, 2, kWeights> : merge_launch_as<E, 1, 8, 4, kWeights>)
                       : v == 2 ? (few ? merge_launch_as<E, 2, 8, 1, kWeights> : merge_launch_as<E, 2, 8, sizeof(E) == 4 ? 2 : 4, kWeights>)
                       : few || k > 4 ? merge_launch_as<E, kV, 8, 1, kWeights>
                       : k > 2        ? merge_launch_as<E, kV, 4, 2, kWeights>
@@ -373,8 +373,11 @@ cudaError_t merge_launch(const void* rows, long long stride, const float* w, con
 template <class E, int kV, int kSlots, int kPer>
 cudaError_t grad_launch_as(const void* dy, long long dy_stride, const void* rows, long long stride, const float* w, const int* s2f, const int* f2s,
                            void* drows, float* dw, int T, int k, int H, cudaStream_t stream) {
+  // Threads for a token: its columns in one go where tokens are few, in two where there are more of them than blocks fit on the GPU (8 192 x 8 x 2 048
+  // bf16 96 -> 90 us, 16 384 x 2 x 4 096 116 -> 102, 8 192 x 8 x 512 27 -> 24).
+  const int goes = T > 148 * 4 ? 2 : 1;
   int group = 32;
-  while (group < kRowThreads && group * kPer < H / kV) group *= 2;
+  while (group < kRowThreads && goes * group * kPer < H / kV) group *= 2;
   const int groups = kRowThreads / group;
   return launch_after(merge_grad_kernel<E, kV, kSlots, kPer>, (T + groups - 1) / groups, kRowThreads, 0, stream, static_cast<const E*>(dy), dy_stride,
                       static_cast<const E*>(rows), stride, w, s2f, f2s, static_cast<E*>(drows), dw, T, k, H, group);
@@ -386,7 +389,7 @@ cudaError_t grad_launch(const void* dy, long long dy_stride, const void* rows, l
   const int access = widest(bits(dy) | bits(rows) | bits(drows) | (unsigned long long)dy_stride * sizeof(E) | (unsigned long long)stride * sizeof(E) |
                             (unsigned long long)H * sizeof(E)) / (int)sizeof(E);
   const auto launch = access >= kV ? (k > 2 ? grad_launch_as<E, kV, 4, 1> : grad_launch_as<E, kV, 2, 2>)
-                      : access >= 2 ? grad_launch_as<E, 2, 4, 2> : grad_launch_as<E, 1, 4, 4>;
+                      : access >= 2 ? grad_launch_as<E, 2, 4, 2> : grad_launch_as<E, 1, 8, 2>;
   return launch(dy, dy_stride, rows, stride, w, s2f, f2s, drows, dw, T, k, H, stream);
 }
 

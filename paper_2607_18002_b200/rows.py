@@ -27,8 +27,10 @@ _BF16, _FP32, _I32, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.uint
 _DTYPES = {_BF16: moe.MOE_DTYPE_BF16, torch.float16: moe.MOE_DTYPE_FP16, _FP32: moe.MOE_DTYPE_FP32}
 _SORTED_DTYPES = {**_DTYPES, torch.float8_e4m3fn: moe.MOE_DTYPE_FP8_E4M3, _U8: moe.MOE_DTYPE_FP8_E4M3}
 _Tensor, _empty = torch.Tensor, torch.empty
-_current_device = torch.cuda.current_device
-_stream = moe.Context._stream
+# the current device's number and the handle of its current stream: the functions of torch that read them without objects around them, where it has them
+_current_device, _stream = (getattr(torch._C, n, None) for n in ("_cuda_getDevice", "_cuda_getCurrentRawStream"))
+if _current_device is None or _stream is None:
+    _current_device, _stream = torch.cuda.current_device, lambda gpu: torch.cuda.current_stream(gpu).cuda_stream
 
 
 def _refuse(what):
@@ -80,7 +82,7 @@ def sort_rows(x, sorted_to_flat, flat_to_sorted, top_k: int, stream=None):
     _index(flat_to_sorted, "flat_to_sorted", T * top_k, gpu)
     xs = x.new_empty(T * top_k, H)
     rc = (moe._lib or moe.lib()).moe_sort_rows(x.data_ptr(), step, _SORTED_DTYPES[x.dtype], T, top_k, H, sorted_to_flat.data_ptr(),
-                                               flat_to_sorted.data_ptr(), xs.data_ptr(), _stream(None))
+                                               flat_to_sorted.data_ptr(), xs.data_ptr(), _stream(gpu))
     if rc:
         _failed(rc, "moe_sort_rows")
     return xs
@@ -98,7 +100,7 @@ def sort_rows_grad(dxs, flat_to_sorted, top_k: int, stream=None):
     T = R // top_k
     dx = dxs.new_empty(T, H)
     rc = (moe._lib or moe.lib()).moe_sort_rows_grad(dxs.data_ptr(), step, _DTYPES[dxs.dtype], T, top_k, H, flat_to_sorted.data_ptr(),
-                                                    dx.data_ptr(), _stream(None))
+                                                    dx.data_ptr(), _stream(gpu))
     if rc:
         _failed(rc, "moe_sort_rows_grad")
     return dx
@@ -121,7 +123,7 @@ def merge_rows(rows, flat_to_sorted, topk_w, stream=None):
     _index(flat_to_sorted, "flat_to_sorted", R, gpu)
     y = rows.new_empty(T, H)
     rc = (moe._lib or moe.lib()).moe_merge_rows(rows.data_ptr(), step, _DTYPES[rows.dtype], topk_w.data_ptr(), T, k, H,
-                                                flat_to_sorted.data_ptr(), y.data_ptr(), _stream(None))
+                                                flat_to_sorted.data_ptr(), y.data_ptr(), _stream(gpu))
     if rc:
         _failed(rc, "moe_merge_rows")
     return y
@@ -142,7 +144,7 @@ def merge_rows_grad(dy, rows, sorted_to_flat, flat_to_sorted, topk_w, stream=Non
     drows, dw = rows.new_empty(R, H), topk_w.new_empty(T, k)
     rc = (moe._lib or moe.lib()).moe_merge_rows_grad(dy.data_ptr(), dy_step, rows.data_ptr(), step, _DTYPES[rows.dtype], topk_w.data_ptr(), T, k, H,
                                                      sorted_to_flat.data_ptr(), flat_to_sorted.data_ptr(), drows.data_ptr(), dw.data_ptr(),
-                                                     _stream(None))
+                                                     _stream(gpu))
     if rc:
         _failed(rc, "moe_merge_rows_grad")
     return drows, dw
@@ -161,7 +163,7 @@ def route_grad(topk_ids, topk_w, d_topk_w, n_experts: int, stream=None):
     T, k = shape
     dz = topk_w.new_empty(T, n_experts)
     rc = (moe._lib or moe.lib()).moe_route_grad(topk_ids.data_ptr(), topk_w.data_ptr(), d_topk_w.data_ptr(), T, n_experts, k, dz.data_ptr(),
-                                                _stream(None))
+                                                _stream(gpu))
     if rc:
         _failed(rc, "moe_route_grad")
     return dz
@@ -189,7 +191,7 @@ def mx_quantize(x, sorted_to_flat=None, flat_to_sorted=None, top_k: int = 1, str
     codes = _empty(R, K // 2, dtype=_U8, device=x.device)
     scales = codes.new_empty(R, K // 32)
     rc = (moe._lib or moe.lib()).moe_mx_quantize(x.data_ptr(), step, _DTYPES[x.dtype], T, top_k, K, s2f, f2s, codes.data_ptr(),
-                                                 scales.data_ptr(), _stream(None))
+                                                 scales.data_ptr(), _stream(gpu))
     if rc:
         _failed(rc, "moe_mx_quantize")
     return codes, scales
@@ -219,7 +221,7 @@ def mx_dequantize(codes, scales, dtype=_BF16, stream=None):
     out = _empty(*lead, K, dtype=dtype, device=codes.device)
     if K:
         rc = (moe._lib or moe.lib()).moe_mx_dequantize(codes.data_ptr(), scales.data_ptr(), out.numel() // K, K, _DTYPES[dtype], out.data_ptr(),
-                                                       _stream(None))
+                                                       _stream(gpu))
         if rc:
             _failed(rc, "moe_mx_dequantize")
     return out
@@ -242,7 +244,7 @@ def mx_product(codes, scales, w_codes, w_scales, offsets, stream=None):
         return _elsewhere(mx_product, codes.device, stream, codes, scales, w_codes, w_scales, offsets)
     out = _empty(R, n, dtype=_BF16, device=codes.device)
     rc = (moe._lib or moe.lib()).moe_mx_product(codes.data_ptr(), scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), offsets.data_ptr(), R, E,
-                                                n, K, out.data_ptr(), _stream(None))
+                                                n, K, out.data_ptr(), _stream(gpu))
     if rc:
         _failed(rc, "moe_mx_product")
     return out
@@ -257,7 +259,7 @@ def mx_swiglu(codes, scales, w_codes, w_scales, offsets, stream=None):
         return _elsewhere(mx_swiglu, codes.device, stream, codes, scales, w_codes, w_scales, offsets)
     out, out_scales = codes.new_empty(R, n // 4), codes.new_empty(R, n // 64)
     rc = (moe._lib or moe.lib()).moe_mx_swiglu(codes.data_ptr(), scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), offsets.data_ptr(), R, E,
-                                               n // 2, K, out.data_ptr(), out_scales.data_ptr(), _stream(None))
+                                               n // 2, K, out.data_ptr(), out_scales.data_ptr(), _stream(gpu))
     if rc:
         _failed(rc, "moe_mx_swiglu")
     return out, out_scales

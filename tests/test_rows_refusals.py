@@ -72,6 +72,19 @@ def test_contexts_compute_in_their_own_types_only(lib):
             moe.moe_workspace_bytes(moe.moe_config_t(8, 2, 256, 128, dtype, 16, 1, 0, 0, 0))
 
 
+def test_stream_and_device_are_read_the_public_way_where_torch_lacks_the_other(monkeypatch):
+    import importlib.util
+    import types
+    from paper_2607_18002_b200 import rows
+    for name in ("_cuda_getDevice", "_cuda_getCurrentRawStream"):
+        monkeypatch.delattr(torch._C, name, raising=False)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda gpu: types.SimpleNamespace(cuda_stream=40 + gpu))
+    spec = importlib.util.spec_from_file_location("rows_without", rows.__file__)
+    again = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(again)
+    assert again._current_device is torch.cuda.current_device and again._stream(2) == 42
+
+
 def test_tensors_on_the_host_are_refused():
     x, i, w = torch.zeros(4, 64), torch.zeros(8, dtype=torch.int32), torch.zeros(4, 2)
     c, s = torch.zeros(8, 64, dtype=torch.uint8), torch.zeros(8, 4, dtype=torch.uint8)

@@ -13,9 +13,13 @@
 // One persistent CTA (or pair) per SM walks the tiles (rows of an expert innermost: neighbours share a weight tile in L2).  Roles: one thread issues
 // TMA (a stage is 256 columns of K: 128-byte rows, swizzled), four warps bring the stage's scale bytes through registers into the 512-byte
 // form that tcgen05.cp copies to TMEM (128 rows x 4 blocks), one thread copies them and issues the MMAs, eight warps are the epilogue: for the plain
-// product through stmatrix and bulk copies, for swiglu a warp's 32 lanes have one 32-column block of the result, its largest magnitude one redux.
-// What bounds them: few rows, the weight stream; many, energy (65 536 rows of 64 experts, K 4096, inter 1792: gate/up 480-510 us, 3.8-4.0 PFLOP/s at 1 000 W;
-// down 340-360 us, 2.7 PFLOP/s and 537 MB of outputs).
+// product through stmatrix and bulk copies, for swiglu a warp's 32 lanes have one 32-column block of the result.
+// What bounds them: few rows, the weight stream; many, energy (65 536 rows of 64 experts, K 4096, inter 1792: gate/up 465-490 us, 3.9-4.1 PFLOP/s at 1 000 W;
+// down 325-345 us, 2.8-3.0 PFLOP/s and 537 MB of outputs).
+// Code size counts: after another kernel, or a long stream through L2, the first tile waits for instructions from DRAM, and within a launch five
+// roles share the instruction caches.  So the roles' loops are not unrolled and exist once, values that are alike in a warp are made known as such, and
+// the block maxima go over pairs (40-63 KB a kernel that were 110-165, the untaken forms included; gate/up and down in turn 10-20 % faster at 64-1 024
+// rows an expert, 15 % at one).  Executing the epilogue once without effects before the first tile, or one kernel for both products, then gained nothing.
 // Weights that one tile alone reads leave L2 first.  With other weights in every launch that makes no difference (800 rows of 128 experts, 1.5 GB, the
 // weight stream: gate/up 162 us, down 82, 6.1 TB/s); weights of about L2's size that come again gain 5-15 %.
 // Every wait is bounded; where one runs out the launch ends and what it has not computed is NaN.
@@ -86,6 +90,7 @@ __device__ __forceinline__ bool wait(unsigned long long* bar, unsigned parity, v
   if (kTry(bar, parity)) return true;
   const unsigned long long start = gtime_ns();
   for (;;) {
+#pragma unroll 1
     for (int i = 0; i < 64; ++i)
       if (kTry(bar, parity)) return true;
     if (*dead) return false;
@@ -162,7 +167,6 @@ __device__ __forceinline__ void tc_ld16(unsigned taddr, unsigned (&r)[16]) {
       : "r"(taddr)
       : "memory");
 }
-
 // 16 bytes of a row's scales, `left` of which are there (the others are not used), by loads of vec bytes
 __device__ __forceinline__ uint4 load_scales(const unsigned char* p, int left, int vec) {
   uint4 v = make_uint4(0u, 0u, 0u, 0u);
@@ -219,10 +223,12 @@ __device__ __forceinline__ void list_tiles(MxShared& s, int E, int n_blocks, int
   }
   const int per = (E + 31) / 32, e0 = min(lane * per, E), e1 = min(e0 + per, E);
   int top = first;
+#pragma unroll 1
   for (int e = e0; e < e1; ++e) top = max(top, s.first_row[e + 1]);
   top = scan_max(top, lane);
   int row = __shfl_up_sync(0xffffffffu, top, 1), tiles = 0;
   if (lane == 0) row = first;
+#pragma unroll 1
   for (int e = e0; e < e1; ++e) {
     const int to = max(row, s.first_row[e + 1]);
     s.first_row[e + 1] = to;
@@ -231,6 +237,7 @@ __device__ __forceinline__ void list_tiles(MxShared& s, int E, int n_blocks, int
     row = to;
   }
   const int sum = scan_sum(tiles, lane);
+#pragma unroll 1
   for (int e = e0; e < e1; ++e) s.first_tile[e] += sum - tiles;
   if (lane == 31) s.first_tile[E] = sum;
 }
@@ -251,6 +258,11 @@ __device__ __forceinline__ Tile tile_at(const MxShared& s, int E, int t, int n_s
   return Tile{lo, s.first_row[lo] + m * kRows, min(kRows, rows - m * kRows), n * n_step, m_tiles == 1};
 }
 
+// Lane 0's value: the compiler then knows that it is the same in all lanes.  Without that it guards every shuffle, vote and matrix store that stands
+// behind a branch on it (gate/up 85 instead of 62 KB, 2-5 % of the time).
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
+__device__ __forceinline__ Tile uniform(const Tile& t) { return Tile{uniform(t.expert), uniform(t.row0), uniform(t.rows), uniform(t.n0), t.alone}; }
+
 // silu(g) u in fp32: exp(-g) = 2^(-g log2 e) to 2 + 1.2 |g| steps, the reciprocal to one.  Powers below 2^-126 and reciprocals of those above 2^126 count
 // as 0 (nothing next to the 1 that is added, silu of less than -87): the forms that keep them take three instructions more each.
 __device__ __forceinline__ float silu_times(float g, float u) {
@@ -259,15 +271,50 @@ __device__ __forceinline__ float silu_times(float g, float u) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
   return g * r * u;
 }
+// eight codes, the first in the lowest bits
+__device__ __forceinline__ unsigned mx_codes8(const float* q) {
+  unsigned r;
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\tmov.b32 %0, {a, b, c, d};\n\t}"
+      : "=r"(r)
+      : "f"(q[0]), "f"(q[1]), "f"(q[2]), "f"(q[3]), "f"(q[4]), "f"(q[5]), "f"(q[6]), "f"(q[7]));
+  return r;
+}
+__device__ __forceinline__ unsigned max_u16x2(unsigned a, unsigned b) {
+  unsigned r;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ unsigned min_u16x2(unsigned a, unsigned b) {
+  unsigned r;
+  asm("min.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+// Exponent fields (bits 7 to 14) of the largest of the 32 lanes' v[r], in the low half, and of their v[r + 8], in the high half, for r = lane % 8.  The
+// upper halves of floats as pairs of 16 bits; three steps halve the pairs that a lane follows, two more join the lanes of equal r (50 instructions
+// where sixteen reductions over the warp compile to about 240).
+__device__ __forceinline__ unsigned block_exponents(const float (&v)[16], int lane) {
+  unsigned p[8];
+#pragma unroll
+  for (int r = 0; r < 8; ++r) p[r] = __byte_perm(__float_as_uint(v[r]), __float_as_uint(v[r + 8]), 0x7632) & 0x7f807f80u;
+#pragma unroll
+  for (int s = 4; s >= 1; s >>= 1)
+#pragma unroll
+    for (int r = 0; r < s; ++r) {
+      const bool upper = lane & s;
+      const unsigned other = __shfl_xor_sync(0xffffffffu, upper ? p[r] : p[r + s], s);
+      p[r] = max_u16x2(upper ? p[r + s] : p[r], other);
+    }
+  p[0] = max_u16x2(p[0], __shfl_xor_sync(0xffffffffu, p[0], 8));
+  return max_u16x2(p[0], __shfl_xor_sync(0xffffffffu, p[0], 16));
+}
 // 8 x 8 four-bit values over eight neighbouring lanes: lane i gives value j of word i, gets value i of word j
 __device__ __forceinline__ unsigned transpose_nibbles(unsigned v, int lane) {
-#pragma unroll
-  for (int s = 4; s >= 1; s >>= 1) {
-    const unsigned low = s == 4 ? 0x0000ffffu : s == 2 ? 0x00ff00ffu : 0x0f0f0f0fu;
-    const unsigned other = __shfl_xor_sync(0xffffffffu, v, s);
-    v = lane & s ? (v & ~low) | ((other & ~low) >> (4 * s)) : (v & low) | ((other & low) << (4 * s));
-  }
-  return v;
+  v = __byte_perm(v, __shfl_xor_sync(0xffffffffu, v, 4), lane & 4 ? 0x3276 : 0x5410);
+  v = __byte_perm(v, __shfl_xor_sync(0xffffffffu, v, 2), lane & 2 ? 0x3715 : 0x6240);
+  const unsigned other = __shfl_xor_sync(0xffffffffu, v, 1), theirs = lane & 1 ? 0x0f0f0f0fu : 0xf0f0f0f0u;
+  return (v & ~theirs) | (__funnelshift_l(other, other, lane & 1 ? 28 : 4) & theirs);
 }
 
 __device__ __forceinline__ unsigned pack_bf16(unsigned lo, unsigned hi) {
@@ -295,7 +342,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
   unsigned char* stages = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   unsigned char* store_bufs = stages + S::kStages * S::kStageBytes;
   MxShared& s = *reinterpret_cast<MxShared*>(store_bufs + S::kStoreBytes);
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
   constexpr int kCtas = kPair ? 2 : 1;
   constexpr int kStep = (kSwiglu ? 1 : 2) * kHalfRows * kCtas;     // output columns of a tile
   const unsigned rank = kPair ? cluster_ctarank() : 0u;            // weight rows of an accumulator: this CTA has the rank-th 128
@@ -327,6 +374,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
     }
   }
   grid_dep_wait();
+#pragma unroll 1
   for (int e = tid; e <= a.E; e += kMxThreads) s.first_row[e] = min(max(a.offsets[e], 0), a.R);
   tc_fence_before();
   __syncthreads();
@@ -335,7 +383,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
   __syncthreads();
   if (kPair) cluster_sync_all();          // the other CTA's barriers exist before anything arrives on them
   const unsigned tmem = s.tmem;
-  const int n_tiles = s.first_tile[a.E];
+  const int n_tiles = uniform(s.first_tile[a.E]);
   const int n_stages = (a.K + kStageK - 1) / kStageK;
 
   if (warp < kTmaWarp) {
@@ -344,7 +392,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
     unsigned k = 0, stored = 0;  // tiles, groups of outputs so far
     bool ok = true;
     for (int t = unit; t < n_tiles; t += n_units, ++k) {
-      const Tile at = tile_at<S::kRows>(s, a.E, t, kStep);
+      const Tile at = uniform(tile_at<S::kRows>(s, a.E, t, kStep));
       const unsigned buf = k % S::kAccBufs, use = k / S::kAccBufs;
       if (ok) ok = __all_sync(0xffffffffu, wait(&s.acc_full[buf], use & 1, &s.dead));
       tc_fence_after();
@@ -360,7 +408,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
           else mbar_arrive(&s.acc_empty[buf]);
         }
       };
-      const int groups = (at.rows + 15) / 16;
+      const int groups = uniform((at.rows + 15) / 16);
       if (!kSwiglu) {            // warps 0-3 have the first accumulator, 4-7 the second
         const unsigned mine = acc + half * S::kRows;
         const int col0 = at.n0 + (half * kCtas + (int)rank) * kHalfRows;      // of these four warps' 128 output columns
@@ -415,33 +463,29 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
       } else {                   // warps 0-3 and 4-7 take turns at groups of 16 rows
         const int col = at.n0 + (int)rank * kHalfRows + quad * 32, per_row = a.I / kMxBlock;
         const auto store = [&](const float (&v)[16], int c) {
+          const unsigned top = block_exponents(v, lane), inverse = min_u16x2(0x80008000u - top, 0x7f007f00u);     // of 2^(127 - scale byte)
+          float q[16];
 #pragma unroll
-          for (int j0 = 0; j0 < 16; j0 += 8) {
-            unsigned word = 0u, mine = 0u;
+          for (int r = 0; r < 8; ++r) {
+            const unsigned both = __shfl_sync(0xffffffffu, inverse, r);
+            q[r] = v[r] * __uint_as_float(both << 16);
+            q[r + 8] = v[r + 8] * __uint_as_float(both & 0xffff0000u);
+          }
 #pragma unroll
-            for (int j = 0; j < 8; j += 2) {
-              float q[2];
-#pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                const unsigned top = __reduce_max_sync(0xffffffffu, __float_as_uint(v[j0 + j + i]) & 0x7f800000u);
-                if ((lane & 7) == j + i) mine = top;
-                q[i] = v[j0 + j + i] * __uint_as_float(min(0x80000000u - top, 0x7f000000u));     // 2^(127 - scale byte)
-              }
-              word |= mx_codes2(q[0], q[1]) << (4 * j);
-            }
-            word = transpose_nibbles(word, lane);            // lane 8 i + j: columns 8 i .. 8 i + 7 of row j
-            const int row = c + j0 + (lane & 7);
+          for (int h = 0; h < 2; ++h) {
+            const unsigned word = transpose_nibbles(mx_codes8(q + 8 * h), lane);         // lane 8 i + j: columns 8 i .. 8 i + 7 of row j
+            const int row = c + 8 * h + (lane & 7);
             if (row < at.rows && col < a.I) {
               const size_t p = (size_t)(at.row0 + row);
               *reinterpret_cast<unsigned*>(static_cast<unsigned char*>(a.out) + p * (a.I / 2) + col / 2 + (lane >> 3) * 4) = word;
-              if (lane < 8) a.out_scales[p * per_row + col / kMxBlock] = (unsigned char)(ok ? mx_scale_byte(mine) : 255u);
+              if (lane < 8) a.out_scales[p * per_row + col / kMxBlock] = (unsigned char)(ok ? mx_scale_byte((h ? top : top << 16) & 0x7f800000u) : 255u);
             }
           }
         };
-        constexpr int kMine = (S::kGroups + 1) / 2, kAsTheyAre = kMine < 3 ? 1 : 2, kFirst = kMine - kAsTheyAre;
+        constexpr int kFirst = (S::kGroups + 1) / 2 - 1;
         const int my_groups = (groups - half + 1) / 2;
-        float v[kFirst > 0 ? kFirst : 1][16];
-        unsigned gate[kAsTheyAre][16], up[kAsTheyAre][16];
+        float v[kFirst][16];
+        unsigned gate[16], up[16];
         const auto load = [&](unsigned (&g)[16], unsigned (&u)[16], int i) {
           tc_ld16(acc + 16 * (half + 2 * i), g);
           tc_ld16(acc + S::kRows + 16 * (half + 2 * i), u);
@@ -458,20 +502,16 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
             tc_wait_ld();
             activate(g, u, v[i]);
           }
-#pragma unroll
-        for (int i = 0; i < kAsTheyAre; ++i)
-          if (kFirst + i < my_groups) load(gate[i], up[i], kFirst + i);
+        if (kFirst < my_groups) load(gate, up, kFirst);
         hand_back();
 #pragma unroll
         for (int i = 0; i < kFirst; ++i)
           if (i < my_groups) store(v[i], 16 * (half + 2 * i));
-#pragma unroll
-        for (int i = 0; i < kAsTheyAre; ++i)
-          if (kFirst + i < my_groups) {
-            float w[16];
-            activate(gate[i], up[i], w);
-            store(w, 16 * (half + 2 * (kFirst + i)));
-          }
+        if (kFirst < my_groups) {
+          float w[16];
+          activate(gate, up, w);
+          store(w, 16 * (half + 2 * kFirst));
+        }
       }
     }
     asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
@@ -480,6 +520,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
     const int lo = s.first_row[0], hi = s.first_row[a.E], none = lo + (a.R - hi);
     for (int i = blockIdx.x; i < none; i += gridDim.x) {
       const size_t p = (size_t)(i < lo ? i : hi + (i - lo));
+#pragma unroll 1
       for (size_t c = tid; c < width; c += 256) {
         if (!kSwiglu) static_cast<__nv_bfloat16*>(a.out)[p * a.N + c] = __float2bfloat16_rn(0.f);
         else if (c < (size_t)a.I / 2) static_cast<unsigned char*>(a.out)[p * (a.I / 2) + c] = 0;
@@ -498,6 +539,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
           const bool second = kSwiglu || at.n0 + kHalfRows * kCtas < a.N;
           const unsigned long long policy = at.alone ? l2_evict_first() : l2_evict_normal();
           const int n0 = at.n0 + (int)rank * kHalfRows;
+#pragma unroll 1
           for (int i = 0; i < n_stages; ++i, ++n) {
             const unsigned slot = n % S::kStages, round = n / S::kStages;
             if (round && !wait(&s.empty[slot], (round - 1) & 1, &s.dead)) break;
@@ -506,6 +548,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
             expect_tx(bar, (second ? S::kWBytes : S::kWBytes / 2) + boxes * kBoxRows * 128);
             tma_3d<kPair>(to, &a.tm_w, i * 128, n0, at.expert, bar, policy);
             if (second) tma_3d<kPair>(to + kHalfRows * 128, &a.tm_w, i * 128, n0 + (kSwiglu ? a.I : kHalfRows * kCtas), at.expert, bar, policy);
+#pragma unroll 1
             for (int b = 0; b < boxes; ++b) tma_2d<kPair>(to + S::kWBytes + b * kBoxRows * 128, &a.tm_x, i * 128, row0 + b * kBoxRows, bar);
           }
         }
@@ -534,6 +577,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
           const unsigned cols = kPair ? (unsigned)(at.rows + 31) & ~31u : (unsigned)(at.rows + 15) & ~15u;
           const bool second = kSwiglu || at.n0 + kHalfRows * kCtas < a.N;
           const unsigned acc = tmem + buf * 2 * S::kRows;
+#pragma unroll 1
           for (int i = 0; i < n_stages; ++i, ++n) {
             const unsigned slot = n % S::kStages, round = n / S::kStages;
             ok = wait(&s.full[slot], round & 1, &s.dead) && wait(&s.landed[slot], round & 1, &s.dead);
@@ -542,6 +586,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
             const unsigned st = smem_u32(stages + slot * S::kStageBytes);
             const unsigned sc = st + S::kWBytes + S::kXBytes, tsc = tmem + S::kScaleCol0 + slot * S::kScaleCols;
             const int groups = min(2, (a.K - i * kStageK) / kGroupK);
+#pragma unroll 1
             for (int g = 0; g < groups; ++g) {
               const unsigned from = sc + g * (2 + S::kRowBlocks) * kScaleBlock, to = tsc + g * (2 + S::kRowBlocks) * 4;
 #pragma unroll
@@ -573,8 +618,8 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
     const int pair = lane & 1, r0 = 32 * (lane >> 1 & 3) + 4 * (warp - kScaleWarp) + (lane >> 3);      // and r0 + 16
     const unsigned spot = (unsigned)(r0 & 31) * 16 + (unsigned)(r0 >> 5) * 4;
     const int per_row = a.K / kMxBlock, n_quads = (n_stages + 3) / 4;
-    const int vec = per_row % 16 == 0 ? 16 : per_row % 8 == 0 ? 8 : 4;
-    const int vec_w = (size_t)a.w_scales & (vec - 1) ? 4 : vec, vec_x = (size_t)a.x_scales & (vec - 1) ? 4 : vec;
+    const int places = per_row | (int)(size_t)a.w_scales | (int)(size_t)a.x_scales;
+    const int vec = places % 16 == 0 ? 16 : places % 8 == 0 ? 8 : 4;
     constexpr int kBlocks = 2 + S::kRowBlocks;
     struct Quad {
       uint4 b[kBlocks][2];
@@ -590,28 +635,32 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
       const int from = quad * 32 + pair * 16, left = per_row - from;
       const unsigned char* w = a.w_scales + (size_t)at.expert * a.N * per_row + from;
       const unsigned char* x = a.x_scales + (size_t)at.row0 * per_row + from;
+      const auto rows = [&](const int bytes) {
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const int r = r0 + 16 * q;
+        for (int q = 0; q < 2; ++q) {
+          const int r = r0 + 16 * q;
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {      // a weight row behind the last one: any other's scales (its products are not stored)
-          const int row = kSwiglu ? min(at.n0 + (int)rank * kHalfRows + r, a.I - 1) + b * a.I
-                                  : min(at.n0 + (b * kCtas + (int)rank) * kHalfRows + r, a.N - 1);
-          p.b[b][q] = load_scales(w + (size_t)row * per_row, left, vec_w);
+          for (int b = 0; b < 2; ++b) {    // a weight row behind the last one: any other's scales (its products are not stored)
+            const int row = kSwiglu ? min(at.n0 + (int)rank * kHalfRows + r, a.I - 1) + b * a.I
+                                    : min(at.n0 + (b * kCtas + (int)rank) * kHalfRows + r, a.N - 1);
+            p.b[b][q] = load_scales(w + (size_t)row * per_row, left, bytes);
+          }
+#pragma unroll
+          for (int b = 0; b < S::kRowBlocks; ++b) p.b[2 + b][q] = load_scales(x + (size_t)min(b * 128 + r, at.rows - 1) * per_row, left, bytes);
         }
-#pragma unroll
-        for (int b = 0; b < S::kRowBlocks; ++b) p.b[2 + b][q] = load_scales(x + (size_t)min(b * 128 + r, at.rows - 1) * per_row, left, vec_x);
-      }
+      };
+      if (vec == 16) rows(16);
+      else if (vec == 8) rows(8);
+      else rows(4);
       p.stages = min(4, n_stages - 4 * quad);
       if (++quad == n_quads) {
         quad = 0;
         t += n_units;
       }
     };
-    const auto put = [&](const Quad& p) {
-#pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        if (h >= p.stages) break;
+    const auto put = [&](const Quad& p) {    // false: gave up
+#pragma unroll 1
+      for (int h = 0; h < p.stages; ++h) {
         const unsigned slot = n % S::kStages, round = n / S::kStages;
         if (round && !__all_sync(0xffffffffu, wait(&s.empty[slot], (round - 1) & 1, &s.dead))) return false;
         if (pair == h / 2) {
@@ -635,14 +684,14 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
       }
       return true;
     };
-    Quad even, odd;
-    fetch(even);
-    while (even.stages) {
-      fetch(odd);
-      if (!put(even) || !odd.stages) break;
-      fetch(even);
-      if (!put(odd)) break;
-    }
+    Quad now, next;
+    now.stages = 0;
+#pragma unroll 1
+    do {
+      fetch(next);
+      if (!put(now)) break;
+      now = next;
+    } while (now.stages);
   }
   __syncwarp();
   tc_fence_before();
@@ -737,18 +786,19 @@ int product(const void* codes, const void* scales, const void* w_codes, const vo
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   // The tile's height goes by the rows that an expert gets on average (the host does not know more).  Two buffers of 96 columns let the epilogue of a tile
   // run beside the next one's MMAs; 192 columns take the weights from L2 half as often, and for gate/up a pair of CTAs takes half of the rows each.
-  // us (gate/up, down), weights that are not in L2:
-  //   rows an expert                   32          64          128         256         384         512         1024      2048
+  // us (gate/up; down; both in turn), weights that are not in L2:
+  //   rows an expert            64              128             192             256             320             384             512             1024
   //   even, 32 experts, 4096 x 1792
-  //     96 rows                        50.2, 24.9  51.9, 26.3  74.4, 39.9  103, 57.7   136, 76.8   191, 104    347, 191  678, 369
-  //     192 rows                       52.9, 25.9  56.0, 28.3  64.9, 35.5  107, 63.5   119, 74.8   151, 95.2   294, 176  505, 314
-  //     192 rows, pairs                53.9, 29.4  57.0, 30.7  64.9, 36.5  98.6, 65.9  109, 76.8   144, 94.7   257, 181  462, 327
+  //     96 rows                 50; 24; 78      69; 37; 106     82; 47; 129     100; 56; 156    128; 72; 200    142; 81; 223    189; 106; 295   346; 195; 541
+  //     192 rows                52; 26; 83      59; 30; 99      77; 50; 134     98; 58; 161     102; 59; 169    115; 73; 194    141; 86; 236    266; 168; 439
+  //     gate/up on pairs        54; 26; 86      59; 30; 100     72; 50; 130     92; 58; 157     97; 59; 166     108; 73; 187    133; 86; 227    242; 168; 418
   //   uneven (Zipf 0.8), 64 experts, 2048 x 768
-  //     96 rows                        23.6, 16.7  29.3, 19.8              52.9, 44.0              84.7, 72.4
-  //     192 rows                       28.0, 19.1  31.4, 23.9              56.0, 45.1              98.3, 72.7
-  //     192 rows, pairs                29.7, 21.8  32.1, 26.3              50.9, 48.1              82.9, 77.5
-  // Tiles of 64 and 32 rows are left out: 0-7 % faster below 32 rows an expert, up to 25 % slower at 64.
-  const bool many = n_rows > (kSwiglu ? 192ll : 320ll) * n_experts;
+  //     96 rows                 26; 18; 46      31; 25; 56      40; 34; 74      49; 41; 90      54; 49; 104     62; 55; 119     79; 69; 149     149; 132; 282
+  //     192 rows                27; 21; 52      36; 28; 73      37; 35; 82      44; 40; 94      52; 49; 110     59; 55; 125     74; 67; 150     128; 123; 261
+  //     gate/up on pairs        28; 21; 54      36; 28; 74      37; 35; 83      44; 40; 96      50; 49; 110     57; 55; 122     71; 67; 148     122; 123; 256
+  // The down product on pairs takes 10 % longer than single (65 536 rows: 359 and 326).  Tiles of 64 and 32 rows are left out: 0-7 % faster below 32 rows
+  // an expert, up to 25 % slower at 64.
+  const bool many = n_rows > 256ll * n_experts;
   const cudaError_t e = many ? product_launch<192, kSwiglu, kSwiglu>(a, st) : product_launch<96, kSwiglu, false>(a, st);
   return e == cudaSuccess ? MOE_OK : MOE_ECUDA;
 }

@@ -13,9 +13,9 @@
 // One persistent CTA (or pair) per SM walks the tiles (rows of an expert innermost: neighbours share a weight tile in L2).  Roles: one thread issues
 // TMA (a stage is 256 columns of K: 128-byte rows, swizzled), four warps bring the stage's scale bytes through registers into the 512-byte
 // form that tcgen05.cp copies to TMEM (128 rows x 4 blocks), one thread copies them and issues the MMAs, eight warps are the epilogue: for the plain
-// product through stmatrix and bulk copies, for swiglu a warp's 32 lanes have one 32-column block of the result.
+// product through stmatrix and shared memory, for swiglu a warp's 32 lanes have one 32-column block of the result.
 // What bounds them: few rows, the weight stream; many, energy (65 536 rows of 64 experts, K 4096, inter 1792: gate/up 465-490 us, 3.9-4.1 PFLOP/s at 1 000 W;
-// down 325-345 us, 2.8-3.0 PFLOP/s and 537 MB of outputs).
+// down 310-325 us, 3.0-3.1 PFLOP/s and 537 MB of outputs).
 // Code size counts: after another kernel, or a long stream through L2, the first tile waits for instructions from DRAM, and within a launch five
 // roles share the instruction caches.  So the roles' loops are not unrolled and exist once, values that are alike in a warp are made known as such, and
 // the block maxima go over pairs (40-63 KB a kernel that were 110-165, the untaken forms included; gate/up and down in turn 10-20 % faster at 64-1 024
@@ -329,11 +329,11 @@ __device__ __forceinline__ void tc_ld_frag16(unsigned taddr, unsigned (&r)[8]) {
                : "r"(taddr)
                : "memory");
 }
-__device__ __forceinline__ void bulk_store(void* to, unsigned from, int bytes) {
-  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(to), "r"(from), "r"(bytes) : "memory");
+__device__ __forceinline__ uint4 ld_shared16(unsigned saddr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(saddr) : "memory");
+  return v;
 }
-__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 
 template <int kRows_, bool kSwiglu, bool kPair>
 __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_constant__ MxArgs a) {
@@ -430,7 +430,9 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
             }
         }
         hand_back();
-        if (a.wide) {            // transposed into shared memory, 16 rows of 256 bytes at a time, and out by bulk copies
+        // Transposed into shared memory, 16 rows of 256 bytes at a time, and out by 16 bytes a lane.  (65 536 rows of 4096 x 1792: 319 us; bulk copies of
+        // a row each 343, the copy engine's rate of them bounds the launch; 32 rows at a time 320; each warp its own 64 bytes of the rows, with no barrier, 345.)
+        if (a.wide) {
           const int bytes = min(2 * kHalfRows, 2 * (a.N - col0));
 #pragma unroll
           for (int g = 0; g < S::kGroups; ++g) {
@@ -439,12 +441,13 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
             const unsigned to = buf_at + (lane & 7) * kStorePitch + quad * 64 + (lane >> 3) * 16;
 #pragma unroll
             for (int j = 0; j < 2; ++j) st_matrix4_trans(to + 8 * j * kStorePitch, v[g][4 * j], v[g][4 * j + 1], v[g][4 * j + 2], v[g][4 * j + 3]);
-            fence_async_proxy_smem();
-            bulk_wait_read();    // the copies out of the other buffer, which the next group is written to, have read it
-            asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");
-            const int row = 4 * quad + lane;
-            if (lane < 4 && 16 * g + row < at.rows && bytes > 0) bulk_store(out + (size_t)(16 * g + row) * a.N, buf_at + row * kStorePitch, bytes);
-            bulk_commit();
+            asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");     // the other buffer, which the next group goes to, has been read too
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const int row = 4 * quad + 2 * h + (lane >> 4);
+              const uint4 x = ld_shared16(buf_at + row * kStorePitch + (lane & 15) * 16);
+              if (16 * g + row < at.rows && (lane & 15) * 16 < bytes) *reinterpret_cast<uint4*>(out + (size_t)(16 * g + row) * a.N + (lane & 15) * 8) = x;
+            }
             ++stored;
           }
         } else {
@@ -514,7 +517,6 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
         }
       }
     }
-    asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     // rows that belong to no expert: zeros, by the epilogue warps of the whole grid
     const size_t width = kSwiglu ? (size_t)a.I / 32 * 17 : (size_t)a.N;
     const int lo = s.first_row[0], hi = s.first_row[a.E], none = lo + (a.R - hi);
@@ -789,15 +791,13 @@ int product(const void* codes, const void* scales, const void* w_codes, const vo
   // us (gate/up; down; both in turn), weights that are not in L2:
   //   rows an expert            64              128             192             256             320             384             512             1024
   //   even, 32 experts, 4096 x 1792
-  //     96 rows                 50; 24; 78      69; 37; 106     82; 47; 129     100; 56; 156    128; 72; 200    142; 81; 223    189; 106; 295   346; 195; 541
-  //     192 rows                52; 26; 83      59; 30; 99      77; 50; 134     98; 58; 161     102; 59; 169    115; 73; 194    141; 86; 236    266; 168; 439
-  //     gate/up on pairs        54; 26; 86      59; 30; 100     72; 50; 130     92; 58; 157     97; 59; 166     108; 73; 187    133; 86; 227    242; 168; 418
+  //     96 rows                 50; 24; 81      73; 38; 112     87; 49; 136     106; 58; 163    132; 73; 205    150; 84; 234    197; 109; 306   356; 199; 556
+  //     192 rows                54; 25; 88      60; 31; 103     75; 50; 132     96; 57; 159     99; 59; 166     113; 71; 189    139; 86; 231    248; 159; 415
   //   uneven (Zipf 0.8), 64 experts, 2048 x 768
-  //     96 rows                 26; 18; 46      31; 25; 56      40; 34; 74      49; 41; 90      54; 49; 104     62; 55; 119     79; 69; 149     149; 132; 282
-  //     192 rows                27; 21; 52      36; 28; 73      37; 35; 82      44; 40; 94      52; 49; 110     59; 55; 125     74; 67; 150     128; 123; 261
-  //     gate/up on pairs        28; 21; 54      36; 28; 74      37; 35; 83      44; 40; 96      50; 49; 110     57; 55; 122     71; 67; 148     122; 123; 256
-  // The down product on pairs takes 10 % longer than single (65 536 rows: 359 and 326).  Tiles of 64 and 32 rows are left out: 0-7 % faster below 32 rows
-  // an expert, up to 25 % slower at 64.
+  //     96 rows                 27; 16; 44      31; 22; 53      40; 28; 68      51; 34; 85      57; 41; 98      68; 47; 115     87; 58; 145     162; 108; 269
+  //     192 rows                28; 18; 52      36; 23; 68      37; 27; 75      45; 32; 87      53; 39; 102     61; 44; 115     77; 54; 140     131; 94; 237
+  // Gate/up without pairs takes 3-10 % longer (1024 rows: 128 for 122, 266 for 242), the down product on pairs 1-14 % (161 for 159, 107 for 94).  Tiles of
+  // 64 and 32 rows are left out: 0-7 % faster below 32 rows an expert, up to 25 % slower at 64.
   const bool many = n_rows > 256ll * n_experts;
   const cudaError_t e = many ? product_launch<192, kSwiglu, kSwiglu>(a, st) : product_launch<96, kSwiglu, false>(a, st);
   return e == cudaSuccess ? MOE_OK : MOE_ECUDA;

@@ -329,6 +329,11 @@ __device__ __forceinline__ void tc_ld_frag16(unsigned taddr, unsigned (&r)[8]) {
                : "r"(taddr)
                : "memory");
 }
+__device__ __forceinline__ unsigned short ld_shared2(unsigned saddr) {
+  unsigned short v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(saddr) : "memory");
+  return v;
+}
 __device__ __forceinline__ uint4 ld_shared16(unsigned saddr) {
   uint4 v;
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(saddr) : "memory");
@@ -432,34 +437,41 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
         hand_back();
         // Transposed into shared memory, 16 rows of 256 bytes at a time, and out by 16 bytes a lane.  (65 536 rows of 4096 x 1792: 319 us; bulk copies of
         // a row each 343, the copy engine's rate of them bounds the launch; 32 rows at a time 320; each warp its own 64 bytes of the rows, with no barrier, 345.)
+        const int cols = min(kHalfRows, a.N - col0);
+        const auto stage = [&](int g) {
+          const unsigned buf_at = smem_u32(store_bufs) + (2 * half + (stored++ & 1)) * kStoreBuf;
+          const unsigned to = buf_at + (lane & 7) * kStorePitch + quad * 64 + (lane >> 3) * 16;
+#pragma unroll
+          for (int j = 0; j < 2; ++j) st_matrix4_trans(to + 8 * j * kStorePitch, v[g][4 * j], v[g][4 * j + 1], v[g][4 * j + 2], v[g][4 * j + 3]);
+          asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");     // the other buffer, which the next group goes to, has been read too
+          return buf_at;
+        };
         if (a.wide) {
-          const int bytes = min(2 * kHalfRows, 2 * (a.N - col0));
 #pragma unroll
           for (int g = 0; g < S::kGroups; ++g) {
             if (g >= groups) break;
-            const unsigned buf_at = smem_u32(store_bufs) + (2 * half + (stored & 1)) * kStoreBuf;
-            const unsigned to = buf_at + (lane & 7) * kStorePitch + quad * 64 + (lane >> 3) * 16;
-#pragma unroll
-            for (int j = 0; j < 2; ++j) st_matrix4_trans(to + 8 * j * kStorePitch, v[g][4 * j], v[g][4 * j + 1], v[g][4 * j + 2], v[g][4 * j + 3]);
-            asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");     // the other buffer, which the next group goes to, has been read too
+            const unsigned from = stage(g);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              const int row = 4 * quad + 2 * h + (lane >> 4);
-              const uint4 x = ld_shared16(buf_at + row * kStorePitch + (lane & 15) * 16);
-              if (16 * g + row < at.rows && (lane & 15) * 16 < bytes) *reinterpret_cast<uint4*>(out + (size_t)(16 * g + row) * a.N + (lane & 15) * 8) = x;
+              const int row = 4 * quad + 2 * h + (lane >> 4), c = 8 * (lane & 15);
+              const uint4 x = ld_shared16(from + row * kStorePitch + 2 * c);
+              if (16 * g + row < at.rows && c < cols) *reinterpret_cast<uint4*>(out + (size_t)(16 * g + row) * a.N + c) = x;
             }
-            ++stored;
           }
-        } else {
+        } else {                 // (kept short: what is never executed costs too where it parts what is)
 #pragma unroll
           for (int g = 0; g < S::kGroups; ++g) {
             if (g >= groups) break;
+            const unsigned from = stage(g);
+#pragma unroll 1
+            for (int row = 4 * quad; row < min(4 * quad + 4, at.rows - 16 * g); ++row) {
+              unsigned short x[4];
 #pragma unroll
-            for (int f = 0; f < 8; ++f) {
-              const int row = 16 * g + 8 * (f >> 2) + 2 * (lane & 3), c = quad * 32 + 8 * (f & 3) + (lane >> 2);
-              unsigned short* p = reinterpret_cast<unsigned short*>(out) + (size_t)row * a.N + c;
-              if (col0 + c < a.N && row < at.rows) *p = (unsigned short)v[g][f];
-              if (col0 + c < a.N && row + 1 < at.rows) p[a.N] = (unsigned short)(v[g][f] >> 16);
+              for (int i = 0; i < 4; ++i) x[i] = ld_shared2(from + row * kStorePitch + 64 * i + 2 * lane);
+              unsigned short* to = reinterpret_cast<unsigned short*>(out) + (size_t)(16 * g + row) * a.N + lane;
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (32 * i + lane < cols) to[32 * i] = x[i];
             }
           }
         }

@@ -18,8 +18,7 @@
 // down 310-325 us, 3.0-3.1 PFLOP/s and 537 MB of outputs).
 // Code size counts: after another kernel, or a long stream through L2, the first tile waits for instructions from DRAM, and within a launch five
 // roles share the instruction caches.  So the roles' loops are not unrolled and exist once, values that are alike in a warp are made known as such, and
-// the block maxima go over pairs (40-63 KB a kernel that were 110-165, the untaken forms included; gate/up and down in turn 10-20 % faster at 64-1 024
-// rows an expert, 15 % at one).  Executing the epilogue once without effects before the first tile, or one kernel for both products, then gained nothing.
+// the block maxima go over pairs (gate/up and down in turn 10-20 % faster at 64-1 024 rows an expert, 15 % at one).  Executing the epilogue once without effects before the first tile, or one kernel for both products, then gained nothing.
 // Weights that one tile alone reads leave L2 first.  With other weights in every launch that makes no difference (800 rows of 128 experts, 1.5 GB, the
 // weight stream: gate/up 162 us, down 82, 6.1 TB/s); weights of about L2's size that come again gain 5-15 %.
 // Every wait is bounded; where one runs out the launch ends and what it has not computed is NaN.
@@ -258,13 +257,12 @@ __device__ __forceinline__ Tile tile_at(const MxShared& s, int E, int t, int n_s
   return Tile{lo, s.first_row[lo] + m * kRows, min(kRows, rows - m * kRows), n * n_step, m_tiles == 1};
 }
 
-// Lane 0's value: the compiler then knows that it is the same in all lanes.  Without that it guards every shuffle, vote and matrix store that stands
-// behind a branch on it (gate/up 85 instead of 62 KB, 2-5 % of the time).
+// Lane 0's value, which the compiler then knows to be the same in all lanes (without it gate/up took 2-5 % longer).
 __device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
 __device__ __forceinline__ Tile uniform(const Tile& t) { return Tile{uniform(t.expert), uniform(t.row0), uniform(t.rows), uniform(t.n0), t.alone}; }
 
 // silu(g) u in fp32: exp(-g) = 2^(-g log2 e) to 2 + 1.2 |g| steps, the reciprocal to one.  Powers below 2^-126 and reciprocals of those above 2^126 count
-// as 0 (nothing next to the 1 that is added, silu of less than -87): the forms that keep them take three instructions more each.
+// as 0: nothing next to the 1 that is added, silu of less than -87.  (Gate/up with the forms that keep them 547 us, so 509.)
 __device__ __forceinline__ float silu_times(float g, float u) {
   float e, r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(g * -1.4426950408889634f));
@@ -292,8 +290,8 @@ __device__ __forceinline__ unsigned min_u16x2(unsigned a, unsigned b) {
   return r;
 }
 // Exponent fields (bits 7 to 14) of the largest of the 32 lanes' v[r], in the low half, and of their v[r + 8], in the high half, for r = lane % 8.  The
-// upper halves of floats as pairs of 16 bits; three steps halve the pairs that a lane follows, two more join the lanes of equal r (50 instructions
-// where sixteen reductions over the warp compile to about 240).
+// upper halves of floats as pairs of 16 bits; three steps halve the pairs that a lane follows, two more join the lanes of equal r.  (With
+// sixteen reductions over the warp, and more rows handed on as they are, both products in turn took 851 us for 65 536 rows, 830 so.)
 __device__ __forceinline__ unsigned block_exponents(const float (&v)[16], int lane) {
   unsigned p[8];
 #pragma unroll

@@ -237,8 +237,8 @@ __device__ __forceinline__ void st_cluster_v4(unsigned cluster_addr, uint4 v) {
   asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(cluster_addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 
-// one lane of a converged warp.  The compiler knows a branch on elect.sync for a region of one thread: instructions that take uniform
-// registers (TMA, MMA, commit) are then issued as they stand
+// one lane of a converged warp.  A branch on it is a region of one thread: TMA, MMA and commit are issued in half the time that they take under
+// a predicate in a loop of the whole warp (moe_run_pair.cu, MMA issuer)
 __device__ __forceinline__ bool elect_one() {
   unsigned e;
   asm volatile("{\n\t.reg .pred p;\n\t.reg .b32 r;\n\telect.sync r|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));

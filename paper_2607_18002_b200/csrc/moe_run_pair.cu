@@ -523,8 +523,7 @@ moe_apk_pair_kernel(const __grid_constant__ RunArgs args, RunHead* rh) {
     __syncwarp();
   } else if (warp == 1 && leader) {
     // ============================================================ MMA issuer (leader)
-    // One thread runs the whole role.  Inside a branch on elect.sync the compiler knows that a single thread is there and feeds the
-    // instructions from uniform registers as they are.  With the whole warp in the loop and an election around each group, the same four MMAs
+    // One thread runs the whole role, inside a branch on elect.sync.  With the whole warp in the loop and an election around each group, the same four MMAs
     // and commit took 300 clocks to issue (350 with the fence of a gathered tile), whatever the tile's rows, now 240 (260); a probe without
     // loads issues them in 155, and in 315 that way.  A k-block of up to 64 gathered rows went from 445 to 390 clocks (4096 tokens on 16
     // experts), 16 384 + 256 paired from 4330 to 4300 us: the 1000 W cap takes most of it back as clock.  One token: 56.0 -> 54.9 us a pass.

@@ -83,7 +83,8 @@ struct MxArgs {
   int wide;                      // rows of out are 16-byte aligned
 };
 
-// false: gave up, or somebody of this block has.  kTry: mbar_try, or mbar_try_cluster where the other CTA of a pair hands something over
+// false: gave up, or somebody of this block has.  kTry: mbar_try; where threads of the other CTA of a pair hand over what they wrote or read,
+// mbar_try_cluster (an accumulator), or mbar_try_relaxed and a fence (the scales of a stage)
 template <bool (*kTry)(void*, unsigned) = mbar_try>
 __device__ __forceinline__ bool wait(unsigned long long* bar, unsigned parity, volatile int* dead) {
   if (kTry(bar, parity)) return true;
@@ -592,8 +593,9 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
 #pragma unroll 1
           for (int i = 0; i < n_stages; ++i, ++n) {
             const unsigned slot = n % S::kStages, round = n / S::kStages;
-            ok = wait(&s.full[slot], round & 1, &s.dead) && wait(&s.landed[slot], round & 1, &s.dead);
+            ok = wait(&s.full[slot], round & 1, &s.dead) && wait<kPair ? mbar_try_relaxed : mbar_try>(&s.landed[slot], round & 1, &s.dead);
             if (!ok) break;
+            if (kPair) fence_acquire_pair_smem();
             tc_fence_after();
             const unsigned st = smem_u32(stages + slot * S::kStageBytes);
             const unsigned sc = st + S::kWBytes + S::kXBytes, tsc = tmem + S::kScaleCol0 + slot * S::kScaleCols;
@@ -689,8 +691,12 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
         }
         __syncwarp();
         if (lane == 0) {
-          if (kPair) mbar_arrive_remote(map_to_cta(&s.landed[slot], 0));
-          else mbar_arrive(&s.landed[slot]);
+          if (kPair) {           // the leader's MMAs read this CTA's scales too: fences of shared memory alone (65 536 rows 434 us; an arrival and a wait that order all memory 707)
+            fence_release_own_smem();
+            mbar_arrive_relaxed(map_to_cta(&s.landed[slot], 0));
+          } else {
+            mbar_arrive(&s.landed[slot]);
+          }
         }
         ++n;
       }

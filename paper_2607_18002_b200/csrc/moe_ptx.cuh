@@ -233,6 +233,14 @@ __device__ __forceinline__ bool mbar_try_relaxed(void* bar, unsigned parity) {
       : "memory");
   return ok != 0;
 }
+// The fences of a relaxed arrival and of the wait for it where shared memory alone is handed over: in front of the arrival, for what threads of this CTA
+// did in its own shared memory; behind the wait, for what this thread does in that of either CTA
+__device__ __forceinline__ void fence_release_own_smem() {
+  asm volatile("fence.release.sync_restrict::shared::cta.cluster;" ::: "memory");
+}
+__device__ __forceinline__ void fence_acquire_pair_smem() {
+  asm volatile("fence.acquire.sync_restrict::shared::cluster.cluster;" ::: "memory");
+}
 __device__ __forceinline__ void st_cluster_v4(unsigned cluster_addr, uint4 v) {
   asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(cluster_addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }

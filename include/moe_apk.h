@@ -337,7 +337,8 @@ int moe_mx_dequantize(const void* codes, const void* scales, int64_t n_rows, int
  * The experts of a layer: moe_mx_quantize (sorting) -> moe_mx_swiglu -> moe_mx_product -> moe_merge_rows.
  * Rows that belong to no expert (before offsets[0], from offsets[E] on) are 0.  (Offsets are held inside [0, R] and never lower than
  * those before, whatever is there.)  k_cols a multiple of 128, inter one of 32, n_cols >= 1, all at most 2^30 (inter 2^29), R < 2^27, E <= 1024; codes and w_codes 16-byte aligned, scales and w_scales 4-byte aligned, else MOE_EINVAL.  No context, no
- * workspace.  Waits inside the kernel are bounded (2 s); what a launch that gave up has not computed is NaN. */
+ * workspace.  Each wait inside the kernel is bounded (2 s).  A launch that gave up ends some seconds later; the call has returned MOE_OK, there is no status to
+ * read, and NaN (scale byte 255) in what it has not computed is the only sign. */
 int moe_mx_product(const void* codes, const void* scales, const void* w_codes, const void* w_scales, const int32_t* offsets,
                    int32_t n_rows, int32_t n_experts, int32_t n_cols, int32_t k_cols, void* out, void* stream);
 int moe_mx_swiglu(const void* codes, const void* scales, const void* w_codes, const void* w_scales, const int32_t* offsets,

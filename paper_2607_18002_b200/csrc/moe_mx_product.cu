@@ -21,7 +21,7 @@
 // the block maxima go over pairs (gate/up and down in turn 10-20 % faster at 64-1 024 rows an expert, 15 % at one).  Executing the epilogue once without effects before the first tile, or one kernel for both products, then gained nothing.
 // Weights that one tile alone reads leave L2 first.  With other weights in every launch that makes no difference (800 rows of 128 experts, 1.5 GB, the
 // weight stream: gate/up 162 us, down 82, 6.1 TB/s); weights of about L2's size that come again gain 5-15 %.
-// Every wait is bounded; where one runs out the launch ends and what it has not computed is NaN.
+// Every wait is bounded (2 s); where one runs out the launch ends, after another such limit for its copies in flight, and what it has not computed is NaN.
 #include "moe_dev.cuh"
 #include "moe_mx.cuh"
 #include "moe_ptx.cuh"
@@ -565,11 +565,13 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
             for (int b = 0; b < boxes; ++b) tma_2d<kPair>(to + S::kWBytes + b * kBoxRows * 128, &a.tm_x, i * 128, row0 + b * kBoxRows, bar);
           }
         }
-        // copies that nobody has waited for (after a wait that ran out): the block's shared memory is theirs until they have landed
-        for (unsigned m = n > S::kStages ? n - S::kStages : 0; s.dead && m < n; ++m) {
-          const unsigned long long start = gtime_ns();
-          while (!(rank ? mbar_try(&s.empty[m % S::kStages], (m / S::kStages) & 1) : mbar_try(&s.full[m % S::kStages], (m / S::kStages) & 1)) &&
-                 gtime_ns() - start < kWaitNs) {}
+        // The block's shared memory belongs to its copies until they have landed, and where another role has given up nobody else waits for the last ones.
+        // The second CTA of a pair, whose copies count on the leader's barriers, sees its own by the stages that the MMAs are done with (or runs into the limit).
+        const unsigned long long start = gtime_ns();
+#pragma unroll 1
+        for (unsigned m = n > S::kStages ? n - S::kStages : 0; m < n; ++m) {
+          unsigned long long* bar = rank ? &s.empty[m % S::kStages] : &s.full[m % S::kStages];
+          while (!mbar_try(bar, (m / S::kStages) & 1) && gtime_ns() - start < kWaitNs) {}
         }
       }
       __syncwarp();

@@ -25,3 +25,15 @@ def test_what_one_cta_hands_to_the_other_is_ordered_for_the_cluster():
         assert len(waits) == 1, (bar, waits)
         kind, behind = waits[0]
         assert kind == "<kPair ? %s : mbar_try>" % ("mbar_try_relaxed" if fenced else "mbar_try_cluster") and bool(behind) == fenced, (bar, waits)
+
+
+def test_copies_in_flight_are_waited_for_whatever_ended_the_launch():
+    """Shared memory is not given back under a copy: the thread that issued the copies looks at all that may be outstanding when it is done, also where another
+    role gave up after it, and within one limit for all of them."""
+    code = re.sub(r"\s+", " ", _code())
+    at = code.index("tma_2d<kPair>(to + S::kWBytes")
+    tail = code[at:code.index("__syncwarp()", at)]
+    limit, loop = tail.index("start = gtime_ns()"), tail.index("for (unsigned m")
+    head = tail[loop:tail.index(")", tail.index("++m"))]
+    assert "dead" not in head and "n > S::kStages ? n - S::kStages : 0" in head and "m < n" in head
+    assert limit < loop and tail.count("gtime_ns()") == 2 and "gtime_ns() - start < kWaitNs" in tail[loop:]

@@ -280,7 +280,7 @@ int moe_route(const float* logits, int32_t n_tokens, int32_t n_experts, int32_t 
 /* The router's gradient: from d_topk_w [T, k], the gradient of the router weights of moe_route, to that of the logits,
  *     d_logits[t, e] = sum_{j: topk_ids[t,j] = e} w_j (dw_j - sum_i w_i dw_i),   0 for an expert that was not chosen
  * (the weights are a softmax over the chosen logits).  Every entry of d_logits [T, E] fp32 is written.  A slot whose id is
- * outside [0, n_experts) is left out of both sums.  Limits as for moe_route. */
+ * outside [0, n_experts) is left out of both sums.  Limits as for moe_route; 4-byte aligned addresses, else MOE_EINVAL. */
 int moe_route_grad(const int32_t* topk_ids, const float* topk_w, const float* d_topk_w, int32_t n_tokens,
                    int32_t n_experts, int32_t top_k, float* d_logits, void* stream);
 

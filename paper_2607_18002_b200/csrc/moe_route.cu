@@ -128,6 +128,9 @@ extern "C" int moe_route_grad(const int32_t* topk_ids, const float* topk_w, cons
     return MOE_EINVAL;
   if (n_tokens == 0) return MOE_OK;
   if (!topk_ids || !topk_w || !d_topk_w || !d_logits) return MOE_EINVAL;
+  if ((reinterpret_cast<uintptr_t>(topk_ids) | reinterpret_cast<uintptr_t>(topk_w) | reinterpret_cast<uintptr_t>(d_topk_w) |
+       reinterpret_cast<uintptr_t>(d_logits)) & 3)
+    return MOE_EINVAL;
   const int blocks = (n_tokens + kRouteWarps - 1) / kRouteWarps;
   const bool vec = n_experts % 4 == 0 && (reinterpret_cast<uintptr_t>(d_logits) & 15) == 0;
   return launch_after(route_grad_kernel, blocks, kRouteWarps * 32, 0, static_cast<cudaStream_t>(stream), topk_ids, topk_w, d_topk_w, n_tokens,

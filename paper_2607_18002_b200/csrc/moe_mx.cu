@@ -198,10 +198,10 @@ int moe_mx_quantize(const void* x, int64_t x_stride, int32_t dtype, int32_t n_to
                     const int32_t* sorted_to_flat, const int32_t* flat_to_sorted, void* codes, void* scales, void* stream) {
   using namespace moe;
   if (n_tokens < 0 || top_k < 1 || top_k > 32 || cols < kMxBlock || cols > 1 << 30 || cols % kMxBlock || !value_type(dtype)) return MOE_EINVAL;
+  if (n_tokens == 0) return MOE_OK;           // (a permutation of no rows may have no address)
   if (!sorted_to_flat != !flat_to_sorted || (!flat_to_sorted && top_k != 1)) return MOE_EINVAL;
   if (flat_to_sorted && (long long)n_tokens * top_k >= (1ll << kRowSlotShift)) return MOE_EINVAL;
   if ((long long)n_tokens * (cols / kMxBlock) >= (1ll << 32)) return MOE_EINVAL;
-  if (n_tokens == 0) return MOE_OK;
   if (!x || !codes || !scales || x_stride < cols) return MOE_EINVAL;
   if (misaligned(x, dtype == MOE_DTYPE_FP32 ? 4 : 2) || misaligned(codes, 16) || misaligned(sorted_to_flat, 4) || misaligned(flat_to_sorted, 4))
     return MOE_EINVAL;

@@ -21,3 +21,20 @@ def test_the_routers_gradient_refuses_addresses_between_elements(lib, at, off):
     args = [P, P, P, 4, 8, 2, P, None]
     args[at] += off
     assert lib.moe_route_grad(*args) == moe.MOE_EINVAL
+
+
+@pytest.mark.parametrize("s2f,f2s", [(None, None), (P, None), (None, P), (P, P)])
+def test_a_batch_without_tokens_needs_no_permutation(lib, s2f, f2s):
+    """Arrays of no entries have no address: quantise-and-sort of no tokens is nothing to do whatever k is."""
+    for dtype in (moe.MOE_DTYPE_BF16, moe.MOE_DTYPE_FP16, moe.MOE_DTYPE_FP32):
+        assert lib.moe_mx_quantize(None, 64, dtype, 0, 8, 64, s2f, f2s, None, None, None) == moe.MOE_OK
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("k", [1, 8])
+def test_quantise_and_sort_of_a_batch_without_tokens(k):
+    x, e = torch.empty(0, 128, dtype=torch.bfloat16, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda")
+    one = torch.zeros(1, dtype=torch.int32, device="cuda")           # (a plan without rows has arrays of one entry)
+    for s2f, f2s in ((e, e), (one, one), (e, one)):
+        codes, scales = moe.mx_quantize(x, s2f, f2s, k)
+        assert codes.shape == (0, 64) and scales.shape == (0, 4)

@@ -38,3 +38,21 @@ def test_quantise_and_sort_of_a_batch_without_tokens(k):
     for s2f, f2s in ((e, e), (one, one), (e, one)):
         codes, scales = moe.mx_quantize(x, s2f, f2s, k)
         assert codes.shape == (0, 64) and scales.shape == (0, 4)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(0, 128, 256), (4, 0, 64), (0, 0, 32), (2, 3, 0, 96), (1, 2, 3, 64)])
+def test_quantise_of_more_dimensions_without_elements(shape):
+    """A rank without experts, experts without rows."""
+    x = torch.ones(shape, dtype=torch.bfloat16, device="cuda")
+    codes, scales = moe.mx_quantize(x)
+    assert codes.shape == (*shape[:-1], shape[-1] // 2) and scales.shape == (*shape[:-1], shape[-1] // 32)
+    values = moe.mx_dequantize(codes, scales)
+    assert values.shape == shape and torch.equal(values, x)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(2, 3, 0), (0, 2, 0), (2, 3, 48)])
+def test_quantise_of_more_dimensions_refuses_widths(shape):
+    with pytest.raises(ValueError):
+        moe.mx_quantize(torch.ones(shape, dtype=torch.bfloat16, device="cuda"))

@@ -170,10 +170,11 @@ def route_grad(topk_ids, topk_w, d_topk_w, n_experts: int, stream=None):
 
 
 def mx_quantize(x, sorted_to_flat=None, flat_to_sorted=None, top_k: int = 1, stream=None):
-    """x [..., K] -> codes uint8 [..., K/2], scales uint8 [..., K/32]; with a permutation x [T, K] -> the T*k rows by expert."""
-    if isinstance(x, _Tensor) and x.dim() > 2 and x.is_contiguous() and sorted_to_flat is None and flat_to_sorted is None:
-        codes, scales = mx_quantize(x.flatten(0, -2), None, None, top_k, stream)
-        return codes.view(*x.shape[:-1], codes.shape[1]), scales.view(*x.shape[:-1], scales.shape[1])
+    """x [..., K] -> codes uint8 [..., K/2], scales uint8 [..., K/32]; with a permutation x [T, K] -> the T*k rows by expert.  Contiguous, or [T, K] of any row stride."""
+    if isinstance(x, _Tensor) and x.dim() not in (0, 2) and x.is_contiguous() and sorted_to_flat is None and flat_to_sorted is None:
+        *lead, K = x.shape
+        codes, scales = mx_quantize(x.view(x.numel() // K if K else 0, K), None, None, top_k, stream)
+        return codes.view(*lead, codes.shape[1]), scales.view(*lead, scales.shape[1])
     T, K, step = _rows(x, "x", _DTYPES)
     gpu = x.get_device()
     if stream is not None or gpu != _current_device():

@@ -56,3 +56,17 @@ def test_quantise_of_more_dimensions_without_elements(shape):
 def test_quantise_of_more_dimensions_refuses_widths(shape):
     with pytest.raises(ValueError):
         moe.mx_quantize(torch.ones(shape, dtype=torch.bfloat16, device="cuda"))
+
+
+@pytest.mark.gpu
+def test_quantise_of_one_dimension_is_a_row():
+    x = torch.randn(96, device="cuda")
+    codes, scales = moe.mx_quantize(x)
+    c2, s2 = moe.mx_quantize(x[None])
+    assert codes.shape == (48,) and scales.shape == (3,) and torch.equal(codes, c2[0]) and torch.equal(scales, s2[0])
+    assert torch.equal(moe.mx_dequantize(codes, scales, torch.float32), moe.mx_dequantize(c2, s2, torch.float32)[0])
+    for bad in (x[::3], x[:48], torch.zeros((), device="cuda"), torch.zeros(0, device="cuda")):
+        with pytest.raises(ValueError):
+            moe.mx_quantize(bad)
+    with pytest.raises(ValueError):
+        moe.mx_quantize(x, *[torch.zeros(1, dtype=torch.int32, device="cuda")] * 2)

@@ -286,7 +286,7 @@ int moe_route_grad(const int32_t* topk_ids, const float* topk_w, const float* d_
 
 /* Rows sorted by expert and put together again, for experts that the caller computes (in training, or with other weights than
  * moe_run knows), and the gradients of both.  R = n_tokens * top_k; sorted_to_flat and flat_to_sorted [R] are the permutation
- * that moe_plan or moe_plan_static wrote (inverses of one another), topk_w [T, k] the router weights:
+ * that moe_plan or moe_plan_static wrote, or any other stable sort of the ids (inverses of one another), topk_w [T, k] the router weights:
  *   moe_sort_rows        xs[flat_to_sorted[t*k+j], :] = x[t, :]
  *   moe_sort_rows_grad   dx[t, :] = sum_j dxs[flat_to_sorted[t*k+j], :]
  *   moe_merge_rows       y[t, :] = sum_j topk_w[t,j] rows[flat_to_sorted[t*k+j], :]

@@ -14,8 +14,10 @@
 // TMA (a stage is 256 columns of K: 128-byte rows, swizzled), four warps bring the stage's scale bytes through registers into the 512-byte
 // form that tcgen05.cp copies to TMEM (128 rows x 4 blocks), one thread copies them and issues the MMAs, eight warps are the epilogue: for the plain
 // product through stmatrix and shared memory, for swiglu a warp's 32 lanes have one 32-column block of the result.
-// What bounds them: few rows, the weight stream; many, energy (65 536 rows of 64 experts, K 4096, inter 1792: gate/up 465-490 us, 3.9-4.1 PFLOP/s at 1 000 W;
-// down 310-325 us, 3.0-3.1 PFLOP/s and 537 MB of outputs).
+// What bounds them: few rows, the weight stream; many, energy and the accumulators' way out between two tiles' MMAs (65 536 rows of 64 experts, K 4096, inter
+// 1792, boxes differ: gate/up 430-490 us, 3.9-4.4 PFLOP/s at 1 000 W; down 275-320 us, 3.0-3.5 PFLOP/s and 537 MB of outputs).
+// Outputs are rounded to bf16, like the expert outputs of moe_run: half of the bytes that the down product writes and the merge reads.  A layer is then
+// off by 2.4e-3 (2-norm, against 64 bits) where fp32 rows would give 1.7e-3, the rounding of the layer's own outputs.
 // Code size counts: after another kernel, or a long stream through L2, the first tile waits for instructions from DRAM, and within a launch five
 // roles share the instruction caches.  So the roles' loops are not unrolled and exist once, values that are alike in a warp are made known as such, and
 // the block maxima go over pairs (gate/up and down in turn 10-20 % faster at 64-1 024 rows an expert, 15 % at one).  Executing the epilogue once without effects before the first tile, or one kernel for both products, then gained nothing.
@@ -804,7 +806,8 @@ int product(const void* codes, const void* scales, const void* w_codes, const vo
   a.R = n_rows; a.E = n_experts; a.N = n; a.K = K; a.I = n / 2;
   a.wide = n % 8 == 0 && (reinterpret_cast<uintptr_t>(out) & 15) == 0;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  // The tile's height goes by the rows that an expert gets on average (the host does not know more).  Two buffers of 96 columns let the epilogue of a tile
+  // The tile's height goes by the rows that an expert gets on average (the host does not know more); the line lies where high tiles stop losing on uneven
+  // loads, which costs even ones 9, 3 and 3 % of both products in turn at 128, 192 and 256 rows an expert.  Two buffers of 96 columns let the epilogue of a tile
   // run beside the next one's MMAs; 192 columns take the weights from L2 half as often, and for gate/up a pair of CTAs takes half of the rows each.
   // us (gate/up; down; both in turn), weights that are not in L2:
   //   rows an expert            64              128             192             256             320             384             512             1024

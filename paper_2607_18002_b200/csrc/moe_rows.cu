@@ -13,7 +13,7 @@
 //
 // Device time, bf16, and the rate of the bytes that have to move (a plain copy runs at 6.5 TB/s): 8 192 tokens x 8 slots x 4 096 columns sort 98 us
 // (6.2 TB/s), its gradient 89 us (6.8); 4 096 x 8 x 6 144 merge 68 us (6.6), its gradient 134 us (6.4); 16 384 x 2 x 4 096 63 and 102 us; one token
-// 2.2-2.5 us, launch included.  8 192 x 8 rows of odd width (3 001) move at 2.6-4.4 TB/s: accesses of two bytes.
+// 2.2-2.5 us, launch included (gradient of merge 5.1).  8 192 x 8 rows of odd width (3 001) move at 2.6-4.4 TB/s: accesses of two bytes.
 #include <cuda_fp16.h>
 
 #include "moe_dev.cuh"

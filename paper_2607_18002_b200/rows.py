@@ -3,8 +3,14 @@ experts in 4 bits (moe_sort_rows ... moe_mx_swiglu of include/moe_apk.h).
 
 Checks of arguments and marshalling only; a call enqueues one kernel on `stream` (the current stream of the tensors' device if
 None) and allocates its outputs there.  Nothing is recorded for autograd: gradients are calls of their own.  Wrong types, shapes, strides
-or devices raise ValueError, what the library refuses MoeError.
-A permutation is the pair (sorted_to_flat, flat_to_sorted) of a plan, int32 [T*k] each.
+or devices raise ValueError, what the library refuses MoeError.  Inputs may require gradients (experts' outputs of a graph of the caller's own do); results never do.
+As with any work on another stream, inputs have to live until `stream` has read them, and `stream` has to be waited for before results are used elsewhere.
+A permutation is the pair (sorted_to_flat, flat_to_sorted) of a plan, int32 [T*k] each, the inverses of one another: of moe_plan (a Context's), of moe_plan_static
+(up to 32 768 rows and 256 experts, no context) or, for any size and without either, by a stable sort of the expert ids:
+
+    order = torch.argsort(topk_ids.flatten(), stable=True)
+    s2f, f2s = order.int(), torch.argsort(order).int()
+    offsets = torch.nn.functional.pad(torch.bincount(topk_ids.flatten(), minlength=n_experts).cumsum(0), (1, 0)).int()
 
     codes, scales = mx_quantize(x, s2f, f2s, k)                          # experts of a layer in 4 bits
     codes, scales = mx_swiglu(codes, scales, w1_codes, w1_scales, offsets)

@@ -70,3 +70,17 @@ def test_quantise_of_one_dimension_is_a_row():
             moe.mx_quantize(bad)
     with pytest.raises(ValueError):
         moe.mx_quantize(x, *[torch.zeros(1, dtype=torch.int32, device="cuda")] * 2)
+
+
+@pytest.mark.parametrize("T,E,k", [(1, 8, 2), (300, 40, 5), (8192, 300, 8), (2, 1024, 1)])
+def test_the_permutation_of_the_documentation_is_a_plans(T, E, k):
+    """The three lines of rows.py for permutations of any size, run as they stand there."""
+    from paper_2607_18002_b200 import rows
+    from rows_util import routing
+    ids, w, offsets, s2f, f2s = routing(T, E, k, 17)
+    lines = [line.strip() for line in rows.__doc__.splitlines()]
+    at = lines.index("order = torch.argsort(topk_ids.flatten(), stable=True)")
+    names = dict(torch=torch, topk_ids=torch.from_numpy(ids), n_experts=E)
+    exec("\n".join(lines[at:at + 3]), names)
+    for name, want in (("s2f", s2f), ("f2s", f2s), ("offsets", offsets)):
+        assert names[name].dtype == torch.int32 and names[name].is_contiguous() and torch.equal(names[name], torch.from_numpy(want)), name

@@ -1,6 +1,6 @@
 """The 4-bit products beyond one turn of their rings and one tile a block, in both heights of tiles.
 
-A stage holds 256 columns and a block has at most seven of them, so rings turn over from 2 048 columns on.  Low tiles (96 rows) are walked by 148 blocks, high
+A stage holds 256 columns and a block has three or four of them, so rings turn over beyond 1 024 columns.  Low tiles (96 rows) are walked by 148 blocks, high
 ones (192 rows, more than 256 rows an expert) by 148 blocks or, for gate/up, by 74 pairs: every launch here has more than two tiles for each of them where it
 says so.  Operands are small multiples of common powers of two, so fp32 sums are exact in any order (up to 4 096 terms of at most 2^11.2 steps)."""
 import numpy as np

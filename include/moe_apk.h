@@ -332,8 +332,8 @@ int moe_mx_dequantize(const void* codes, const void* scales, int64_t n_rows, int
 /* Sorted 4-bit rows times the experts' 4-bit matrices: rows [R, K], weights [E, n, K] (K contiguous), offsets [E+1] as moe_plan
  * wrote them (rows offsets[e] .. offsets[e+1]-1 are expert e's; offsets must not decrease).  One dense matrix is E = 1.
  *   moe_mx_product  out[p, :] = rows[p, :] . w[e]^T, bf16 [R, n_cols], fp32 accumulation, one rounding
- *   moe_mx_swiglu   weights [E, 2*inter, K], gate rows first: silu(gate) * up, computed in fp32 and quantised as by
- *                   moe_mx_quantize: codes [R, inter/2], scales [R, inter/32], the rows of the down product
+ *   moe_mx_swiglu   weights [E, 2*inter, K], gate rows first: silu(gate) * up, computed in fp32 (0 for gates below
+ *                   -87.3, where silu is smaller than 2^-119) and quantised as by moe_mx_quantize: codes [R, inter/2], scales [R, inter/32], the rows of the down product
  * The experts of a layer: moe_mx_quantize (sorting) -> moe_mx_swiglu -> moe_mx_product -> moe_merge_rows.
  * Rows that belong to no expert (before offsets[0], from offsets[E] on) are 0.  (Offsets are held inside [0, R] and never lower than
  * those before, whatever is there.)  k_cols a multiple of 128, inter one of 32, n_cols >= 1, all at most 2^30 (inter 2^29), R < 2^27, E <= 1024; codes and w_codes 16-byte aligned, scales and w_scales 4-byte aligned, else MOE_EINVAL.  No context, no

@@ -53,9 +53,10 @@ enum {
   MOE_ENOTPLANNED = -7 /* moe_run / moe_combine on a slot with no moe_plan               */
 };
 
-/* fp16 and fp32: of rows that are sorted, merged or quantised; a context computes in the first two */
+/* fp16 and fp32: of logits and of rows that are sorted, merged, quantised or results; a context computes in the first two */
 enum { MOE_DTYPE_BF16 = 0, MOE_DTYPE_FP8_E4M3 = 1, MOE_DTYPE_FP16 = 2, MOE_DTYPE_FP32 = 3 };
 enum { MOE_CLASS_DECODE = 0, MOE_CLASS_PREFILL = 1 };
+enum { MOE_SCORES_SOFTMAX = 0, MOE_SCORES_SIGMOID = 1 };
 /* How an op's activations are laid out (Section 2.4).  GATHERED: x is [T, H] in token order and the
  * plan packs the routed rows per expert (the contiguous layout).  MASKED: x already sits in per-expert
  * slabs [E, slab_rows, H] of which the first counts[e] rows of slab e are valid (what a dispatch step
@@ -284,6 +285,26 @@ int moe_route(const float* logits, int32_t n_tokens, int32_t n_experts, int32_t 
 int moe_route_grad(const int32_t* topk_ids, const float* topk_w, const float* d_topk_w, int32_t n_tokens,
                    int32_t n_experts, int32_t top_k, float* d_logits, void* stream);
 
+/* Routers with other scores than moe_route's.  logits [T, E] (BF16, FP16 or FP32; logits_stride elements from a token to the next), bias [E] fp32 or NULL:
+ *   scores   s = softmax of the row (MOE_SCORES_SOFTMAX) or 1 / (1 + exp(-logit)) (MOE_SCORES_SIGMOID);   c = s + bias
+ *   groups   the experts stand in n_groups groups of neighbours; the top_groups groups are kept whose value, the sum of the group_sum (1 or 2) largest c
+ *            of their experts, is largest (an expert alone in its group: its c)
+ *   choice   the k largest c of the kept groups' experts, in order of decreasing c (without a bias: of the logit) -> topk_ids [T, k]
+ *   weights  topk_w[t,j] = scale * s of that expert, renormalize != 0: divided by the sum of the k chosen s (the bias is not in them), fp32
+ * Ties go to the lower index.  The choice is that of an evaluation in 64 bits, the weights are fp32.  A logit of -infinity is an expert that is masked: its
+ * score is 0, it is chosen when fewer than k others are left, with weight 0; in a row of nothing else all weights are 0.  NaN ranks above every number; a
+ * score that is NaN (softmax: all of a row that holds NaN or +infinity) makes the weights that it is in NaN, ids are in range all the same.  A bias of -infinity keeps an expert out in the same way; others must be finite.
+ * n_experts <= 1024, top_k <= 32, n_groups <= 32 and a divisor of n_experts, top_k <= top_groups * n_experts / n_groups, else MOE_EINVAL.
+ *
+ * moe_choose_experts_grad: from d_topk_w [T, k], the gradient of those weights, to that of the logits, every entry of d_logits [T, E], of the logits' type (the bias and
+ * the choice have none).  topk_ids may be any: a slot whose id is outside [0, n_experts) is left out, an expert named twice gets both. */
+int moe_choose_experts(const void* logits, int64_t logits_stride, int32_t dtype, const float* bias, int32_t n_tokens,
+                       int32_t n_experts, int32_t top_k, int32_t n_groups, int32_t top_groups, int32_t group_sum,
+                       int32_t scores, int32_t renormalize, float scale, int32_t* topk_ids, float* topk_w, void* stream);
+int moe_choose_experts_grad(const void* logits, int64_t logits_stride, int32_t dtype, const int32_t* topk_ids,
+                            const float* d_topk_w, int32_t n_tokens, int32_t n_experts, int32_t top_k, int32_t scores,
+                            int32_t renormalize, float scale, void* d_logits, void* stream);
+
 /* Rows sorted by expert and put together again, for experts that the caller computes (in training, or with other weights than
  * moe_run knows), and the gradients of both.  R = n_tokens * top_k; sorted_to_flat and flat_to_sorted [R] are the permutation
  * that moe_plan or moe_plan_static wrote, or any other stable sort of the ids (inverses of one another), topk_w [T, k] the router weights:
@@ -344,6 +365,42 @@ int moe_mx_product(const void* codes, const void* scales, const void* w_codes, c
 int moe_mx_swiglu(const void* codes, const void* scales, const void* w_codes, const void* w_scales, const int32_t* offsets,
                   int32_t n_rows, int32_t n_experts, int32_t inter, int32_t k_cols, void* out_codes, void* out_scales,
                   void* stream);
+
+/* Rows in e4m3 with a scale per 128 columns, weights in e4m3 with a scale per 128 x 128: the form of a context's e4m3 operands, for experts of the caller's own.
+ * A value is code * scale.  [rows, cols] rows have codes [rows, cols] and fp32 scales [rows, ceil(cols/128)]; matrices [E, n, cols] have scales
+ * [E, ceil(n/128), ceil(cols/128)]; blocks at the edges are smaller.  The scale of a block is amax / 448 (one fp32 division), 1 for a block of
+ * zeros, 2^-126 at least; a code is the e4m3 value nearest to the exact quotient, ties to the even code.  A block that holds NaN or infinity
+ * has a NaN scale: all of it is NaN (its codes say nothing).  cols: a multiple of 16, at most 2^30;
+ * weights and dequantised values: 2^40 at most.
+ *
+ * moe_scaled_quantize: x [T, cols] (BF16, FP16 or FP32) -> codes and scales, sorted by expert as by moe_mx_quantize where a permutation is given (zero
+ * codes and scales of 1 where a row belongs to no token), row by row with both NULL (top_k = 1).  codes 16-byte aligned.
+ * moe_scaled_quantize_weights: w [E, n, cols], contiguous.  codes and w 16-byte aligned.
+ * moe_scaled_dequantize: the values [E, n, cols] that codes and scales stand for, rounded to dtype; scale_rows 1 (scales [E, n, .]; E * n rows) or 128.
+ * codes and values 16-byte aligned. */
+int moe_scaled_quantize(const void* x, int64_t x_stride, int32_t dtype, int32_t n_tokens, int32_t top_k, int32_t cols,
+                        const int32_t* sorted_to_flat, const int32_t* flat_to_sorted, void* codes, float* scales, void* stream);
+int moe_scaled_quantize_weights(const void* w, int32_t dtype, int32_t n_experts, int32_t n_rows, int32_t cols, void* codes,
+                                float* scales, void* stream);
+int moe_scaled_dequantize(const void* codes, const float* scales, int32_t n_experts, int32_t n_rows, int32_t cols,
+                          int32_t scale_rows, int32_t dtype, void* values, void* stream);
+
+/* Sorted e4m3 rows times the experts' e4m3 matrices: rows [R, K], weights [E, n, K], offsets [E+1] as for moe_mx_product; offsets NULL: one
+ * matrix (n_experts = 1) for all rows.
+ *   moe_scaled_product  out[p, :] = rows[p, :] . w[e]^T, rounded once to dtype (BF16, FP16 or FP32)
+ *   moe_scaled_swiglu   weights [E, 2*inter, K], gate rows first: silu(gate) * up, computed in fp32 and quantised as by moe_scaled_quantize (codes: of a
+ *                       quotient that is off by some steps of fp32; 0 for gates below -87.3): codes [R, inter], scales [R, inter/128], the rows of the down product
+ * The products of a block of 128 columns are added up in the tensor core, the blocks with their scales in fp32.  Rows that belong to no expert are 0
+ * (swiglu: codes 0, scales 1).  The gradient of a product to its rows is a product with the transposed codes and scales.
+ * k_cols a multiple of 16, inter of 128, n_cols >= 1, all at most 2^30 (inter 2^29), R < 2^27, E <= 1024; codes, w_codes and out_codes 16-byte, the others
+ * 4-byte aligned (out: to its elements), else MOE_EINVAL.  No context, no workspace.  Each wait inside the kernel is bounded (2 s); what a launch that gave
+ * up has not computed is NaN (a scale of NaN), which is the only sign. */
+int moe_scaled_product(const void* codes, const float* scales, const void* w_codes, const float* w_scales,
+                       const int32_t* offsets, int32_t n_rows, int32_t n_experts, int32_t n_cols, int32_t k_cols,
+                       int32_t dtype, void* out, void* stream);
+int moe_scaled_swiglu(const void* codes, const float* scales, const void* w_codes, const float* w_scales,
+                      const int32_t* offsets, int32_t n_rows, int32_t n_experts, int32_t inter, int32_t k_cols,
+                      void* out_codes, float* out_scales, void* stream);
 
 /* Multiprocessor count of the context's device (the default persistent grid). */
 int moe_sm_count(moe_ctx_t* ctx);

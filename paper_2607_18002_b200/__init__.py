@@ -24,6 +24,7 @@ MOE_OK, MOE_EINVAL, MOE_ENOSPC, MOE_ECUDA = 0, -1, -2, -3
 MOE_ETIMEOUT, MOE_EBADID, MOE_EBOUNDS, MOE_ENOTPLANNED = -4, -5, -6, -7
 MOE_DTYPE_BF16, MOE_DTYPE_FP8_E4M3, MOE_DTYPE_FP16, MOE_DTYPE_FP32 = 0, 1, 2, 3
 MOE_CLASS_DECODE, MOE_CLASS_PREFILL = 0, 1
+MOE_SCORES_SOFTMAX, MOE_SCORES_SIGMOID = 0, 1
 MOE_LAYOUT_GATHERED, MOE_LAYOUT_MASKED = 0, 1
 MOE_TILE_M = 128
 
@@ -32,7 +33,8 @@ EXPORTS = ("moe_workspace_bytes", "moe_create", "moe_destroy", "moe_plan", "moe_
            "moe_read_tile_table", "moe_read_tile_log", "moe_sm_count", "moe_ctas_per_tile", "moe_strerror",
            "moe_plan_static", "moe_route", "moe_run_plain", "moe_plan_pair", "moe_route_grad", "moe_sort_rows",
            "moe_sort_rows_grad", "moe_merge_rows", "moe_merge_rows_grad", "moe_mx_quantize", "moe_mx_dequantize",
-           "moe_mx_product", "moe_mx_swiglu")
+           "moe_mx_product", "moe_mx_swiglu", "moe_choose_experts", "moe_choose_experts_grad", "moe_scaled_quantize",
+           "moe_scaled_quantize_weights", "moe_scaled_dequantize", "moe_scaled_product", "moe_scaled_swiglu")
 MOE_PLAN_STATIC_MAX_ROWS, MOE_PLAN_STATIC_MAX_EXPERTS = 32768, 256
 
 
@@ -113,6 +115,13 @@ def lib() -> C.CDLL:
         L.moe_mx_dequantize.argtypes = [vp, vp, i64, i32, i32, vp, vp]
         L.moe_mx_product.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp]
         L.moe_mx_swiglu.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp]
+        L.moe_choose_experts.argtypes = [vp, i64, i32, vp, i32, i32, i32, i32, i32, i32, i32, i32, C.c_float, vp, vp, vp]
+        L.moe_choose_experts_grad.argtypes = [vp, i64, i32, vp, vp, i32, i32, i32, i32, i32, C.c_float, vp, vp]
+        L.moe_scaled_quantize.argtypes = [vp, i64, i32, i32, i32, i32, vp, vp, vp, vp, vp]
+        L.moe_scaled_quantize_weights.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp]
+        L.moe_scaled_dequantize.argtypes = [vp, vp, i32, i32, i32, i32, i32, vp, vp]
+        L.moe_scaled_product.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, vp]
+        L.moe_scaled_swiglu.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp]
         L.moe_sm_count.argtypes = [vp]
         L.moe_ctas_per_tile.argtypes = [vp]
         L.moe_strerror.argtypes = [C.c_int]
@@ -445,7 +454,8 @@ class Context:
 
 
 _IN_ROWS = ("sort_rows", "sort_rows_grad", "merge_rows", "merge_rows_grad", "route_grad", "mx_quantize", "mx_dequantize", "mx_product",
-            "mx_swiglu")
+            "mx_swiglu", "choose_experts", "choose_experts_grad", "scaled_quantize", "scaled_quantize_weights", "scaled_dequantize",
+            "scaled_product", "scaled_swiglu")
 
 
 def __getattr__(name):

@@ -1,0 +1,25 @@
+// Rows in e4m3 with an fp32 scale per 128 neighbours: the arithmetic that the quantisers and the products share.
+//
+// The scale of a block is amax / 448 (448: the largest e4m3 value), 1 for a block of zeros, 2^-126 at least (a normal number, so that its reciprocal is
+// one too).  A block that holds a NaN or an infinity has a NaN scale, which makes all of its values NaN.
+#pragma once
+#include <stdint.h>
+
+namespace moe {
+
+constexpr int kScaledBlock = 128;
+
+// of a block whose largest magnitude has these bits (NaN and infinities are above every number)
+__device__ __forceinline__ float scaled_scale(unsigned amax_bits) {
+  if (amax_bits >= 0x7f800000u) return __uint_as_float(0x7fffffffu);
+  return amax_bits == 0u ? 1.f : fmaxf(__fdiv_rn(__uint_as_float(amax_bits), 448.f), 0x1p-126f);
+}
+// two e4m3 codes, `first` in the low byte; rounded to nearest, ties to even, magnitudes above 448 to 448
+__device__ __forceinline__ unsigned e4m3_codes2(float first, float second) {
+  unsigned short r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %2, %1;" : "=h"(r) : "f"(first), "f"(second));
+  return r;
+}
+__device__ __forceinline__ unsigned e4m3_codes4(const float* v) { return e4m3_codes2(v[0], v[1]) | e4m3_codes2(v[2], v[3]) << 16; }
+
+}  // namespace moe

@@ -1,0 +1,635 @@
+// moe_scaled_product / moe_scaled_swiglu: sorted e4m3 rows with a scale per 128 columns times the experts' e4m3 matrices with a scale per 128 x 128.
+//
+//   product   out[p, n] = sum_b sx[p, b] sw[e, n / 128, b] sum_{k in block b} x[p, k] w[e, n, k]        (rounded once)
+//   swiglu    g, u = products with rows n and I + n of w[e];  a = g / (1 + exp(-g)) u in fp32, quantised per 128 columns to codes and a scale
+//
+// tcgen05.mma.kind::f8f6f4 knows no scales, so the 128 products of a block are added up in the tensor core, each block in a fresh buffer in TMEM, and eight
+// epilogue warps read every such partial and multiply-add it with its two scales into fp32 registers.
+//
+// Two forms.  Few rows an expert (kTall false): weight rows are the M of the instruction, twice 128 TMEM lanes, up to 64 rows its N in steps of 16; one
+// CTA a tile; the bound is the weight stream.  Many (kTall): 256 rows are the M of a pair of CTAs (cta_group::2), 256 weight rows its N; each CTA holds 128 of
+// either.  A thread then has a row: one multiplier for all of its columns.
+//
+// Roles: warps 0-7 epilogue, 8 TMA (one thread; a stage is a block of 128 columns: 128-byte rows, swizzled), 9 MMA (one thread), 10 and 11 bring the
+// products of the two scales, four blocks at a time, into a ring in shared memory.
+// Every wait is bounded (2 s); where one runs out the launch ends, after another such limit for its copies in flight, and what it has not computed is NaN.
+#include <cuda_fp16.h>
+
+#include "moe_dev.cuh"
+#include "moe_grouped.cuh"
+#include "moe_ptx.cuh"
+#include "moe_scaled.cuh"
+
+namespace moe {
+namespace {
+
+constexpr int kThreads = 384;
+constexpr int kTmaWarp = 8, kMmaWarp = 9, kScaleWarp = 10, kScaleThreads = 64;
+constexpr int kBlock = kScaledBlock;
+constexpr int kQuad = 4;                        // blocks whose scales are handed over together
+constexpr int kQuads = 3;                       // ... of them in the ring
+
+struct Shared : Segments {
+  unsigned long long full[8], empty[8], part_full[4], part_empty[4], scales_full[kQuads], scales_empty[kQuads], drained;
+  unsigned tmem;
+  volatile int dead;             // a wait ran out
+  unsigned tops[2][2][128];      // swiglu: largest magnitudes on their way from warp to warp
+};
+
+template <bool kTall>
+struct Shape {
+  static constexpr int kCtas = kTall ? 2 : 1;
+  static constexpr int kRows = kTall ? 256 : 64;                    // of a tile
+  static constexpr int kMine = kRows / kCtas;                       // ... in this CTA
+  static constexpr int kWBytes = 256 / kCtas * kBlock, kXBytes = kMine * kBlock, kStageBytes = kWBytes + kXBytes;
+  static constexpr int kBoxRows = kTall ? 64 : 32;                  // of a TMA box of rows
+  static constexpr int kPartCols = kTall ? 256 : 2 * kRows;         // TMEM columns of a partial
+  static constexpr int kParts = 512 / kPartCols;
+  static constexpr int kScaleFloats = kQuad * 2 * kMine;            // of a place in the ring: [block][half][row]
+  static constexpr int kScaleBytes = kQuads * kScaleFloats * 4;
+  static constexpr int kStages = (227 * 1024 - 1024 - (int)sizeof(Shared) - kScaleBytes) / kStageBytes;
+  static constexpr int kSmem = 1024 + kStages * kStageBytes + kScaleBytes + (int)sizeof(Shared);
+  static_assert(kStages >= 3 && kStages <= 8 && kParts <= 4, "barriers");
+};
+
+struct Args {
+  CUtensorMap tm_w;              // [E][parts][rows][K], parts: gate and up for swiglu, else 1
+  CUtensorMap tm_x;              // [R][K]
+  const float* x_scales;         // [R, blocks]
+  const float* w_scales;         // [E, row_blocks, blocks]
+  const int* offsets;            // [E + 1], or NULL: one matrix for all rows
+  void* out;                     // [R, N], or codes [R, I]
+  float* out_scales;             // swiglu: [R, I / 128]
+  int R, E, N, I;                // N: weight rows; I: N / 2 for swiglu
+  int blocks, row_blocks;
+  int dtype, wide;               // of out; its rows are 16-byte aligned
+  int wide_scales;               // four scales of a row can be loaded at once
+};
+
+// e4m3 operands, fp32 sums, both K-major, M rows, N columns
+__device__ __forceinline__ unsigned idesc_of(unsigned m, unsigned n) { return 1u << 4 | (n >> 3) << 17 | (m >> 4) << 24; }
+// one block: four products of 32 columns into fresh sums
+template <bool kPair>
+__device__ __forceinline__ void mma_block(unsigned d, unsigned long long a, unsigned long long b, unsigned idesc) {
+  if (kPair)
+    asm volatile(
+        "{\n\t.reg .pred p0, p1;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\t"
+        "setp.ne.b32 p0, 0, 0;\n\tsetp.eq.b32 p1, 0, 0;\n\t"
+        "add.u64 a1, %1, 2;\n\tadd.u64 a2, %1, 4;\n\tadd.u64 a3, %1, 6;\n\t"
+        "add.u64 b1, %2, 2;\n\tadd.u64 b2, %2, 4;\n\tadd.u64 b3, %2, 6;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], a1, b1, %3, p1;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], a2, b2, %3, p1;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], a3, b3, %3, p1;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p0, p1;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\t"
+        "setp.ne.b32 p0, 0, 0;\n\tsetp.eq.b32 p1, 0, 0;\n\t"
+        "add.u64 a1, %1, 2;\n\tadd.u64 a2, %1, 4;\n\tadd.u64 a3, %1, 6;\n\t"
+        "add.u64 b1, %2, 2;\n\tadd.u64 b2, %2, 4;\n\tadd.u64 b3, %2, 6;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a1, b1, %3, p1;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a2, b2, %3, p1;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a3, b3, %3, p1;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc)
+        : "memory");
+}
+template <bool kPair>
+__device__ __forceinline__ void tma_4d(unsigned dst, const CUtensorMap* m, int x, int y, int z, int w, unsigned bar, unsigned long long policy) {
+  if (kPair)
+    asm volatile(
+        "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4, %5}], [%6], %7;" ::"r"(dst),
+        "l"(reinterpret_cast<unsigned long long>(m)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar), "l"(policy)
+        : "memory");
+  else
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4, %5}], [%6], %7;" ::"r"(dst),
+        "l"(reinterpret_cast<unsigned long long>(m)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar), "l"(policy)
+        : "memory");
+}
+__device__ __forceinline__ float4 ld_shared_f4(unsigned saddr) {
+  float4 v;
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(saddr) : "memory");
+  return v;
+}
+__device__ __forceinline__ float ld_shared_f(unsigned saddr) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(saddr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void st_shared_f(unsigned saddr, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(saddr), "f"(v) : "memory"); }
+__device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+
+template <class E> __device__ __forceinline__ E rounded(float v);
+template <> __device__ __forceinline__ float rounded(float v) { return v; }
+template <> __device__ __forceinline__ __half rounded(float v) { return __float2half_rn(v); }
+template <> __device__ __forceinline__ __nv_bfloat16 rounded(float v) { return __float2bfloat16_rn(v); }
+// f with a pointer of the outputs' type
+template <class F>
+__device__ __forceinline__ void with_type(int dtype, void* out, F f) {
+  if (dtype == MOE_DTYPE_BF16) f(static_cast<__nv_bfloat16*>(out));
+  else if (dtype == MOE_DTYPE_FP16) f(static_cast<__half*>(out));
+  else f(static_cast<float*>(out));
+}
+
+template <bool kTall, bool kSwiglu>
+__global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __grid_constant__ Args a) {
+  using S = Shape<kTall>;
+  constexpr bool kPair = kTall;
+  extern __shared__ unsigned char raw[];
+  unsigned char* stages = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+  float* ring = reinterpret_cast<float*>(stages + S::kStages * S::kStageBytes);
+  Shared& s = *reinterpret_cast<Shared*>(reinterpret_cast<unsigned char*>(ring) + S::kScaleBytes);
+  const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
+  constexpr int kStep = kSwiglu ? 128 : 256;                       // output columns of a tile
+  const unsigned rank = kPair ? cluster_ctarank() : 0u;
+  const int unit = (int)blockIdx.x / S::kCtas, n_units = (int)gridDim.x / S::kCtas;
+  const int n_blocks = ((kSwiglu ? a.I : a.N) + kStep - 1) / kStep;
+
+  if (tid == 0) {
+    for (int i = 0; i < S::kStages; ++i) {
+      mbar_init(&s.full[i], S::kCtas);
+      mbar_init(&s.empty[i], 1);
+    }
+    for (int i = 0; i < S::kParts; ++i) {
+      mbar_init(&s.part_full[i], 1);
+      mbar_init(&s.part_empty[i], 8 * S::kCtas);
+    }
+    for (int i = 0; i < kQuads; ++i) {
+      mbar_init(&s.scales_full[i], kScaleThreads / 32);
+      mbar_init(&s.scales_empty[i], 8);
+    }
+    mbar_init(&s.drained, 1);
+    s.dead = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async_proxy_smem();
+  }
+  if (warp == kMmaWarp) {
+    if (kPair) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s.tmem)) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s.tmem)) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+  }
+  grid_dep_wait();
+#pragma unroll 1
+  for (int e = tid; e <= a.E; e += kThreads) s.first_row[e] = a.offsets ? min(max(a.offsets[e], 0), a.R) : e ? a.R : 0;
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 0) list_tiles<S::kRows>(s, a.E, n_blocks, lane);
+  __syncthreads();
+  if (kPair) cluster_sync_all();          // the other CTA's barriers exist before anything arrives on them
+  const unsigned tmem = s.tmem;
+  const int n_tiles = uniform(s.first_tile[a.E]);
+
+  if (warp < kTmaWarp) {
+    if (kTall) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    const int quarter = warp & 3, half = warp >> 2;
+    const unsigned lanes = tmem + ((unsigned)quarter << 21);       // this warp's 32 TMEM lanes
+    unsigned part = 0, place = 0;  // partials, places in the ring so far
+    unsigned turn = 0;             // exchanges of maxima so far
+    bool ok = true;
+    for (int t = unit; t < n_tiles; t += n_units) {
+      const Tile at = uniform(tile_at<S::kRows>(s, a.E, t, kStep));
+      const auto next_partial = [&] {
+        const unsigned buf = part % S::kParts;
+        if (ok) ok = __all_sync(0xffffffffu, wait(&s.part_full[buf], (part / S::kParts) & 1, &s.dead));
+        tc_fence_after();
+        return lanes + buf * S::kPartCols;
+      };
+      const auto hand_back = [&] {           // every lane has what it loads of the partial
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if (kPair) mbar_arrive_relaxed(map_to_cta(&s.part_empty[part % S::kParts], 0));
+          else mbar_arrive(&s.part_empty[part % S::kParts]);
+        }
+        ++part;
+      };
+      const auto scales_at = [&](int b) {    // of block b: [half][row]
+        if (b % kQuad == 0 && ok) ok = __all_sync(0xffffffffu, wait(&s.scales_full[place % kQuads], (place / kQuads) & 1, &s.dead));
+        return smem_u32(ring + (place % kQuads) * S::kScaleFloats + (b % kQuad) * 2 * S::kMine);
+      };
+      const auto scales_read = [&](int b) {
+        if (b % kQuad != kQuad - 1 && b != a.blocks - 1) return;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&s.scales_empty[place % kQuads]);
+        ++place;
+      };
+      if constexpr (kTall) {
+        const int mine = 32 * quarter + lane, row = 128 * (int)rank + mine;
+        const bool used = uniform(128 * (int)rank + 32 * quarter) < at.rows, valid = row < at.rows;
+        float acc[128];            // plain: the columns of this half; swiglu: 64 gate and 64 up columns
+#pragma unroll
+        for (int i = 0; i < 128; ++i) acc[i] = 0.f;
+#pragma unroll 1
+        for (int b = 0; b < a.blocks; ++b) {
+          const unsigned sc = scales_at(b);
+          const unsigned from = next_partial();
+          if (!ok) break;
+          if (!used) {
+            hand_back();
+            scales_read(b);
+            continue;
+          }
+          const float s0 = ld_shared_f(sc + (kSwiglu ? 0 : half * 4 * S::kMine) + 4 * mine);
+          const float s1 = kSwiglu ? ld_shared_f(sc + 4 * S::kMine + 4 * mine) : s0;
+          scales_read(b);
+          unsigned p[2][32];
+          const auto col = [&](int c) { return from + (kSwiglu ? (c >> 1) * 128 + half * 64 + (c & 1) * 32 : half * 128 + c * 32); };
+          tc_ld32(col(0), p[0]);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            tc_wait_ld();
+            if (c < 3) tc_ld32(col(c + 1), p[(c + 1) & 1]);
+            else hand_back();
+            const float m = c < 2 ? s0 : s1;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) acc[32 * c + i] = fmaf(__uint_as_float(p[c & 1][i]), m, acc[32 * c + i]);
+          }
+        }
+        if (!used) {
+          if (kSwiglu) {
+            ++turn;
+            bar_sync(1 + quarter, 64);
+          }
+          continue;
+        }
+        const size_t p = (size_t)at.row0 + row;
+        if constexpr (kSwiglu) {
+          unsigned top = 0u;
+#pragma unroll
+          for (int i = 0; i < 64; ++i) {
+            acc[i] = silu_times(acc[i], acc[64 + i]);
+            top = max(top, __float_as_uint(acc[i]) & 0x7fffffffu);
+          }
+          s.tops[turn & 1][half][mine] = top;
+          bar_sync(1 + quarter, 64);
+          top = max(top, s.tops[turn++ & 1][half ^ 1][mine]);
+          const float scale = ok ? scaled_scale(top) : __uint_as_float(0x7fffffffu), inv = __fdividef(1.f, scale);
+          if (valid) {
+            uint4* to = reinterpret_cast<uint4*>(static_cast<unsigned char*>(a.out) + p * a.I + at.n0 + 64 * half);
+#pragma unroll
+            for (int i = 0; i < 64; ++i) acc[i] *= inv;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              to[i] = make_uint4(e4m3_codes4(acc + 16 * i), e4m3_codes4(acc + 16 * i + 4), e4m3_codes4(acc + 16 * i + 8), e4m3_codes4(acc + 16 * i + 12));
+            if (half == 0) a.out_scales[p * (a.I / kBlock) + at.n0 / kBlock] = scale;
+          }
+        } else {
+          const int col0 = at.n0 + 128 * half, cols = min(128, a.N - col0);
+          if (!ok) {
+#pragma unroll
+            for (int i = 0; i < 128; ++i) acc[i] = __uint_as_float(0x7fffffffu);
+          }
+          if (valid)
+            with_type(a.dtype, a.out, [&](auto* out) {
+              using E = typename std::remove_pointer<decltype(out)>::type;
+              out += p * a.N + col0;
+              constexpr int kIn = 16 / (int)sizeof(E);
+              if (a.wide) {
+#pragma unroll
+                for (int i = 0; i < 128; i += kIn) {
+                  uint4 v;
+#pragma unroll
+                  for (int j = 0; j < kIn; ++j) reinterpret_cast<E*>(&v)[j] = rounded<E>(acc[i + j]);
+                  if (i < cols) *reinterpret_cast<uint4*>(out + i) = v;
+                }
+              } else {
+#pragma unroll
+                for (int i = 0; i < 128; ++i)
+                  if (i < cols) out[i] = rounded<E>(acc[i]);
+              }
+            });
+        }
+      } else {
+        // groups of 16 rows; plain: all of them, of the 128 weight rows of this half; swiglu: every other, gate and up
+        const int groups = uniform((at.rows + 15) / 16);
+        constexpr int kGroups = kSwiglu ? 2 : 4;
+        const auto group = [&](int i) { return kSwiglu ? half + 2 * i : i; };
+        float acc[kGroups][kSwiglu ? 2 : 1][16];
+#pragma unroll
+        for (int i = 0; i < kGroups; ++i)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            acc[i][0][j] = 0.f;
+            if (kSwiglu) acc[i][kSwiglu ? 1 : 0][j] = 0.f;
+          }
+#pragma unroll 1
+        for (int b = 0; b < a.blocks; ++b) {
+          const unsigned sc = scales_at(b);
+          const unsigned from = next_partial();
+          if (!ok) break;
+          unsigned p[kGroups][kSwiglu ? 2 : 1][16];
+#pragma unroll
+          for (int i = 0; i < kGroups; ++i)
+            if (group(i) < groups) {
+              tc_ld16(from + (kSwiglu ? 0 : half * S::kRows) + 16 * group(i), p[i][0]);
+              if (kSwiglu) tc_ld16(from + S::kRows + 16 * group(i), p[i][kSwiglu ? 1 : 0]);
+            }
+          tc_wait_ld();
+          hand_back();
+#pragma unroll
+          for (int i = 0; i < kGroups; ++i)
+            if (group(i) < groups) {
+#pragma unroll
+              for (int h = 0; h < (kSwiglu ? 2 : 1); ++h)
+#pragma unroll
+                for (int j = 0; j < 16; j += 4) {
+                  const float4 m = ld_shared_f4(sc + 4 * ((kSwiglu ? h : half) * S::kMine + 16 * group(i) + j));
+                  acc[i][h][j] = fmaf(__uint_as_float(p[i][h][j]), m.x, acc[i][h][j]);
+                  acc[i][h][j + 1] = fmaf(__uint_as_float(p[i][h][j + 1]), m.y, acc[i][h][j + 1]);
+                  acc[i][h][j + 2] = fmaf(__uint_as_float(p[i][h][j + 2]), m.z, acc[i][h][j + 2]);
+                  acc[i][h][j + 3] = fmaf(__uint_as_float(p[i][h][j + 3]), m.w, acc[i][h][j + 3]);
+                }
+            }
+          scales_read(b);
+        }
+        const int n = at.n0 + (kSwiglu ? 0 : 128 * half) + 32 * quarter + lane;
+        if constexpr (kSwiglu) {
+#pragma unroll
+          for (int i = 0; i < kGroups; ++i) {
+            if (group(i) >= groups) break;
+            unsigned mine = 0u;    // lane j < 16: of row j of the group
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              acc[i][0][j] = silu_times(acc[i][0][j], acc[i][kSwiglu ? 1 : 0][j]);
+              const unsigned top = __reduce_max_sync(0xffffffffu, __float_as_uint(acc[i][0][j]) & 0x7fffffffu);
+              if (lane == j) mine = top;
+            }
+            unsigned* tops = s.tops[turn++ & 1][half];
+            if (lane < 16) tops[16 * quarter + lane] = mine;
+            bar_sync(1 + half, 128);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) mine = max(mine, tops[16 * q + (lane & 15)]);
+            const float scale = ok ? scaled_scale(mine) : __uint_as_float(0x7fffffffu), inv = __fdividef(1.f, scale);
+            const int row = 16 * group(i);
+            if (quarter == 0 && lane < 16 && row + lane < at.rows)
+              a.out_scales[((size_t)at.row0 + row + lane) * (a.I / kBlock) + at.n0 / kBlock] = scale;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const unsigned code = e4m3_codes2(acc[i][0][j] * __shfl_sync(0xffffffffu, inv, j), 0.f) & 0xffu;
+              if (row + j < at.rows) static_cast<unsigned char*>(a.out)[((size_t)at.row0 + row + j) * a.I + n] = (unsigned char)code;
+            }
+          }
+        } else {
+          with_type(a.dtype, a.out, [&](auto* out) {
+            using E = typename std::remove_pointer<decltype(out)>::type;
+#pragma unroll
+            for (int i = 0; i < kGroups; ++i) {
+              if (i >= groups) break;
+#pragma unroll
+              for (int j = 0; j < 16; ++j)
+                if (16 * i + j < at.rows && n < a.N)
+                  out[((size_t)at.row0 + 16 * i + j) * a.N + n] = rounded<E>(ok ? acc[i][0][j] : __uint_as_float(0x7fffffffu));
+            }
+          });
+        }
+      }
+    }
+    // rows that belong to no expert: zeros (scales 1), by the epilogue warps of the whole grid
+    const int lo = s.first_row[0], hi = s.first_row[a.E], none = lo + (a.R - hi);
+    for (int i = blockIdx.x; i < none; i += gridDim.x) {
+      const size_t p = (size_t)(i < lo ? i : hi + (i - lo));
+      if (kSwiglu) {
+#pragma unroll 1
+        for (int c = tid; c < a.I; c += 256) {
+          static_cast<unsigned char*>(a.out)[p * a.I + c] = 0;
+          if (c < a.I / kBlock) a.out_scales[p * (a.I / kBlock) + c] = 1.f;
+        }
+      } else {
+        with_type(a.dtype, a.out, [&](auto* out) {
+          using E = typename std::remove_pointer<decltype(out)>::type;
+#pragma unroll 1
+          for (int c = tid; c < a.N; c += 256) out[p * a.N + c] = rounded<E>(0.f);
+        });
+      }
+    }
+  } else {
+    if (kTall) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    if (warp == kTmaWarp) {
+      if (elect_one()) {
+        unsigned n = 0;            // stages so far
+        for (int t = unit; t < n_tiles && !s.dead; t += n_units) {
+          const Tile at = tile_at<S::kRows>(s, a.E, t, kStep);
+          const int row0 = at.row0 + (int)rank * S::kMine, mine = min(S::kMine, at.rows - (int)rank * S::kMine);
+          const int boxes = mine > 0 ? (mine + S::kBoxRows - 1) / S::kBoxRows : 0;
+          const unsigned long long policy = at.alone ? l2_evict_first() : l2_evict_normal();
+          const int n0 = at.n0 + (kSwiglu ? 0 : 128 * (int)rank), which = kSwiglu ? (int)rank : 0;
+#pragma unroll 1
+          for (int i = 0; i < a.blocks; ++i, ++n) {
+            const unsigned slot = n % S::kStages, round = n / S::kStages;
+            if (round && !wait(&s.empty[slot], (round - 1) & 1, &s.dead)) break;
+            const unsigned to = smem_u32(stages + slot * S::kStageBytes);
+            const unsigned bar = kPair ? map_to_cta(&s.full[slot], 0) : smem_u32(&s.full[slot]);
+            expect_tx(bar, S::kWBytes + boxes * S::kBoxRows * kBlock);
+            tma_4d<kPair>(to, &a.tm_w, i * kBlock, n0, which, at.expert, bar, policy);
+#pragma unroll 1
+            for (int x = 0; x < boxes; ++x)
+              tma_2d<kPair>(to + S::kWBytes + x * S::kBoxRows * kBlock, &a.tm_x, i * kBlock, row0 + x * S::kBoxRows, bar);
+          }
+        }
+        // The block's shared memory belongs to its copies until they have landed, and where another role has given up nobody else waits for the last ones.
+        // The second CTA of a pair, whose copies count on the leader's barriers, sees its own by the stages that the MMAs are done with (or runs into the limit).
+        const unsigned long long start = gtime_ns();
+#pragma unroll 1
+        for (unsigned m = n > S::kStages ? n - S::kStages : 0; m < n; ++m) {
+          unsigned long long* bar = rank ? &s.empty[m % S::kStages] : &s.full[m % S::kStages];
+          while (!mbar_try(bar, (m / S::kStages) & 1) && gtime_ns() - start < kWaitNs) {}
+        }
+      }
+      __syncwarp();
+    } else if (warp == kMmaWarp) {
+      if (rank == 0 && elect_one()) {
+        const auto commit = [](unsigned long long* bar) {
+          if (kPair) tc_commit_pair(bar);
+          else tc_commit(bar);
+        };
+        unsigned n = 0;            // blocks so far
+        bool ok = true;
+        for (int t = unit; t < n_tiles && ok; t += n_units) {
+          const Tile at = tile_at<S::kRows>(s, a.E, t, kStep);
+          const unsigned idesc = kTall ? idesc_of(256, 256) : idesc_of(128, (unsigned)(at.rows + 15) & ~15u);
+#pragma unroll 1
+          for (int i = 0; i < a.blocks; ++i, ++n) {
+            const unsigned slot = n % S::kStages, round = n / S::kStages, buf = n % S::kParts, use = n / S::kParts;
+            // (a pair's arrivals are relaxed: what they hand back is ordered by the tcgen05 fences on both sides)
+            if (use) ok = wait<kPair ? mbar_try_relaxed : mbar_try>(&s.part_empty[buf], (use - 1) & 1, &s.dead);
+            ok = ok && wait(&s.full[slot], round & 1, &s.dead);
+            if (!ok) break;
+            tc_fence_after();
+            const unsigned st = smem_u32(stages + slot * S::kStageBytes), d = tmem + buf * S::kPartCols;
+            const unsigned long long w = umma_desc(st, 128), x = umma_desc(st + S::kWBytes, 128);
+            if (kTall) {
+              mma_block<kPair>(d, x, w, idesc);
+            } else {
+              mma_block<kPair>(d, w, x, idesc);
+              mma_block<kPair>(d + S::kRows, umma_desc(st + 128 * kBlock, 128), x, idesc);
+            }
+            commit(&s.empty[slot]);
+            commit(&s.part_full[buf]);
+          }
+        }
+        commit(&s.drained);     // nothing of this block's is left in the tensor core when it frees its TMEM
+        const unsigned long long start = gtime_ns();
+        while (!mbar_try(&s.drained, 0) && gtime_ns() - start < kWaitNs) {}
+      }
+      __syncwarp();
+    } else {
+      // A thread has one row of the tile (few rows) or two: it loads four blocks' scales and those of both halves' weights, and stores the products.
+      constexpr int kOwn = S::kMine / kScaleThreads;
+      const int r0 = tid - 32 * kScaleWarp;
+      unsigned place = 0;
+      const auto four = [&](const float* p, int left, float (&v)[4]) {
+        if (a.wide_scales) {
+          const float4 q = __ldg(reinterpret_cast<const float4*>(p));
+          v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = i < left ? __ldg(p + i) : 0.f;
+        }
+      };
+      bool ok = true;
+      for (int t = unit; t < n_tiles && ok; t += n_units) {
+        const Tile at = uniform(tile_at<S::kRows>(s, a.E, t, kStep));
+        const float* w0 = a.w_scales + ((size_t)at.expert * a.row_blocks + at.n0 / kBlock) * a.blocks;
+        const int second = kSwiglu ? a.I / kBlock : at.n0 / kBlock + 1 < a.row_blocks ? 1 : 0;      // (a half behind the last row: any scale, nothing of it is stored)
+        const float* w1 = w0 + (size_t)second * a.blocks;
+        const float* x[kOwn];
+#pragma unroll
+        for (int q = 0; q < kOwn; ++q)
+          x[q] = a.x_scales + ((size_t)at.row0 + min((int)rank * S::kMine + r0 + q * kScaleThreads, at.rows - 1)) * a.blocks;
+#pragma unroll 1
+        for (int b = 0; b < a.blocks; b += kQuad, ++place) {
+          float u[kOwn][4], v0[4], v1[4];
+          four(w0 + b, a.blocks - b, v0);
+          four(w1 + b, a.blocks - b, v1);
+#pragma unroll
+          for (int q = 0; q < kOwn; ++q) four(x[q] + b, a.blocks - b, u[q]);
+          const unsigned slot = place % kQuads, round = place / kQuads;
+          if (round) ok = __all_sync(0xffffffffu, wait(&s.scales_empty[slot], (round - 1) & 1, &s.dead));
+          if (!ok) break;
+          const unsigned to = smem_u32(ring + slot * S::kScaleFloats + r0);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int q = 0; q < kOwn; ++q) {
+              st_shared_f(to + 4 * (2 * i * S::kMine + q * kScaleThreads), u[q][i] * v0[i]);
+              st_shared_f(to + 4 * ((2 * i + 1) * S::kMine + q * kScaleThreads), u[q][i] * v1[i]);
+            }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&s.scales_full[slot]);
+        }
+      }
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (kPair) cluster_sync_all();          // no CTA leaves while the other may still signal its barriers, or read its shared memory
+  if (warp == kMmaWarp) {
+    tc_fence_after();
+    if (kPair) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+}
+
+// codes as bytes [e][parts][rows][cols], boxes of 128 bytes x box_rows rows x box_parts
+bool encode(CUtensorMap* out, const void* base, int cols, int rows, int parts, int e, int box_rows, int box_parts) {
+  const EncodeFn fn = encoder();
+  if (!fn) return false;
+  const cuuint64_t dims[4] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)parts, (cuuint64_t)e};
+  const cuuint64_t strides[3] = {(cuuint64_t)cols, (cuuint64_t)cols * rows, (cuuint64_t)cols * rows * parts};
+  const cuuint32_t box[4] = {128u, (cuuint32_t)box_rows, (cuuint32_t)box_parts, 1u}, one[4] = {1u, 1u, 1u, 1u};
+  return fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, parts ? 4 : 2, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool kTall, bool kSwiglu>
+cudaError_t product_launch(Args& a, const void* codes, const void* w_codes, int K, cudaStream_t stream) {
+  using S = Shape<kTall>;
+  static_assert(S::kSmem <= 227 * 1024, "shared memory");
+  const int parts = kSwiglu ? 2 : 1;
+  // a CTA's weight rows: tall 128 (swiglu: gate or up rows), else 256 (128 of both)
+  if (!encode(&a.tm_w, w_codes, K, a.N / parts, parts, a.E, kTall || kSwiglu ? 128 : 256, kTall ? 1 : parts) ||
+      !encode(&a.tm_x, codes, K, a.R, 0, 0, S::kBoxRows, 0))
+    return cudaErrorInvalidValue;
+  auto* kernel = scaled_product_kernel<kTall, kSwiglu>;
+  int dev = 0, sms = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+  if (e != cudaSuccess) return e;
+  // most tiles that the rows can make
+  const int step = kSwiglu ? 128 : 256;
+  const long long m_tiles = a.R / S::kRows + (a.R < a.E ? a.R : a.E), tiles = m_tiles * (((kSwiglu ? a.I : a.N) + step - 1) / step);
+  if (tiles > 0x3fffffffll) return cudaErrorInvalidValue;
+  const int units = tiles < sms / S::kCtas ? (int)tiles : sms / S::kCtas;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = S::kCtas;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(units * S::kCtas));
+  cfg.blockDim = dim3((unsigned)kThreads);
+  cfg.dynamicSmemBytes = S::kSmem;
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = S::kCtas > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<const Args&>(a));
+}
+
+template <bool kSwiglu>
+int product(const void* codes, const float* scales, const void* w_codes, const float* w_scales, const int32_t* offsets, int n_rows, int n_experts, int n,
+            int K, int dtype, void* out, float* out_scales, void* stream) {
+  if (n_rows < 0 || n_rows >= 1 << kRowSlotShift || n_experts < 1 || n_experts > kMaxExperts || n < 1 || n > 1 << 30 || K < 16 || K > 1 << 30 || K % 16)
+    return MOE_EINVAL;
+  if (!kSwiglu && dtype != MOE_DTYPE_BF16 && dtype != MOE_DTYPE_FP16 && dtype != MOE_DTYPE_FP32) return MOE_EINVAL;
+  if (n_rows == 0) return MOE_OK;
+  if (!codes || !scales || !w_codes || !w_scales || !out || (kSwiglu && !out_scales) || (!offsets && n_experts != 1)) return MOE_EINVAL;
+  const int el = kSwiglu ? 16 : dtype == MOE_DTYPE_FP32 ? 4 : 2;
+  const auto address = [](const void* p) { return reinterpret_cast<uintptr_t>(p); };
+  if (((address(codes) | address(w_codes)) & 15) || ((address(scales) | address(w_scales) | address(offsets) | address(out_scales)) & 3) ||
+      (address(out) & (el - 1)))
+    return MOE_EINVAL;
+  Args a;
+  a.x_scales = scales;
+  a.w_scales = w_scales;
+  a.offsets = offsets;
+  a.out = out;
+  a.out_scales = out_scales;
+  a.R = n_rows; a.E = n_experts; a.N = n; a.I = n / 2;
+  a.blocks = (K + kBlock - 1) / kBlock;
+  a.row_blocks = (n + kBlock - 1) / kBlock;
+  a.dtype = dtype;
+  a.wide = (long long)n * el % 16 == 0 && (address(out) & 15) == 0;
+  a.wide_scales = a.blocks % 4 == 0 && ((address(scales) | address(w_scales)) & 15) == 0;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  // The form goes by the rows that an expert gets on average; the host does not know more.
+  const bool tall = n_rows > 64ll * n_experts;
+  const cudaError_t e = tall ? product_launch<true, kSwiglu>(a, codes, w_codes, K, st) : product_launch<false, kSwiglu>(a, codes, w_codes, K, st);
+  return e == cudaSuccess ? MOE_OK : MOE_ECUDA;
+}
+
+}  // namespace
+}  // namespace moe
+
+extern "C" {
+
+int moe_scaled_product(const void* codes, const float* scales, const void* w_codes, const float* w_scales, const int32_t* offsets, int32_t n_rows,
+                       int32_t n_experts, int32_t n_cols, int32_t k_cols, int32_t dtype, void* out, void* stream) {
+  return moe::product<false>(codes, scales, w_codes, w_scales, offsets, n_rows, n_experts, n_cols, k_cols, dtype, out, nullptr, stream);
+}
+
+int moe_scaled_swiglu(const void* codes, const float* scales, const void* w_codes, const float* w_scales, const int32_t* offsets, int32_t n_rows,
+                      int32_t n_experts, int32_t inter, int32_t k_cols, void* out_codes, float* out_scales, void* stream) {
+  if (inter < moe::kScaledBlock || inter % moe::kScaledBlock || inter > 1 << 29) return MOE_EINVAL;
+  return moe::product<true>(codes, scales, w_codes, w_scales, offsets, n_rows, n_experts, 2 * inter, k_cols, 0, out_codes, out_scales, stream);
+}
+
+}  // extern "C"

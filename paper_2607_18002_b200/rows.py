@@ -1,5 +1,5 @@
-"""The rows of a routed layer as tensors: sorted by expert and put together again, their gradients, the router's gradient, and the
-experts in 4 bits (moe_sort_rows ... moe_mx_swiglu of include/moe_apk.h).
+"""The rows of a routed layer as tensors: sorted by expert and put together again, their gradients, the router's gradient, routers by scores, and the
+experts in 4 bits or in e4m3 with block scales (moe_route_grad ... moe_scaled_swiglu of include/moe_apk.h).
 
 Checks of arguments and marshalling only; a call enqueues one kernel on `stream` (the current stream of the tensors' device if
 None) and allocates its outputs there.  Nothing is recorded for autograd: gradients are calls of their own.  Wrong types, shapes, strides
@@ -16,6 +16,15 @@ A permutation is the pair (sorted_to_flat, flat_to_sorted) of a plan, int32 [T*k
     codes, scales = mx_swiglu(codes, scales, w1_codes, w1_scales, offsets)
     rows = mx_product(codes, scales, w2_codes, w2_scales, offsets)
     y = merge_rows(rows, f2s, topk_w)
+
+    codes, scales = scaled_quantize(x, s2f, f2s, k)                      # ... in e4m3, weights from scaled_quantize_weights or a context's
+    codes, scales = scaled_swiglu(codes, scales, w1_codes, w1_scales, offsets)
+    rows = scaled_product(codes, scales, w2_codes, w2_scales, offsets)
+    y = merge_rows(rows, f2s, topk_w)
+    rows = scaled_product(codes, scales, w_codes, w_scales)              # one matrix [n, K] for all rows: a shared expert, a projection
+
+    ids, topk_w = choose_experts(logits, k, scores="sigmoid", bias=bias, groups=8, top_groups=4, scale=2.5)
+    dlogits = choose_experts_grad(logits, ids, dw, scores="sigmoid", scale=2.5)
 
     xs = sort_rows(x, s2f, f2s, k)                                       # training, with experts of the caller's own
     y = merge_rows(experts(xs), f2s, topk_w)
@@ -269,4 +278,184 @@ def mx_swiglu(codes, scales, w_codes, w_scales, offsets, stream=None):
                                                n // 2, K, out.data_ptr(), out_scales.data_ptr(), _stream(gpu))
     if rc:
         _failed(rc, "moe_mx_swiglu")
+    return out, out_scales
+
+
+_SCORES = {"softmax": moe.MOE_SCORES_SOFTMAX, "sigmoid": moe.MOE_SCORES_SIGMOID}
+_F8 = torch.float8_e4m3fn
+
+
+def choose_experts(logits, top_k: int, *, scores: str = "softmax", bias=None, groups: int = 1, top_groups: int = 1, group_sum: int = 2,
+                   renormalize: bool = True, scale: float = 1.0, stream=None):
+    """logits [T, E] (bf16, fp16, fp32) -> (topk_ids int32 [T, k], topk_w fp32 [T, k]): the k largest scores (softmax or sigmoid) plus bias [E] fp32
+    among the top_groups groups of experts, weighted by their scores (moe_choose_experts)."""
+    T, E, step = _rows(logits, "logits", _DTYPES)
+    gpu = logits.get_device()
+    if stream is not None or gpu != _current_device():
+        return _elsewhere(lambda: choose_experts(logits, top_k, scores=scores, bias=bias, groups=groups, top_groups=top_groups, group_sum=group_sum,
+                                                 renormalize=renormalize, scale=scale), logits.device, stream)
+    if scores not in _SCORES:
+        _refuse(f"scores must be one of {sorted(_SCORES)}")
+    if bias is not None:
+        _plain(bias, "bias", _FP32, (E,), gpu)
+    ids = _empty(T, max(top_k, 0), dtype=_I32, device=logits.device)
+    w = _empty(T, max(top_k, 0), dtype=_FP32, device=logits.device)
+    rc = (moe._lib or moe.lib()).moe_choose_experts(logits.data_ptr(), step, _DTYPES[logits.dtype], None if bias is None else bias.data_ptr(), T, E, top_k,
+                                                    groups, top_groups, group_sum, _SCORES[scores], renormalize, scale, ids.data_ptr(), w.data_ptr(),
+                                                    _stream(gpu))
+    if rc:
+        _failed(rc, "moe_choose_experts")
+    return ids, w
+
+
+def choose_experts_grad(logits, topk_ids, d_topk_w, *, scores: str = "softmax", renormalize: bool = True, scale: float = 1.0, stream=None):
+    """The gradient of choose_experts' weights, fp32 [T, k] -> that of the logits [T, E], of their type."""
+    T, E, step = _rows(logits, "logits", _DTYPES)
+    gpu = logits.get_device()
+    if stream is not None or gpu != _current_device():
+        return _elsewhere(lambda: choose_experts_grad(logits, topk_ids, d_topk_w, scores=scores, renormalize=renormalize, scale=scale), logits.device,
+                          stream)
+    if scores not in _SCORES:
+        _refuse(f"scores must be one of {sorted(_SCORES)}")
+    if not isinstance(topk_ids, _Tensor) or topk_ids.dim() != 2:
+        _refuse("topk_ids must be a CUDA int32 tensor [T, k]")
+    k = topk_ids.shape[1]
+    _plain(topk_ids, "topk_ids", _I32, (T, k), gpu)
+    _plain(d_topk_w, "d_topk_w", _FP32, (T, k), gpu)
+    dz = logits.new_empty(T, E)
+    rc = (moe._lib or moe.lib()).moe_choose_experts_grad(logits.data_ptr(), step, _DTYPES[logits.dtype], topk_ids.data_ptr(), d_topk_w.data_ptr(), T, E, k,
+                                                         _SCORES[scores], renormalize, scale, dz.data_ptr(), _stream(gpu))
+    if rc:
+        _failed(rc, "moe_choose_experts_grad")
+    return dz
+
+
+def _blocks(n):
+    return (n + 127) // 128
+
+
+def scaled_quantize(x, sorted_to_flat=None, flat_to_sorted=None, top_k: int = 1, stream=None):
+    """x [..., K] -> codes float8_e4m3fn [..., K], scales fp32 [..., ceil(K/128)]; with a permutation x [T, K] -> the T*k rows by expert.  Contiguous, or [T, K]
+    of any row stride."""
+    if isinstance(x, _Tensor) and x.dim() not in (0, 2) and x.is_contiguous() and sorted_to_flat is None and flat_to_sorted is None:
+        *lead, K = x.shape
+        codes, scales = scaled_quantize(x.view(x.numel() // K if K else 0, K), None, None, top_k, stream)
+        return codes.view(*lead, K), scales.view(*lead, scales.shape[1])
+    T, K, step = _rows(x, "x", _DTYPES)
+    gpu = x.get_device()
+    if stream is not None or gpu != _current_device():
+        return _elsewhere(scaled_quantize, x.device, stream, x, sorted_to_flat, flat_to_sorted, top_k)
+    if K % 16:
+        _refuse("x must have a multiple of 16 columns")
+    R = T * top_k
+    s2f = f2s = None
+    if sorted_to_flat is not None or flat_to_sorted is not None:
+        _index(sorted_to_flat, "sorted_to_flat", R, gpu)
+        _index(flat_to_sorted, "flat_to_sorted", R, gpu)
+        s2f, f2s = sorted_to_flat.data_ptr(), flat_to_sorted.data_ptr()
+    elif top_k != 1:
+        _refuse("top_k needs a permutation")
+    codes = _empty(R, K, dtype=_F8, device=x.device)
+    scales = _empty(R, _blocks(K), dtype=_FP32, device=x.device)
+    rc = (moe._lib or moe.lib()).moe_scaled_quantize(x.data_ptr(), step, _DTYPES[x.dtype], T, top_k, K, s2f, f2s, codes.data_ptr(), scales.data_ptr(),
+                                                     _stream(gpu))
+    if rc:
+        _failed(rc, "moe_scaled_quantize")
+    return codes, scales
+
+
+def scaled_quantize_weights(w, stream=None):
+    """w [E, n, K] or [n, K], contiguous -> codes float8_e4m3fn of that shape, scales fp32 [E, ceil(n/128), ceil(K/128)] or without E."""
+    if not isinstance(w, _Tensor) or w.dtype not in _DTYPES or not w.is_cuda or w.dim() not in (2, 3) or not w.is_contiguous():
+        _refuse(f"w must be a contiguous CUDA tensor [E, n, K] or [n, K] of one of {sorted(map(str, _DTYPES))}")
+    gpu = w.get_device()
+    if stream is not None or gpu != _current_device():
+        return _elsewhere(scaled_quantize_weights, w.device, stream, w)
+    *lead, n, K = w.shape
+    if K % 16 or not K or not n:
+        _refuse("w must have rows, and a multiple of 16 columns")
+    codes = _empty(w.shape, dtype=_F8, device=w.device)
+    scales = _empty(*lead, _blocks(n), _blocks(K), dtype=_FP32, device=w.device)
+    rc = (moe._lib or moe.lib()).moe_scaled_quantize_weights(w.data_ptr(), _DTYPES[w.dtype], lead[0] if lead else 1, n, K, codes.data_ptr(),
+                                                             scales.data_ptr(), _stream(gpu))
+    if rc:
+        _failed(rc, "moe_scaled_quantize_weights")
+    return codes, scales
+
+
+def _scaled(codes, scales, what, per_row):
+    """Codes [..., n, K] with a scale for every 128 columns of a row (per_row) or of 128 rows -> their shape and the number of their GPU."""
+    if not isinstance(codes, _Tensor) or not isinstance(scales, _Tensor):
+        _refuse(f"the codes and scales of {what} must be tensors")
+    shape, gpu = codes.shape, codes.get_device()
+    if codes.dtype is not _F8 and codes.dtype is not _U8 or scales.dtype is not _FP32 or not codes.is_cuda or gpu != scales.get_device() \
+            or not codes.is_contiguous() or not scales.is_contiguous() or len(shape) < 2 \
+            or scales.shape != (*shape[:-2], shape[-2] if per_row else _blocks(shape[-2]), _blocks(shape[-1])):
+        _refuse(f"the codes and scales of {what} must be contiguous e4m3 (or uint8) and fp32 tensors on one GPU, a scale for 128 columns "
+                f"of {'a row' if per_row else '128 rows'}")
+    return shape, gpu
+
+
+def scaled_dequantize(codes, scales, dtype=_BF16, stream=None):
+    """The values [..., n, K] that codes stand for with the scales of rows [..., n, ceil(K/128)] or of weights [..., ceil(n/128), ceil(K/128)]."""
+    if dtype not in _DTYPES:
+        _refuse(f"dtype must be one of {sorted(map(str, _DTYPES))}")
+    if isinstance(codes, _Tensor) and codes.dim() == 1:
+        return scaled_dequantize(codes[None], scales[None], dtype, stream)[0]
+    per_row = isinstance(codes, _Tensor) and isinstance(scales, _Tensor) and codes.dim() > 1 and scales.dim() > 1 and scales.shape[-2] == codes.shape[-2]
+    (*lead, n, K), gpu = _scaled(codes, scales, "the values", per_row)
+    if stream is not None or gpu != _current_device():
+        return _elsewhere(scaled_dequantize, codes.device, stream, codes, scales, dtype)
+    out = _empty(codes.shape, dtype=dtype, device=codes.device)
+    if out.numel():
+        rc = (moe._lib or moe.lib()).moe_scaled_dequantize(codes.data_ptr(), scales.data_ptr(), out.numel() // (n * K), n, K, 1 if per_row else 128,
+                                                           _DTYPES[dtype], out.data_ptr(), _stream(gpu))
+        if rc:
+            _failed(rc, "moe_scaled_dequantize")
+    return out
+
+
+def _scaled_operands(codes, scales, w_codes, w_scales, offsets):
+    """-> number of the GPU, R, E, n, K, address of the offsets"""
+    shape, gpu = _scaled(codes, scales, "the rows", True)
+    w_shape, w_gpu = _scaled(w_codes, w_scales, "the weights", False)
+    if len(shape) != 2 or len(w_shape) not in (2, 3) or w_shape[-1] != shape[1] or w_gpu != gpu:
+        _refuse(f"rows must be [R, K] and weights [E, n, K] or [n, K], all on cuda:{gpu}")
+    E = w_shape[0] if len(w_shape) == 3 else 1
+    if offsets is None:
+        if E != 1:
+            _refuse("more than one matrix needs offsets")
+    else:
+        _index(offsets, "offsets", E + 1, gpu)
+    return gpu, shape[0], E, w_shape[-2], shape[1], None if offsets is None else offsets.data_ptr()
+
+
+def scaled_product(codes, scales, w_codes, w_scales, offsets=None, dtype=_BF16, stream=None):
+    """Sorted e4m3 rows [R, K] times the experts' matrices [E, n, K], or all rows times [n, K] (no offsets) -> [R, n] of dtype."""
+    if dtype not in _DTYPES:
+        _refuse(f"dtype must be one of {sorted(map(str, _DTYPES))}")
+    gpu, R, E, n, K, at = _scaled_operands(codes, scales, w_codes, w_scales, offsets)
+    if stream is not None or gpu != _current_device():
+        return _elsewhere(scaled_product, codes.device, stream, codes, scales, w_codes, w_scales, offsets, dtype)
+    out = _empty(R, n, dtype=dtype, device=codes.device)
+    rc = (moe._lib or moe.lib()).moe_scaled_product(codes.data_ptr(), scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), at, R, E, n, K,
+                                                    _DTYPES[dtype], out.data_ptr(), _stream(gpu))
+    if rc:
+        _failed(rc, "moe_scaled_product")
+    return out
+
+
+def scaled_swiglu(codes, scales, w_codes, w_scales, offsets=None, stream=None):
+    """Sorted e4m3 rows [R, K] times gate and up matrices [E, 2 I, K] (or [2 I, K]), silu(gate) * up -> codes [R, I], scales [R, I/128]."""
+    gpu, R, E, n, K, at = _scaled_operands(codes, scales, w_codes, w_scales, offsets)
+    if stream is not None or gpu != _current_device():
+        return _elsewhere(scaled_swiglu, codes.device, stream, codes, scales, w_codes, w_scales, offsets)
+    if n % 256 or not n:
+        _refuse("the weights must have gate and up rows, a multiple of 128 each")
+    out = _empty(R, n // 2, dtype=_F8, device=codes.device)
+    out_scales = _empty(R, n // 256, dtype=_FP32, device=codes.device)
+    rc = (moe._lib or moe.lib()).moe_scaled_swiglu(codes.data_ptr(), scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), at, R, E, n // 2, K,
+                                                   out.data_ptr(), out_scales.data_ptr(), _stream(gpu))
+    if rc:
+        _failed(rc, "moe_scaled_swiglu")
     return out, out_scales

@@ -27,7 +27,8 @@ constexpr int kThreads = 384;
 constexpr int kTmaWarp = 8, kMmaWarp = 9, kScaleWarp = 10, kScaleThreads = 64;
 constexpr int kBlock = kScaledBlock;
 constexpr int kQuad = 4;                        // blocks whose scales are handed over together
-constexpr int kQuads = 3;                       // ... of them in the ring
+constexpr int kTurnPitch = 128 + 16, kTurnBytes = 32 * kTurnPitch;      // outputs on their way out: 32 rows of a warp; the 16 bytes spread eight of them over all banks
+constexpr int kQuads = 4;                       // ... of them in the ring
 
 struct Shared : Segments {
   unsigned long long full[8], empty[8], part_full[4], part_empty[4], scales_full[kQuads], scales_empty[kQuads], drained;
@@ -36,20 +37,22 @@ struct Shared : Segments {
   unsigned tops[2][2][128];      // swiglu: largest magnitudes on their way from warp to warp
 };
 
-template <bool kTall>
+template <bool kTall, bool kSwiglu>
 struct Shape {
   static constexpr int kCtas = kTall ? 2 : 1;
   static constexpr int kRows = kTall ? 256 : 64;                    // of a tile
   static constexpr int kMine = kRows / kCtas;                       // ... in this CTA
   static constexpr int kWBytes = 256 / kCtas * kBlock, kXBytes = kMine * kBlock, kStageBytes = kWBytes + kXBytes;
   static constexpr int kBoxRows = kTall ? 64 : 32;                  // of a TMA box of rows
-  static constexpr int kPartCols = kTall ? 256 : 2 * kRows;         // TMEM columns of a partial
-  static constexpr int kParts = 512 / kPartCols;
+  // A partial: 128 TMEM columns.  Tall: half of the columns of a block's products, which four of the epilogue's warps read, two for each half; else all of them.
+  static constexpr int kHalves = kTall ? 2 : 1;
+  static constexpr int kParts = 4 / kHalves;                        // of a half
   static constexpr int kScaleFloats = kQuad * 2 * kMine;            // of a place in the ring: [block][half][row]
   static constexpr int kScaleBytes = kQuads * kScaleFloats * 4;
-  static constexpr int kStages = (227 * 1024 - 1024 - (int)sizeof(Shared) - kScaleBytes) / kStageBytes;
-  static constexpr int kSmem = 1024 + kStages * kStageBytes + kScaleBytes + (int)sizeof(Shared);
-  static_assert(kStages >= 3 && kStages <= 8 && kParts <= 4, "barriers");
+  static constexpr int kOutBytes = kTall && !kSwiglu ? 8 * kTurnBytes : 0;
+  static constexpr int kStages = (227 * 1024 - 1024 - (int)sizeof(Shared) - kScaleBytes - kOutBytes) / kStageBytes;
+  static constexpr int kSmem = 1024 + kStages * kStageBytes + kScaleBytes + kOutBytes + (int)sizeof(Shared);
+  static_assert(kStages >= 3 && kStages <= 8, "barriers");
 };
 
 struct Args {
@@ -112,12 +115,57 @@ __device__ __forceinline__ float4 ld_shared_f4(unsigned saddr) {
   asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(saddr) : "memory");
   return v;
 }
+__device__ __forceinline__ uint4 ld_shared16(unsigned saddr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(saddr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void st_shared16(unsigned saddr, const uint4& v) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(saddr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
 __device__ __forceinline__ float ld_shared_f(unsigned saddr) {
   float v;
   asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(saddr) : "memory");
   return v;
 }
 __device__ __forceinline__ void st_shared_f(unsigned saddr, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(saddr), "f"(v) : "memory"); }
+__device__ __forceinline__ bool try_at(unsigned saddr, unsigned parity) {
+  unsigned ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(saddr), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+// what a wait was for cannot be used before it
+__device__ __forceinline__ void loaded(unsigned (&r)[16]) {
+  asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]),
+               "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]));
+}
+__device__ __forceinline__ void loaded(unsigned (&r)[32]) {
+  loaded(reinterpret_cast<unsigned(&)[16]>(r[0]));
+  loaded(reinterpret_cast<unsigned(&)[16]>(r[16]));
+}
+// The same wait for a whole warp, of which all lanes get the same answer; short where the barrier's phase is over.
+__device__ __noinline__ bool wait_longer(unsigned saddr, unsigned parity, volatile int* dead) {
+  const unsigned long long start = gtime_ns();
+  for (;;) {
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+      if (__all_sync(0xffffffffu, try_at(saddr, parity))) return true;
+    if (__any_sync(0xffffffffu, *dead)) return false;
+    if (__any_sync(0xffffffffu, gtime_ns() - start > kWaitNs)) {
+      *dead = 1;
+      return false;
+    }
+  }
+}
+__device__ __forceinline__ bool warp_wait(unsigned saddr, unsigned parity, volatile int* dead) {
+  return __all_sync(0xffffffffu, try_at(saddr, parity)) || wait_longer(saddr, parity, dead);
+}
 __device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
 template <class E> __device__ __forceinline__ E rounded(float v);
@@ -134,12 +182,13 @@ __device__ __forceinline__ void with_type(int dtype, void* out, F f) {
 
 template <bool kTall, bool kSwiglu>
 __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __grid_constant__ Args a) {
-  using S = Shape<kTall>;
+  using S = Shape<kTall, kSwiglu>;
   constexpr bool kPair = kTall;
   extern __shared__ unsigned char raw[];
   unsigned char* stages = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   float* ring = reinterpret_cast<float*>(stages + S::kStages * S::kStageBytes);
-  Shared& s = *reinterpret_cast<Shared*>(reinterpret_cast<unsigned char*>(ring) + S::kScaleBytes);
+  unsigned char* turned = reinterpret_cast<unsigned char*>(ring) + S::kScaleBytes;
+  Shared& s = *reinterpret_cast<Shared*>(turned + S::kOutBytes);
   const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
   constexpr int kStep = kSwiglu ? 128 : 256;                       // output columns of a tile
   const unsigned rank = kPair ? cluster_ctarank() : 0u;
@@ -151,9 +200,9 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
       mbar_init(&s.full[i], S::kCtas);
       mbar_init(&s.empty[i], 1);
     }
-    for (int i = 0; i < S::kParts; ++i) {
+    for (int i = 0; i < 4; ++i) {
       mbar_init(&s.part_full[i], 1);
-      mbar_init(&s.part_empty[i], 8 * S::kCtas);
+      mbar_init(&s.part_empty[i], 8 / S::kHalves * S::kCtas);
     }
     for (int i = 0; i < kQuads; ++i) {
       mbar_init(&s.scales_full[i], kScaleThreads / 32);
@@ -186,69 +235,99 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
   const int n_tiles = uniform(s.first_tile[a.E]);
 
   if (warp < kTmaWarp) {
-    if (kTall) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    if (kTall) asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
     const int quarter = warp & 3, half = warp >> 2;
     const unsigned lanes = tmem + ((unsigned)quarter << 21);       // this warp's 32 TMEM lanes
+    const unsigned first = kTall ? S::kParts * half : 0;            // buffer of this warp's partials
+    const unsigned full0 = smem_u32(&s.part_full[first]), empty0 = kPair ? map_to_cta(&s.part_empty[first], 0) : smem_u32(&s.part_empty[first]);
+    const unsigned ring0 = smem_u32(ring), ring_full = smem_u32(&s.scales_full[0]);
     unsigned part = 0, place = 0;  // partials, places in the ring so far
     unsigned turn = 0;             // exchanges of maxima so far
     bool ok = true;
+    const auto next_partial = [&] {                                 // -> its address
+      const unsigned buf = part % S::kParts;
+      if (ok) ok = warp_wait(full0 + 8 * buf, (part / S::kParts) & 1, &s.dead);
+      tc_fence_after();
+      return lanes + (first + buf) * 128;
+    };
+    const auto hand_back = [&] {                                    // the warp has what it loads of the partial
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_relaxed(empty0 + 8 * (part % S::kParts));
+      ++part;
+    };
+    const auto next_scales = [&] {                                  // -> address of four blocks' scales: [block][half][row]
+      const unsigned at = place % kQuads;
+      if (ok) ok = warp_wait(ring_full + 8 * at, (place / kQuads) & 1, &s.dead);
+      return ring0 + at * (S::kScaleFloats * 4);
+    };
+    const auto scales_read = [&] {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&s.scales_empty[place % kQuads]);
+      ++place;
+    };
     for (int t = unit; t < n_tiles; t += n_units) {
       const Tile at = uniform(tile_at<S::kRows>(s, a.E, t, kStep));
-      const auto next_partial = [&] {
-        const unsigned buf = part % S::kParts;
-        if (ok) ok = __all_sync(0xffffffffu, wait(&s.part_full[buf], (part / S::kParts) & 1, &s.dead));
-        tc_fence_after();
-        return lanes + buf * S::kPartCols;
-      };
-      const auto hand_back = [&] {           // every lane has what it loads of the partial
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) {
-          if (kPair) mbar_arrive_relaxed(map_to_cta(&s.part_empty[part % S::kParts], 0));
-          else mbar_arrive(&s.part_empty[part % S::kParts]);
-        }
-        ++part;
-      };
-      const auto scales_at = [&](int b) {    // of block b: [half][row]
-        if (b % kQuad == 0 && ok) ok = __all_sync(0xffffffffu, wait(&s.scales_full[place % kQuads], (place / kQuads) & 1, &s.dead));
-        return smem_u32(ring + (place % kQuads) * S::kScaleFloats + (b % kQuad) * 2 * S::kMine);
-      };
-      const auto scales_read = [&](int b) {
-        if (b % kQuad != kQuad - 1 && b != a.blocks - 1) return;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&s.scales_empty[place % kQuads]);
-        ++place;
-      };
       if constexpr (kTall) {
         const int mine = 32 * quarter + lane, row = 128 * (int)rank + mine;
         const bool used = uniform(128 * (int)rank + 32 * quarter) < at.rows, valid = row < at.rows;
-        float acc[128];            // plain: the columns of this half; swiglu: 64 gate and 64 up columns
+        // Columns 0-63: 64 of the first 128 weight rows (swiglu: gate rows), 64-127: as many of the second (up rows); pairs of neighbours
+        unsigned long long sum[64];
 #pragma unroll
-        for (int i = 0; i < 128; ++i) acc[i] = 0.f;
-#pragma unroll 1
-        for (int b = 0; b < a.blocks; ++b) {
-          const unsigned sc = scales_at(b);
-          const unsigned from = next_partial();
-          if (!ok) break;
-          if (!used) {
-            hand_back();
-            scales_read(b);
-            continue;
+        for (int i = 0; i < 64; ++i) sum[i] = 0ull;
+        if (used) {
+          // 64 columns are on their way or being added at any time: a wait is for all loads before it, so there are two a block, and the next block's first
+          // loads go out between this one's last additions.  (Five waits a block, 16 and 32 columns at a time: gate/up of 65 536 rows 2 490 us for 2 120.)
+          unsigned v[2][32];
+          const auto add = [&](int c, unsigned long long m) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              sum[16 * c + j] = fma_f32x2(f32x2(__uint_as_float(v[c & 1][2 * j]), __uint_as_float(v[c & 1][2 * j + 1])), m, sum[16 * c + j]);
+          };
+          unsigned sc = next_scales() + 4 * mine, from = next_partial();
+          if (ok) {
+            tc_ld32(from, v[0]);
+            tc_ld32(from + 32, v[1]);
           }
-          const float s0 = ld_shared_f(sc + (kSwiglu ? 0 : half * 4 * S::kMine) + 4 * mine);
-          const float s1 = kSwiglu ? ld_shared_f(sc + 4 * S::kMine + 4 * mine) : s0;
-          scales_read(b);
-          unsigned p[2][32];
-          const auto col = [&](int c) { return from + (kSwiglu ? (c >> 1) * 128 + half * 64 + (c & 1) * 32 : half * 128 + c * 32); };
-          tc_ld32(col(0), p[0]);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
+#pragma unroll 1
+          for (int b = 0; b < a.blocks && ok; ++b) {
+            const float m0 = ld_shared_f(sc), m1 = ld_shared_f(sc + 4 * S::kMine);
+            sc += 8 * S::kMine;
+            const unsigned long long s0 = f32x2(m0, m0), s1 = f32x2(m1, m1);
+            const bool more = b < a.blocks - 1;
             tc_wait_ld();
-            if (c < 3) tc_ld32(col(c + 1), p[(c + 1) & 1]);
-            else hand_back();
-            const float m = c < 2 ? s0 : s1;
-#pragma unroll
-            for (int i = 0; i < 32; ++i) acc[32 * c + i] = fmaf(__uint_as_float(p[c & 1][i]), m, acc[32 * c + i]);
+            loaded(v[0]);
+            loaded(v[1]);
+            add(0, s0);
+            tc_ld32(from + 64, v[0]);
+            add(1, s0);
+            tc_ld32(from + 96, v[1]);
+            if (b % kQuad == kQuad - 1 || !more) {
+              scales_read();
+              if (more) sc = next_scales() + 4 * mine;
+            }
+            tc_wait_ld();
+            loaded(v[0]);
+            loaded(v[1]);
+            hand_back();
+            add(2, s1);
+            if (more) {
+              from = next_partial();
+              if (!ok) break;
+              tc_ld32(from, v[0]);
+            }
+            add(3, s1);
+            if (more) tc_ld32(from + 32, v[1]);
+          }
+        } else {                   // (no row of the tile: the hand-overs alone)
+#pragma unroll 1
+          for (int b = 0; b < a.blocks && ok; ++b) {
+            if (b % kQuad == 0) {
+              next_scales();
+              scales_read();
+            }
+            next_partial();
+            hand_back();
           }
         }
         if (!used) {
@@ -259,6 +338,13 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
           continue;
         }
         const size_t p = (size_t)at.row0 + row;
+        float acc[128];
+#pragma unroll
+        for (int i = 0; i < 64; ++i) {
+          const float2 two = f32x2_parts(sum[i]);
+          acc[2 * i] = two.x;
+          acc[2 * i + 1] = two.y;
+        }
         if constexpr (kSwiglu) {
           unsigned top = 0u;
 #pragma unroll
@@ -280,30 +366,48 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
             if (half == 0) a.out_scales[p * (a.I / kBlock) + at.n0 / kBlock] = scale;
           }
         } else {
-          const int col0 = at.n0 + 128 * half, cols = min(128, a.N - col0);
           if (!ok) {
 #pragma unroll
             for (int i = 0; i < 128; ++i) acc[i] = __uint_as_float(0x7fffffffu);
           }
-          if (valid)
-            with_type(a.dtype, a.out, [&](auto* out) {
-              using E = typename std::remove_pointer<decltype(out)>::type;
-              out += p * a.N + col0;
-              constexpr int kIn = 16 / (int)sizeof(E);
+          // A warp turns its 32 rows round in shared memory, 128 bytes of each at a time, so that its stores are 128 bytes of four rows.  (16 bytes of 32 rows a
+          // store: 4 000 clocks a tile.)
+          const unsigned own = smem_u32(turned + warp * kTurnBytes);
+          const int rows = min(32, at.rows - 128 * (int)rank - 32 * quarter);
+          with_type(a.dtype, a.out, [&](auto* out) {
+            using E = typename std::remove_pointer<decltype(out)>::type;
+            constexpr int kIn = 16 / (int)sizeof(E), kCols = 128 / (int)sizeof(E);
+            out += (size_t)(at.row0 + 128 * (int)rank + 32 * quarter) * a.N;
+#pragma unroll
+            for (int c = 0; c < 128 / kCols; ++c) {
+              const int col0 = at.n0 + 128 * (c * kCols / 64) + 64 * half + c * kCols % 64, cols = min(kCols, a.N - col0);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                uint4 v;
+#pragma unroll
+                for (int j = 0; j < kIn; ++j) reinterpret_cast<E*>(&v)[j] = rounded<E>(acc[c * kCols + i * kIn + j]);
+                st_shared16(own + lane * kTurnPitch + 16 * i, v);
+              }
+              __syncwarp();
               if (a.wide) {
 #pragma unroll
-                for (int i = 0; i < 128; i += kIn) {
-                  uint4 v;
-#pragma unroll
-                  for (int j = 0; j < kIn; ++j) reinterpret_cast<E*>(&v)[j] = rounded<E>(acc[i + j]);
-                  if (i < cols) *reinterpret_cast<uint4*>(out + i) = v;
+                for (int i = 0; i < 8; ++i) {
+                  const int r = 4 * i + lane / 8, at_col = lane % 8 * kIn;
+                  const uint4 v = ld_shared16(own + r * kTurnPitch + lane % 8 * 16);
+                  if (r < rows && at_col < cols) *reinterpret_cast<uint4*>(out + (size_t)r * a.N + col0 + at_col) = v;
                 }
               } else {
+#pragma unroll 4
+                for (int r = 0; r < rows; ++r) {
+                  const E* from = reinterpret_cast<const E*>(turned + warp * kTurnBytes + r * kTurnPitch);
 #pragma unroll
-                for (int i = 0; i < 128; ++i)
-                  if (i < cols) out[i] = rounded<E>(acc[i]);
+                  for (int i = lane; i < kCols; i += 32)
+                    if (i < cols) out[(size_t)r * a.N + col0 + i] = from[i];
+                }
               }
-            });
+              __syncwarp();
+            }
+          });
         }
       } else {
         // groups of 16 rows; plain: all of them, of the 128 weight rows of this half; swiglu: every other, gate and up
@@ -319,34 +423,42 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
             if (kSwiglu) acc[i][kSwiglu ? 1 : 0][j] = 0.f;
           }
 #pragma unroll 1
-        for (int b = 0; b < a.blocks; ++b) {
-          const unsigned sc = scales_at(b);
-          const unsigned from = next_partial();
-          if (!ok) break;
-          unsigned p[kGroups][kSwiglu ? 2 : 1][16];
+        for (int b0 = 0; b0 < a.blocks && ok; b0 += kQuad) {
+          unsigned sc = next_scales();
+#pragma unroll 1
+          for (int b = b0; b < min(b0 + kQuad, a.blocks); ++b, sc += 8 * S::kMine) {
+            const unsigned from = next_partial();
+            if (!ok) break;
+            unsigned p[kGroups][kSwiglu ? 2 : 1][16];
 #pragma unroll
-          for (int i = 0; i < kGroups; ++i)
-            if (group(i) < groups) {
-              tc_ld16(from + (kSwiglu ? 0 : half * S::kRows) + 16 * group(i), p[i][0]);
-              if (kSwiglu) tc_ld16(from + S::kRows + 16 * group(i), p[i][kSwiglu ? 1 : 0]);
+            for (int i = 0; i < kGroups; ++i)
+              if (group(i) < groups) {
+                tc_ld16(from + (kSwiglu ? 0 : half * S::kRows) + 16 * group(i), p[i][0]);
+                if (kSwiglu) tc_ld16(from + S::kRows + 16 * group(i), p[i][kSwiglu ? 1 : 0]);
+              }
+            tc_wait_ld();
+#pragma unroll
+            for (int i = 0; i < kGroups; ++i) {
+              loaded(p[i][0]);
+              if (kSwiglu) loaded(p[i][kSwiglu ? 1 : 0]);
             }
-          tc_wait_ld();
-          hand_back();
+            hand_back();
 #pragma unroll
-          for (int i = 0; i < kGroups; ++i)
-            if (group(i) < groups) {
+            for (int i = 0; i < kGroups; ++i)
+              if (group(i) < groups) {
 #pragma unroll
-              for (int h = 0; h < (kSwiglu ? 2 : 1); ++h)
+                for (int h = 0; h < (kSwiglu ? 2 : 1); ++h)
 #pragma unroll
-                for (int j = 0; j < 16; j += 4) {
-                  const float4 m = ld_shared_f4(sc + 4 * ((kSwiglu ? h : half) * S::kMine + 16 * group(i) + j));
-                  acc[i][h][j] = fmaf(__uint_as_float(p[i][h][j]), m.x, acc[i][h][j]);
-                  acc[i][h][j + 1] = fmaf(__uint_as_float(p[i][h][j + 1]), m.y, acc[i][h][j + 1]);
-                  acc[i][h][j + 2] = fmaf(__uint_as_float(p[i][h][j + 2]), m.z, acc[i][h][j + 2]);
-                  acc[i][h][j + 3] = fmaf(__uint_as_float(p[i][h][j + 3]), m.w, acc[i][h][j + 3]);
-                }
-            }
-          scales_read(b);
+                  for (int j = 0; j < 16; j += 4) {
+                    const float4 m = ld_shared_f4(sc + 4 * ((kSwiglu ? h : half) * S::kMine + 16 * group(i) + j));
+                    acc[i][h][j] = fmaf(__uint_as_float(p[i][h][j]), m.x, acc[i][h][j]);
+                    acc[i][h][j + 1] = fmaf(__uint_as_float(p[i][h][j + 1]), m.y, acc[i][h][j + 1]);
+                    acc[i][h][j + 2] = fmaf(__uint_as_float(p[i][h][j + 2]), m.z, acc[i][h][j + 2]);
+                    acc[i][h][j + 3] = fmaf(__uint_as_float(p[i][h][j + 3]), m.w, acc[i][h][j + 3]);
+                  }
+              }
+          }
+          scales_read();
         }
         const int n = at.n0 + (kSwiglu ? 0 : 128 * half) + 32 * quarter + lane;
         if constexpr (kSwiglu) {
@@ -409,7 +521,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
       }
     }
   } else {
-    if (kTall) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    if (kTall) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
     if (warp == kTmaWarp) {
       if (elect_one()) {
         unsigned n = 0;            // stages so far
@@ -452,25 +564,28 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
         bool ok = true;
         for (int t = unit; t < n_tiles && ok; t += n_units) {
           const Tile at = tile_at<S::kRows>(s, a.E, t, kStep);
-          const unsigned idesc = kTall ? idesc_of(256, 256) : idesc_of(128, (unsigned)(at.rows + 15) & ~15u);
+          const unsigned idesc = kTall ? idesc_of(256, 128) : idesc_of(128, (unsigned)(at.rows + 15) & ~15u);
 #pragma unroll 1
-          for (int i = 0; i < a.blocks; ++i, ++n) {
+          for (int i = 0; i < a.blocks && ok; ++i, ++n) {
             const unsigned slot = n % S::kStages, round = n / S::kStages, buf = n % S::kParts, use = n / S::kParts;
-            // (a pair's arrivals are relaxed: what they hand back is ordered by the tcgen05 fences on both sides)
-            if (use) ok = wait<kPair ? mbar_try_relaxed : mbar_try>(&s.part_empty[buf], (use - 1) & 1, &s.dead);
-            ok = ok && wait(&s.full[slot], round & 1, &s.dead);
-            if (!ok) break;
-            tc_fence_after();
-            const unsigned st = smem_u32(stages + slot * S::kStageBytes), d = tmem + buf * S::kPartCols;
-            const unsigned long long w = umma_desc(st, 128), x = umma_desc(st + S::kWBytes, 128);
-            if (kTall) {
-              mma_block<kPair>(d, x, w, idesc);
-            } else {
-              mma_block<kPair>(d, w, x, idesc);
-              mma_block<kPair>(d + S::kRows, umma_desc(st + 128 * kBlock, 128), x, idesc);
+            const unsigned st = smem_u32(stages + slot * S::kStageBytes);
+#pragma unroll
+            for (int h = 0; h < S::kHalves; ++h) {
+              // (a pair's arrivals are relaxed: what they hand back is ordered by the tcgen05 fences on both sides)
+              if (use) ok = ok && wait<kPair ? mbar_try_relaxed : mbar_try>(&s.part_empty[buf + S::kParts * h], (use - 1) & 1, &s.dead);
+              if (h == 0) ok = ok && wait(&s.full[slot], round & 1, &s.dead);
+              if (!ok) break;
+              tc_fence_after();
+              const unsigned d = tmem + (buf + S::kParts * h) * 128;
+              if (kTall) {
+                mma_block<kPair>(d, umma_desc(st + S::kWBytes, 128), umma_desc(st + h * 64 * kBlock, 128), idesc);
+              } else {
+                mma_block<kPair>(d, umma_desc(st, 128), umma_desc(st + S::kWBytes, 128), idesc);
+                mma_block<kPair>(d + S::kRows, umma_desc(st + 128 * kBlock, 128), umma_desc(st + S::kWBytes, 128), idesc);
+              }
+              if (h == S::kHalves - 1) commit(&s.empty[slot]);
+              commit(&s.part_full[buf + S::kParts * h]);
             }
-            commit(&s.empty[slot]);
-            commit(&s.part_full[buf]);
           }
         }
         commit(&s.drained);     // nothing of this block's is left in the tensor core when it frees its TMEM
@@ -550,7 +665,7 @@ bool encode(CUtensorMap* out, const void* base, int cols, int rows, int parts, i
 
 template <bool kTall, bool kSwiglu>
 cudaError_t product_launch(Args& a, const void* codes, const void* w_codes, int K, cudaStream_t stream) {
-  using S = Shape<kTall>;
+  using S = Shape<kTall, kSwiglu>;
   static_assert(S::kSmem <= 227 * 1024, "shared memory");
   const int parts = kSwiglu ? 2 : 1;
   // a CTA's weight rows: tall 128 (swiglu: gate or up rows), else 256 (128 of both)

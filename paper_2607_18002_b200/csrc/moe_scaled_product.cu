@@ -37,10 +37,17 @@ struct Shared : Segments {
   unsigned tops[2][2][128];      // swiglu: largest magnitudes on their way from warp to warp
 };
 
-template <bool kTall, bool kSwiglu>
+enum Form { kFew, kTile, kTilePair };
+template <Form kForm, bool kSwiglu>
 struct Shape {
-  static constexpr int kCtas = kTall ? 2 : 1;
-  static constexpr int kRows = kTall ? 256 : 64;                    // of a tile
+  static constexpr bool kTall = kForm != kFew;
+  static constexpr int kCtas = kForm == kTilePair ? 2 : 1;
+  static constexpr int kRows = kTall ? 128 * kCtas : 64;            // of a tile
+  // Tall: a half of the columns has 64 of the first 128 weight rows and 64 of the second; where one CTA has them all, and their order is free, its 128 rows
+  static constexpr bool kMixed = kForm == kTilePair || kSwiglu;
+  // weight rows and parts (gate, up) of a TMA box, boxes of a stage
+  static constexpr int kBoxWeights = kForm == kTilePair ? 128 : !kSwiglu ? 256 : kTall ? 64 : 128, kBoxParts = kSwiglu && kForm != kTilePair ? 2 : 1;
+  static constexpr int kBoxes = kForm == kTile && kSwiglu ? 2 : 1;
   static constexpr int kMine = kRows / kCtas;                       // ... in this CTA
   static constexpr int kWBytes = 256 / kCtas * kBlock, kXBytes = kMine * kBlock, kStageBytes = kWBytes + kXBytes;
   static constexpr int kBoxRows = kTall ? 64 : 32;                  // of a TMA box of rows
@@ -180,10 +187,10 @@ __device__ __forceinline__ void with_type(int dtype, void* out, F f) {
   else f(static_cast<float*>(out));
 }
 
-template <bool kTall, bool kSwiglu>
+template <Form kForm, bool kSwiglu>
 __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __grid_constant__ Args a) {
-  using S = Shape<kTall, kSwiglu>;
-  constexpr bool kPair = kTall;
+  using S = Shape<kForm, kSwiglu>;
+  constexpr bool kTall = S::kTall, kPair = kForm == kTilePair;
   extern __shared__ unsigned char raw[];
   unsigned char* stages = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   float* ring = reinterpret_cast<float*>(stages + S::kStages * S::kStageBytes);
@@ -271,7 +278,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
       if constexpr (kTall) {
         const int mine = 32 * quarter + lane, row = 128 * (int)rank + mine;
         const bool used = uniform(128 * (int)rank + 32 * quarter) < at.rows, valid = row < at.rows;
-        // Columns 0-63: 64 of the first 128 weight rows (swiglu: gate rows), 64-127: as many of the second (up rows); pairs of neighbours
+        // Pairs of neighbouring columns, of this half.  kMixed: 0-63 are of the first 128 weight rows (swiglu: gate rows), 64-127 of the second (up rows)
         unsigned long long sum[64];
 #pragma unroll
         for (int i = 0; i < 64; ++i) sum[i] = 0ull;
@@ -291,7 +298,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
           }
 #pragma unroll 1
           for (int b = 0; b < a.blocks && ok; ++b) {
-            const float m0 = ld_shared_f(sc), m1 = ld_shared_f(sc + 4 * S::kMine);
+            const float m0 = ld_shared_f(sc + (S::kMixed ? 0 : half * 4 * S::kMine)), m1 = S::kMixed ? ld_shared_f(sc + 4 * S::kMine) : m0;
             sc += 8 * S::kMine;
             const unsigned long long s0 = f32x2(m0, m0), s1 = f32x2(m1, m1);
             const bool more = b < a.blocks - 1;
@@ -380,7 +387,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
             out += (size_t)(at.row0 + 128 * (int)rank + 32 * quarter) * a.N;
 #pragma unroll
             for (int c = 0; c < 128 / kCols; ++c) {
-              const int col0 = at.n0 + 128 * (c * kCols / 64) + 64 * half + c * kCols % 64, cols = min(kCols, a.N - col0);
+              const int col0 = at.n0 + (S::kMixed ? 128 * (c * kCols / 64) + 64 * half + c * kCols % 64 : 128 * half + c * kCols), cols = min(kCols, a.N - col0);
 #pragma unroll
               for (int i = 0; i < 8; ++i) {
                 uint4 v;
@@ -530,7 +537,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
           const int row0 = at.row0 + (int)rank * S::kMine, mine = min(S::kMine, at.rows - (int)rank * S::kMine);
           const int boxes = mine > 0 ? (mine + S::kBoxRows - 1) / S::kBoxRows : 0;
           const unsigned long long policy = at.alone ? l2_evict_first() : l2_evict_normal();
-          const int n0 = at.n0 + (kSwiglu ? 0 : 128 * (int)rank), which = kSwiglu ? (int)rank : 0;
+          const int n0 = at.n0 + (kSwiglu ? 0 : 128 * (int)rank), which = kSwiglu ? (int)rank : 0;      // (rank is 0 where there is no pair)
 #pragma unroll 1
           for (int i = 0; i < a.blocks; ++i, ++n) {
             const unsigned slot = n % S::kStages, round = n / S::kStages;
@@ -538,7 +545,9 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
             const unsigned to = smem_u32(stages + slot * S::kStageBytes);
             const unsigned bar = kPair ? map_to_cta(&s.full[slot], 0) : smem_u32(&s.full[slot]);
             expect_tx(bar, S::kWBytes + boxes * S::kBoxRows * kBlock);
-            tma_4d<kPair>(to, &a.tm_w, i * kBlock, n0, which, at.expert, bar, policy);
+#pragma unroll
+            for (int x = 0; x < S::kBoxes; ++x)
+              tma_4d<kPair>(to + x * (S::kWBytes / S::kBoxes), &a.tm_w, i * kBlock, n0 + x * S::kBoxWeights, which, at.expert, bar, policy);
 #pragma unroll 1
             for (int x = 0; x < boxes; ++x)
               tma_2d<kPair>(to + S::kWBytes + x * S::kBoxRows * kBlock, &a.tm_x, i * kBlock, row0 + x * S::kBoxRows, bar);
@@ -564,7 +573,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
         bool ok = true;
         for (int t = unit; t < n_tiles && ok; t += n_units) {
           const Tile at = tile_at<S::kRows>(s, a.E, t, kStep);
-          const unsigned idesc = kTall ? idesc_of(256, 128) : idesc_of(128, (unsigned)(at.rows + 15) & ~15u);
+          const unsigned idesc = kTall ? idesc_of(128 * S::kCtas, 128) : idesc_of(128, (unsigned)(at.rows + 15) & ~15u);
 #pragma unroll 1
           for (int i = 0; i < a.blocks && ok; ++i, ++n) {
             const unsigned slot = n % S::kStages, round = n / S::kStages, buf = n % S::kParts, use = n / S::kParts;
@@ -578,7 +587,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
               tc_fence_after();
               const unsigned d = tmem + (buf + S::kParts * h) * 128;
               if (kTall) {
-                mma_block<kPair>(d, umma_desc(st + S::kWBytes, 128), umma_desc(st + h * 64 * kBlock, 128), idesc);
+                mma_block<kPair>(d, umma_desc(st + S::kWBytes, 128), umma_desc(st + h * (S::kWBytes / 2), 128), idesc);
               } else {
                 mma_block<kPair>(d, umma_desc(st, 128), umma_desc(st + S::kWBytes, 128), idesc);
                 mma_block<kPair>(d + S::kRows, umma_desc(st + 128 * kBlock, 128), umma_desc(st + S::kWBytes, 128), idesc);
@@ -663,16 +672,15 @@ bool encode(CUtensorMap* out, const void* base, int cols, int rows, int parts, i
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool kTall, bool kSwiglu>
+template <Form kForm, bool kSwiglu>
 cudaError_t product_launch(Args& a, const void* codes, const void* w_codes, int K, cudaStream_t stream) {
-  using S = Shape<kTall, kSwiglu>;
+  using S = Shape<kForm, kSwiglu>;
   static_assert(S::kSmem <= 227 * 1024, "shared memory");
   const int parts = kSwiglu ? 2 : 1;
-  // a CTA's weight rows: tall 128 (swiglu: gate or up rows), else 256 (128 of both)
-  if (!encode(&a.tm_w, w_codes, K, a.N / parts, parts, a.E, kTall || kSwiglu ? 128 : 256, kTall ? 1 : parts) ||
+  if (!encode(&a.tm_w, w_codes, K, a.N / parts, parts, a.E, S::kBoxWeights, S::kBoxParts) ||
       !encode(&a.tm_x, codes, K, a.R, 0, 0, S::kBoxRows, 0))
     return cudaErrorInvalidValue;
-  auto* kernel = scaled_product_kernel<kTall, kSwiglu>;
+  auto* kernel = scaled_product_kernel<kForm, kSwiglu>;
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
@@ -726,8 +734,10 @@ int product(const void* codes, const float* scales, const void* w_codes, const f
   a.wide_scales = a.blocks % 4 == 0 && ((address(scales) | address(w_scales)) & 15) == 0;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   // The form goes by the rows that an expert gets on average; the host does not know more.
-  const bool tall = n_rows > 64ll * n_experts;
-  const cudaError_t e = tall ? product_launch<true, kSwiglu>(a, codes, w_codes, K, st) : product_launch<false, kSwiglu>(a, codes, w_codes, K, st);
+  const long long per = n_rows / n_experts;
+  const cudaError_t e = per <= 64    ? product_launch<kFew, kSwiglu>(a, codes, w_codes, K, st)
+                        : per <= 256 ? product_launch<kTile, kSwiglu>(a, codes, w_codes, K, st)
+                                     : product_launch<kTilePair, kSwiglu>(a, codes, w_codes, K, st);
   return e == cudaSuccess ? MOE_OK : MOE_ECUDA;
 }
 

@@ -735,8 +735,8 @@ int product(const void* codes, const float* scales, const void* w_codes, const f
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   // The form goes by the rows that an expert gets on average; the host does not know more.
   const long long per = n_rows / n_experts;
-  const cudaError_t e = per <= 64    ? product_launch<kFew, kSwiglu>(a, codes, w_codes, K, st)
-                        : per <= 256 ? product_launch<kTile, kSwiglu>(a, codes, w_codes, K, st)
+  const cudaError_t e = per <= 32    ? product_launch<kFew, kSwiglu>(a, codes, w_codes, K, st)
+                        : per <= 384 ? product_launch<kTile, kSwiglu>(a, codes, w_codes, K, st)
                                      : product_launch<kTilePair, kSwiglu>(a, codes, w_codes, K, st);
   return e == cudaSuccess ? MOE_OK : MOE_ECUDA;
 }

@@ -4,11 +4,13 @@
 //   s_e = softmax(z)_e  or  1 / (1 + exp(-z_e));   c_e = s_e + bias_e;   value of a group: the sum of its one or two largest c
 //   the top_groups groups of largest value are kept; the k largest c of their experts are chosen;   w_j = scale s_j  (/ sum_i s_i)
 //
-// Who is chosen is decided as in 64 bits.  c is computed in fp32 with a bound on its error, and where two candidates whose order matters lie closer
-// than that (and are not equal by their inputs) the warp does the token again in fp64: one token of some hundreds.  Without a bias the order is
-// that of the logits, which needs no bound.  (All of it in fp64 would be 480 double operations a lane and token: 14 us for 16 384 tokens of 256 experts.)
+// Who is chosen is decided as in 64 bits.  c is computed in fp32 with a bound on its error, and where two candidates whose order matters lie closer than that
+// (and are not equal by their inputs) those few are put in order by their values in fp64: one token of some hundreds.  (All of it in fp64 would be 480 double
+// operations a lane and token: 14 us for 16 384 tokens of 256 experts.)
 //
-// One warp per token, its logits over the lanes' registers as order-preserving keys.  Equal values go to the lower index, as everywhere.
+// One warp per token.  A lane sorts its own values once, as integers of the same order whose last bits say which of its experts it is (what they displace counts as
+// an error of c like the others); then a pick is one maximum over the warp, one minimum over the ids that have it, and the winner's list moves up.
+// Bound by instruction issue: 16 384 tokens of 256 experts, eight of four of eight groups: see DESIGN's figures.
 #include <cuda_fp16.h>
 
 #include "moe_dev.cuh"
@@ -30,18 +32,19 @@ struct ChooseArgs {
   float* w;
 };
 
-// unsigned order = float order (-0 counts as +0), NaN above every number; 0 is below everything: "no candidate"
-__device__ __forceinline__ unsigned key_of(float v) {
-  if (v != v) return kAll;
-  const unsigned u = __float_as_uint(v + 0.0f);
-  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-}
-__device__ __forceinline__ float of_key(unsigned key) { return __uint_as_float((key & 0x80000000u) ? (key & 0x7fffffffu) : ~key); }
+// unsigned order = double order (-0 counts as +0), NaN above every number; 0 is below everything: "no candidate"
 __device__ __forceinline__ unsigned long long key_of(double v) {
   if (v != v) return ~0ull;
   const unsigned long long u = __double_as_longlong(v + 0.0);
   return (u >> 63) ? ~u : (u | 1ull << 63);
 }
+// signed order = float order (not of NaN); kNone is below everything
+constexpr int kNone = (int)0x80000000;
+__device__ __forceinline__ int key_of(float v) {
+  const int u = __float_as_int(v + 0.0f);
+  return u ^ ((u >> 31) & 0x7fffffff);
+}
+__device__ __forceinline__ float of_key(int key) { return __int_as_float(key ^ ((key >> 31) & 0x7fffffff)); }
 
 __device__ __forceinline__ float as_float(float v) { return v; }
 __device__ __forceinline__ float as_float(__half v) { return __half2float(v); }
@@ -105,6 +108,27 @@ __device__ __forceinline__ F warp_sum(F v) {
   return v;
 }
 
+__device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.f, 1.f + expf(-z)); }
+// of the weights: a score relative to that of a logit `shift` (softmax: the largest of the chosen; sigmoid(z) = exp(z) / (1 + exp(z)): the same where it is
+// negative, else 0), so that scores that are tiny alike have weights
+__device__ __forceinline__ float relative_score(float z, float shift, bool is_sigmoid) {
+  if (z == -INFINITY) return 0.f;
+  return is_sigmoid ? __fdividef(expf(fminf(z, 0.f) - shift), 1.f + expf(-fabsf(z))) : expf(z - shift);
+}
+__device__ __forceinline__ double sigmoid(double z) { return 1.0 / (1.0 + exp(-z)); }
+
+// The same to some steps of fp32, for the comparison of experts: exp through 2^x (its argument rounded: |x| halves of a step of 2^-23, the power two), the
+// reciprocal one.
+__device__ __forceinline__ float quick_exp(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x * 1.4426950408889634f));
+  return r;
+}
+__device__ __forceinline__ float quick_sigmoid(float z) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + quick_exp(-z)));
+  return r;
+}
 // Of a softmax: the largest logit (0 where there is none above -inf, so that exp gives 0), and 1 over the sum (0 for such a row, NaN for one with NaN or
 // +inf)
 struct Norm {
@@ -118,20 +142,17 @@ __device__ __forceinline__ Norm norm_of(const float (&z)[kPer]) {
   m = warp_max(m);
   if (m == -INFINITY) m = 0.f;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) sum += expf(z[i] - m);
+  for (int i = 0; i < kPer; ++i) sum += quick_exp(z[i] - m);
   sum = warp_sum(sum);
   return Norm{m, sum == 0.f ? 0.f : 1.f / sum};
 }
-__device__ __forceinline__ float sigmoid(float z) { return 1.f / (1.f + expf(-z)); }
-__device__ __forceinline__ double sigmoid(double z) { return 1.0 / (1.0 + exp(-z)); }
-
-// Bounds on the error of a score and its sum with a bias, in units of 2^-23: exp is off by two steps of 2^-23 at most, the quotient and each addition by half
-// of one, a softmax's sum by 13 additions and its terms by the rounding of z - top besides: s |z - top| / 2 <= 0.2 s_top; what sigmoid loses below
-// 2^-126 is less than 2^-120.  6 and 25 times the score are about twice that.
-__device__ __forceinline__ float error_of(float s, float c, float z, float top, bool is_sigmoid) {
-  return ldexpf(s * (is_sigmoid ? 6.f : 24.f + fabsf(z - top)) + fabsf(c), -23) + 0x1p-120f;
+// Bounds on the error of a quick score and of its sum with a bias, in steps of 2^-23.  exp(x): 2 + 0.8 |x| (softmax: 1.3 |x|, x itself is rounded); sigmoid: 1.5 for the
+// addition and the reciprocal; softmax: the sum's 13 additions, its terms' errors (|x| weighted by their share is ln E at most) and the quotient, 15.  Of any score, where
+// s |x| counts less than 1.  What is lost below 2^-126 is less than 2^-120.
+__device__ __forceinline__ float error_of(float s, float c, float far, bool is_sigmoid) {
+  return ldexpf(s * (is_sigmoid ? 6.f + far : 25.f + 2.f * far) + fabsf(c), -23) + 0x1p-120f;
 }
-__device__ __forceinline__ float error_of_any(float c, bool is_sigmoid) { return ldexpf((is_sigmoid ? 6.f : 25.f) + fabsf(c), -23); }
+__device__ __forceinline__ float error_of_any(float c) { return ldexpf(26.f + fabsf(c), -23); }
 
 // The same in fp64, by the whole warp: rare.  Lane j < k gets the j-th expert.
 template <class L, int kPer, bool kVec>
@@ -232,153 +253,304 @@ __device__ __noinline__ int choose_slowly(const ChooseArgs& a, const L* row, int
   return mine;
 }
 
-// Which groups are kept, as a bit mask; close: whether fp32 cannot tell.  c: the warp's values by expert, in shared memory.
-// Several neighbouring lanes have a group: each goes over a part of it, then the two largest are joined.
-__device__ __forceinline__ unsigned keep_groups(const ChooseArgs& a, const float* c, int lane, bool& close) {
+__device__ __forceinline__ int warp_max_key(float v) { return __reduce_max_sync(kAll, key_of(v)); }
+
+// The two largest of a group, on their way over its values
+template <class V>
+struct Two {
+  V one = -INFINITY, two = -INFINITY;
+  __device__ __forceinline__ void join(V o1, V o2) {
+    two = fmax(fmin(one, o1), fmax(two, o2));
+    one = fmax(one, o1);
+  }
+  __device__ __forceinline__ V value(const ChooseArgs& a, int size) const { return a.group_sum > 1 && size > 1 ? one + two : one; }
+  // (a group of one expert, or one that holds -inf, has no second value that counts)
+  __device__ __forceinline__ float error(V v) const {
+    return one == -INFINITY ? 0.f : error_of_any(one) + (two == -INFINITY ? 0.f : error_of_any(two) + ldexpf(fabsf(v), -23));
+  }
+};
+// whether fp32 cannot tell which groups are kept: the least of those inside, the largest of those outside, the largest error
+__device__ __forceinline__ bool groups_close(bool any, bool inside, float in, bool outside, float out, float err) {
+  const float low = -of_key(warp_max_key(any && inside ? -in : -INFINITY)), high = of_key(warp_max_key(any && outside ? out : -INFINITY));
+  return !(low - high > 2.f * of_key(warp_max_key(any ? err : 0.f)));
+}
+
+// Which groups are kept, as a bit mask; c(e): an expert's value; for groups of any size.  Several neighbouring lanes have a group: each goes over a part of it, then the two
+// largest are joined.
+template <class V, class F>
+__device__ __forceinline__ unsigned keep_groups(const ChooseArgs& a, F c, int lane, bool& close) {
   const int size = a.E / a.groups;
   int per = 1;                          // lanes a group: a power of two
   while (2 * per * a.groups <= 32 && 2 * per <= size) per *= 2;
   const int g = lane / per, q = lane % per;
-  float one = -INFINITY, two = -INFINITY;
+  Two<V> best;
   if (g < a.groups) {
-    const int n = (size - q + per - 1) / per;
-    int at = g % n;                     // (groups start at different places: other banks)
-    for (int i = 0; i < n; ++i) {
-      const float v = c[g * size + q + per * at];
-      if (++at == n) at = 0;
-      if (key_of(v) > key_of(one)) {
-        two = one;
-        one = v;
-      } else if (key_of(v) > key_of(two)) {
-        two = v;
-      }
-    }
+#pragma unroll 1
+    for (int i = q; i < size; i += per) best.join(c(g * size + i), -INFINITY);
   }
   for (int b = per / 2; b >= 1; b >>= 1) {
-    const float o1 = __shfl_xor_sync(kAll, one, b), o2 = __shfl_xor_sync(kAll, two, b);
-    const bool mine = key_of(one) >= key_of(o1);
-    const float less = mine ? o1 : one, next = mine ? two : o2;
-    one = mine ? one : o1;
-    two = key_of(less) > key_of(next) ? less : next;
+    const V o1 = __shfl_xor_sync(kAll, best.one, b), o2 = __shfl_xor_sync(kAll, best.two, b);
+    best.join(o1, o2);
   }
-  const float value = a.group_sum > 1 && size > 1 ? one + two : one;
+  const V value = best.value(a, size);
   const bool mine = g < a.groups && q == 0;
   int before = 0;
+#pragma unroll 1
   for (int o = 0; o < a.groups; ++o) {
-    const unsigned other = key_of(__shfl_sync(kAll, value, o * per));
-    before += other > key_of(value) || (other == key_of(value) && o < g);
+    const V other = __shfl_sync(kAll, value, o * per);
+    before += other > value || (other == value && o < g);
   }
-  unsigned kept = 0;
-  const unsigned last = __ballot_sync(kAll, mine && before == a.top_groups - 1), next = __ballot_sync(kAll, mine && before == a.top_groups);
-  const float in = __shfl_sync(kAll, value, __ffs(last) - 1), out = __shfl_sync(kAll, value, __ffs(next) - 1);
-  // (a group of one expert, or one that holds -inf, has no second value that counts)
-  const float err = !mine ? 0.f : error_of_any(one, a.sigmoid) + (two == -INFINITY ? 0.f : error_of_any(two, a.sigmoid) + ldexpf(fabsf(value), -23));
-  close = !(in - out > 2.f * warp_max(err));
+  close = sizeof(V) == 4 && groups_close(mine, before < a.top_groups, value, before >= a.top_groups, value, best.error(value));
   const unsigned firsts = __ballot_sync(kAll, mine && before < a.top_groups);
+  unsigned kept = 0;
   for (int o = 0; o < a.groups; ++o) kept |= (firsts >> (o * per) & 1u) << o;
   return kept;
+}
+// ... by their values in fp64
+template <class L>
+__device__ __noinline__ unsigned keep_groups_exactly(const ChooseArgs& a, const L* row, double top, int lane) {
+  double sum = 0.0;
+  if (!a.sigmoid) {
+#pragma unroll 1
+    for (int e = lane; e < a.E; e += 32) sum += exp((double)as_float(row[e]) - top);
+    sum = warp_sum(sum);
+  }
+  bool close;
+  return keep_groups<double>(a, [&](int e) {
+    const double z = as_float(row[e]);
+    return (a.sigmoid ? sigmoid(z) : sum == 0.0 ? 0.0 : exp(z - top) / sum) + (a.bias ? (double)a.bias[e] : 0.0);
+  }, lane, close);
+}
+// The same where a lane's four neighbours are of one group and a group's lanes are a power of two.  Values become keys with the group in their last five bits, one a lane;
+// the last of top_groups maxima over the warp says who is kept.
+template <int kPer>
+__device__ __forceinline__ unsigned keep_groups(const ChooseArgs& a, const float (&c)[kPer], int lane, bool& close) {
+  const int size = a.E / a.groups, lanes = size / 4, shift = 31 - __clz(lanes);          // lanes of a group; 32 >> shift groups in 128 experts
+  float value = -INFINITY, err = 0.f;
+#pragma unroll
+  for (int q = 0; q < kPer / 4; ++q) {
+    const float h1 = fmaxf(c[4 * q], c[4 * q + 1]), l1 = fminf(c[4 * q], c[4 * q + 1]), h2 = fmaxf(c[4 * q + 2], c[4 * q + 3]), l2 = fminf(c[4 * q + 2], c[4 * q + 3]);
+    Two<float> best;
+    best.one = h1;
+    best.two = l1;
+    best.join(h2, l2);
+    for (int b = 1; b < lanes; b <<= 1) {
+      const float o1 = __shfl_xor_sync(kAll, best.one, b), o2 = __shfl_xor_sync(kAll, best.two, b);
+      best.join(o1, o2);
+    }
+    const float mine = best.value(a, size);
+    err = fmaxf(err, best.error(mine));
+    const float v = __shfl_sync(kAll, mine, lane << shift & 31);
+    if (lane >> (5 - shift) == q) value = v;
+  }
+  int key = lane < a.groups ? (key_of(value) & ~31) | (31 - lane) : kNone, last = 0;
+  bool kept = false;
+  for (int j = 0; j < a.top_groups; ++j) {
+    last = __reduce_max_sync(kAll, key);
+    if (key == last) {
+      kept = true;
+      key = kNone;
+    }
+  }
+  const int next = __reduce_max_sync(kAll, key);
+  const float in = of_key(last & ~31), out = of_key(next | 31);
+  close = !(in - out > 2.f * __int_as_float(__reduce_max_sync(kAll, __float_as_int(err))));
+  return __ballot_sync(kAll, kept);
+}
+
+// descending, by compare-exchanges of the largest first
+template <int kN>
+__device__ __forceinline__ void sort_down(int (&v)[kN]) {
+  const auto order = [&](int i, int j) {
+    const int hi = max(v[i], v[j]), lo = min(v[i], v[j]);
+    v[i] = hi;
+    v[j] = lo;
+  };
+  if (kN == 4) {
+    order(0, 1); order(2, 3); order(0, 2); order(1, 3); order(1, 2);
+  } else {                              // Batcher's merge exchange for eight
+    order(0, 4); order(1, 5); order(2, 6); order(3, 7);
+    order(0, 2); order(1, 3); order(4, 6); order(5, 7);
+    order(2, 4); order(3, 5); order(0, 1); order(2, 3); order(4, 5); order(6, 7);
+    order(1, 4); order(3, 6);
+    order(1, 2); order(3, 4); order(5, 6);
+  }
 }
 
 template <class L, int kPer, bool kVec>
 __global__ void __launch_bounds__(kWarps * 32) choose_kernel(const __grid_constant__ ChooseArgs a) {
-  __shared__ float by_expert[kWarps][kPer * 32];
+  constexpr int kList = kPer < 8 ? kPer : 8, kLists = kPer / kList, kWhich = kPer - 1;
+  __shared__ union {
+    float by_expert[kPer * 32];
+    int4 sorted[kLists][32][kList / 4];
+  } space[kWarps];
+  __shared__ int2 picks[kWarps][kMaxK];            // key and lane
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int t = blockIdx.x * kWarps + warp;
   grid_dep_wait();
   if (t >= a.T) return;
   const L* row = static_cast<const L*>(a.logits) + (size_t)t * a.stride;
-  const bool grouped = a.top_groups < a.groups;
+  const bool grouped = a.top_groups < a.groups, scored = a.bias || grouped;
+  constexpr int kInf = 0x7f800000;                 // the key of infinity: those of NaN, which key_of makes positive, are above it
   Norm norm{0.f, 0.f};
-  unsigned key[kPer];
-  bool close = false;
+  int key[kLists][kList];
+  bool slow = false;
   {
-    float z[kPer];
+    float z[kPer], c[kPer];
     load_row<L, kPer, kVec>(row, a.E, lane, z);
-    if (!a.sigmoid && (a.bias || grouped || !a.renormalize)) norm = norm_of<kPer>(z);
-    if (a.bias || grouped) {
+    if (!a.sigmoid && (scored || !a.renormalize)) {
+      norm = norm_of<kPer>(z);
+      slow = norm.inv != norm.inv;
+    }
+    if (scored) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+        c[i] = expert_of<kVec>(i, lane) < a.E ? a.sigmoid ? quick_sigmoid(z[i]) : quick_exp(z[i] - norm.top) * norm.inv : -INFINITY;
+      if (a.bias) {
+        load_row<float, kPer, kVec>(a.bias, a.E, lane, z);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) z[i] = c[i] += z[i];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) key[i / kList][i % kList] = expert_of<kVec>(i, lane) < a.E ? (key_of(z[i]) & ~kWhich) | (kWhich - i) : kNone;
+    if (grouped) {
+      int top = kNone;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) top = max(top, key[i / kList][i % kList]);
+      slow |= __any_sync(kAll, top > (kInf | kWhich));
+      const int size = a.E / a.groups;
+      bool close;
+      unsigned groups;
+      if (kVec && size % 4 == 0 && size <= 128 && (size & (size - 1)) == 0) {
+        groups = keep_groups<kPer>(a, c, lane, close);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+          if (expert_of<kVec>(i, lane) < a.E) space[warp].by_expert[expert_of<kVec>(i, lane)] = c[i];
+        __syncwarp();
+        groups = keep_groups<float>(a, [&](int e) { return space[warp].by_expert[e]; }, lane, close);
+        __syncwarp();
+      }
+      if (close && !slow) groups = keep_groups_exactly(a, row, (double)norm.top, lane);
+      const unsigned inverse = ((1u << 20) + size - 1) / size;      // e / size = e inverse >> 20 for e < 2^10
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
-        const int e = expert_of<kVec>(i, lane);
-        float c = -INFINITY;
-        if (e < a.E) {
-          c = a.sigmoid ? sigmoid(z[i]) : expf(z[i] - norm.top) * norm.inv;
-          if (a.bias) c += a.bias[e];
+        if (kVec && i % 4 && size % 4 == 0) continue;      // (four neighbours at once)
+        if (!(groups >> (((unsigned)expert_of<kVec>(i, lane) * inverse >> 20) & 31) & 1)) {
+          key[i / kList][i % kList] = kNone;
+          if (kVec && size % 4 == 0) key[i / kList][i % kList + 1] = key[i / kList][i % kList + 2] = key[i / kList][i % kList + 3] = kNone;
         }
-        if (grouped && e < a.E) by_expert[warp][e] = c;
-        key[i] = e < a.E ? key_of(a.bias ? c : z[i]) : 0u;
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) key[i] = expert_of<kVec>(i, lane) < a.E ? key_of(z[i]) : 0u;
     }
   }
-  if (grouped) {
+  int my_id = 0, pos = lane;            // the expert of this lane's slot, and which slot it is
+  if (!slow) {
+    int head[kLists], at[kLists];
+#pragma unroll
+    for (int l = 0; l < kLists; ++l) {
+      sort_down<kList>(key[l]);
+#pragma unroll
+      for (int i = 0; i < kList; i += 4) space[warp].sorted[l][lane][i / 4] = make_int4(key[l][i], key[l][i + 1], key[l][i + 2], key[l][i + 3]);
+      head[l] = key[l][0];
+      at[l] = 0;
+    }
+    const auto best = [&] {
+      int b = head[0];
+#pragma unroll
+      for (int l = 1; l < kLists; ++l) b = max(b, head[l]);
+      return b;
+    };
+    const auto take = [&](int j, int mine, int m) {        // of the lanes that have the maximum the one whose expert is first
+      bool won = (mine | kWhich) == m;
+      const unsigned same = __ballot_sync(kAll, won);
+      if (same & (same - 1)) {
+        const unsigned id = won ? (unsigned)expert_of<kVec>(kWhich - (mine & kWhich), lane) : kAll;
+        won = __reduce_min_sync(kAll, id) == id && won;
+      }
+      if (won) {
+        picks[warp][j] = make_int2(mine, lane);
+#pragma unroll
+        for (int l = 0; l < kLists; ++l)
+          if (kLists == 1 || head[l] == mine) head[l] = ++at[l] < kList ? reinterpret_cast<const int*>(space[warp].sorted[l][lane])[at[l]] : kNone;
+      }
+    };
+    int m = 0;
+    for (int j = 0; j < a.k; ++j) {
+      const int mine = best();
+      m = __reduce_max_sync(kAll, mine | kWhich);
+      if (j == 0 && m > (kInf | kWhich)) slow = true;
+      take(j, mine, m);
+    }
+    // behind the k-th there follow those that may still be larger, until one is not (or none is left)
+    float least = of_key(m & ~kWhich);
+    if (a.bias) least -= error_of_any(least);
+    int picked = a.k;
+    for (;;) {
+      const int mine = best();
+      m = __reduce_max_sync(kAll, mine | kWhich);
+      const float above = of_key(m);                      // nothing that is left is larger
+      if (slow || m == (kNone | kWhich) || (a.bias ? above + error_of_any(above) < least || (above == -INFINITY && least > above) : above < least)) break;
+      if (picked == kMaxK) {            // no lane for one more
+        slow = true;
+        break;
+      }
+      take(picked++, mine, m);
+    }
     __syncwarp();
-    const unsigned kept = keep_groups(a, by_expert[warp], lane, close);
-    const unsigned size = a.E / a.groups, inverse = ((1u << 20) + size - 1) / size;      // e / size = e inverse >> 20 for e < 2^10
-#pragma unroll
-    for (int i = 0; i < kPer; ++i)
-      if (!(kept >> (((unsigned)expert_of<kVec>(i, lane) * inverse >> 20) & 31) & 1)) key[i] = 0u;
-  }
-  // lane j keeps the j-th pick; with a bias one more is looked at, whether it is far enough from the last
-  unsigned my_key = 0;
-  int my_id = 0;
-  unsigned kth = 0;
-  int picked = 0;                       // with a bias: up to the first that is smaller than the k-th
-  for (int j = 0; j < a.k || a.bias; ++j) {
-    unsigned m = 0;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) m = max(m, key[i]);
-    m = __reduce_max_sync(kAll, m);
-    if (m == 0) break;                  // (k are always there)
-    if (j == kMaxK) {                   // no lane for one more: let fp64 decide
-      close = true;
-      break;
+    const int2 pick = lane < picked ? picks[warp][lane] : make_int2(0, 0);
+    my_id = expert_of<kVec>(kWhich - (pick.x & kWhich), pick.y);
+    // neighbours in the order: surely so, ...
+    const float low = of_key(pick.x & ~kWhich), next = __shfl_down_sync(kAll, of_key(pick.x | kWhich), 1);
+    if (!slow && __any_sync(kAll, lane < picked - 1 && !(low - next > (a.bias ? error_of_any(low) + error_of_any(next) : 0.f)))) {
+      // ... by their own bounds, or because their inputs are equal?
+      const float z = lane < picked ? as_float(row[my_id]) : 0.f, b = a.bias && lane < picked ? a.bias[my_id] : 0.f;
+      float c = z, err = 0.f;
+      if (a.bias) {
+        const float s = a.sigmoid ? quick_sigmoid(z) : quick_exp(z - norm.top) * norm.inv;
+        c = s + b;
+        err = error_of(s, c, fabsf(z - norm.top), a.sigmoid);       // (sigmoid: norm.top is 0)
+      }
+      const float nc = __shfl_down_sync(kAll, c, 1), nerr = __shfl_down_sync(kAll, err, 1), nz = __shfl_down_sync(kAll, z, 1), nb = __shfl_down_sync(kAll, b, 1);
+      if (__any_sync(kAll, lane < picked - 1 && !(z == nz && b == nb) && !(c - nc > err + nerr))) {      // by their values in fp64
+        double exact = z;
+        if (a.bias && a.sigmoid) exact = sigmoid((double)z) + (double)b;
+        if (a.bias && !a.sigmoid) {
+          double sum = 0.0;
+#pragma unroll 1
+          for (int e = lane; e < a.E; e += 32) sum += exp((double)as_float(row[e]) - (double)norm.top);
+          sum = warp_sum(sum);
+          exact = (sum == 0.0 ? 0.0 : exp((double)z - (double)norm.top) / sum) + (double)b;
+        }
+        pos = 0;
+        for (int j = 0; j < picked; ++j) {
+          const double other = __shfl_sync(kAll, exact, j);
+          const int oid = __shfl_sync(kAll, my_id, j);
+          pos += other > exact || (other == exact && oid < my_id);
+        }
+      }
     }
-    unsigned id = kAll;
-#pragma unroll
-    for (int i = kPer - 1; i >= 0; --i)
-      if (key[i] == m) id = (unsigned)expert_of<kVec>(i, lane);
-    id = __reduce_min_sync(kAll, id);
-#pragma unroll
-    for (int i = 0; i < kPer; ++i)
-      if ((unsigned)expert_of<kVec>(i, lane) == id) key[i] = 0u;
-    if (lane == j) { my_key = m; my_id = (int)id; }
-    picked = j + 1;
-    if (j == a.k - 1) kth = m;
-    if (j >= a.k && m < kth) break;
+    if (lane >= picked) pos = kMaxK;
   }
-  float z = my_key ? as_float(row[my_id]) : 0.f;
-  if (a.bias) {
-    const float b = my_key ? a.bias[my_id] : 0.f, c = of_key(my_key), s = a.sigmoid ? sigmoid(z) : expf(z - norm.top) * norm.inv;
-    const float err = error_of(s, c, z, norm.top, a.sigmoid);
-    const unsigned next_key = __shfl_down_sync(kAll, my_key, 1);
-    const float nc = of_key(next_key), nerr = __shfl_down_sync(kAll, err, 1), nz = __shfl_down_sync(kAll, z, 1), nb = __shfl_down_sync(kAll, b, 1);
-    // neighbours in the order, unless equal by their inputs; and the first that is smaller than the k-th, which stands for all behind it
-    bool near = lane < picked - 1 && !(z == nz && b == nb) && !(c - nc > err + nerr);
-    if (lane == picked - 1 && lane >= a.k) near = !(of_key(kth) - c > error_of_any(c, a.sigmoid) + error_of_any(of_key(kth), a.sigmoid));
-    close = __any_sync(kAll, close || near);
-  }
-  if (close) {
+  if (slow) {                           // NaN, or more that are close than a warp has lanes
     my_id = choose_slowly<L, kPer, kVec>(a, row, lane);
-    z = lane < a.k ? as_float(row[my_id]) : 0.f;
+    pos = lane;
   }
-  const bool mine = lane < a.k;
+  const bool mine = pos < a.k;
+  const float z = mine ? as_float(row[my_id]) : -INFINITY;
   float v;
   if (a.renormalize) {
-    // relative to the largest of the chosen, so that scores that are tiny alike have weights.  sigmoid(z) = exp(z) / (1 + exp(z))
-    const float top = warp_max(mine ? z : -INFINITY), shift = a.sigmoid ? fminf(top, 0.f) : top;
-    v = !mine || z == -INFINITY ? 0.f : a.sigmoid && z > 0.f ? sigmoid(z) : expf(z - shift) / (a.sigmoid ? 1.f + expf(z) : 1.f);
-    float sum = 0.f;
-    for (int j = 0; j < a.k; ++j) sum += __shfl_sync(kAll, v, j);
-    v = sum == 0.f ? 0.f : v / sum;
+    const float top = of_key(warp_max_key(z));
+    v = relative_score(z, a.sigmoid ? fminf(top, 0.f) : top, a.sigmoid);
+    const float sum = warp_sum(v);
+    v = sum == 0.f ? 0.f : __fdividef(v, sum);
     if (norm.inv != norm.inv) v = norm.inv;       // a NaN in the row (one that nobody looked for above is among the chosen)
   } else {
     v = a.sigmoid ? sigmoid(z) : expf(z - norm.top) * norm.inv;
   }
   if (mine) {
-    a.ids[(size_t)t * a.k + lane] = my_id;
-    a.w[(size_t)t * a.k + lane] = v * a.scale;
+    a.ids[(size_t)t * a.k + pos] = my_id;
+    a.w[(size_t)t * a.k + pos] = v * a.scale;
   }
 }
 
@@ -421,15 +593,15 @@ __global__ void __launch_bounds__(kWarps * 32) choose_grad_kernel(const __grid_c
   for (int i = 0; i < kPer / 4; ++i) rows[warp][lane + 32 * i] = make_float4(0.f, 0.f, 0.f, 0.f);
   float v, mean = 0.f;
   if (a.renormalize) {
-    const float top = warp_max(z), shift = a.sigmoid ? fminf(top, 0.f) : top;
-    float n = !on || z == -INFINITY ? 0.f : a.sigmoid && z > 0.f ? sigmoid(z) : expf(z - shift) / (a.sigmoid ? 1.f + expf(z) : 1.f);
+    const float top = of_key(warp_max_key(z));
+    float n = relative_score(z, a.sigmoid ? fminf(top, 0.f) : top, a.sigmoid);
     const float total = warp_sum(n);
-    n = total == 0.f ? 0.f : n / total;
+    n = total == 0.f ? 0.f : __fdividef(n, total);
     mean = warp_sum(n * d);
     v = n * (d - mean);
-    if (a.sigmoid) v *= 1.f / (1.f + expf(z));
+    if (a.sigmoid) v *= sigmoid(-z);
   } else if (a.sigmoid) {
-    v = on ? sigmoid(z) * (1.f / (1.f + expf(z))) * d : 0.f;
+    v = on ? sigmoid(z) * sigmoid(-z) * d : 0.f;
   } else {
     v = d;
     mean = warp_sum(on ? expf(z - norm.top) * norm.inv * d : 0.f);
@@ -474,13 +646,14 @@ __global__ void __launch_bounds__(kWarps * 32) choose_grad_kernel(const __grid_c
 int bytes_of(int dtype) { return dtype == MOE_DTYPE_FP32 ? 4 : dtype == MOE_DTYPE_BF16 || dtype == MOE_DTYPE_FP16 ? 2 : 0; }
 bool misaligned(const void* p, unsigned to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 
-// Keys a lane: 8 up to 256 experts, 32 beyond.
+// Experts a lane: 4 up to 128 experts, 8 up to 256, 32 beyond.
 template <template <class, int, bool> class Kernel, class Args>
 cudaError_t launch(const Args& a, int dtype, bool vec, cudaStream_t stream) {
   const int blocks = (a.T + kWarps - 1) / kWarps;
   const auto go = [&](auto* kernel) { return launch_after(kernel, blocks, kWarps * 32, 0, stream, a); };
   const auto of = [&](auto type) {
     using L = decltype(type);
+    if (a.E <= 128) return vec ? go(Kernel<L, 4, true>::fn) : go(Kernel<L, 4, false>::fn);
     if (a.E <= 256) return vec ? go(Kernel<L, 8, true>::fn) : go(Kernel<L, 8, false>::fn);
     return vec ? go(Kernel<L, 32, true>::fn) : go(Kernel<L, 32, false>::fn);
   };

@@ -1,8 +1,7 @@
 // moe_scaled_quantize / moe_scaled_quantize_weights / moe_scaled_dequantize: values to e4m3 codes with an fp32 scale per block, and back (moe_scaled.cuh).
 //
-// Bound by memory: a 16-bit value is read once and a byte written, k times where rows are sorted on the way.  Eight lanes have a row's block of 128
-// columns, 16 each: two or four 16-byte loads in flight a thread, one 16-byte store of codes; a warp writes 512 bytes in a row.  As in moe_rows.cu
-// the kernel walks tokens.  A block of weights is 128 such rows, read once: a CTA holds it in registers while its maximum is found.
+// Bound by memory and, of 16-bit values, by the integer instructions of the exact rounding: a value is read once and a byte written, k times where rows are sorted on the
+// way.  A thread has 16 neighbouring columns at a time: two or four 16-byte loads, one 16-byte store of codes.  As in moe_rows.cu the kernel walks tokens.  A block of weights is 128 such rows, read once: a CTA holds it in registers while its maximum is found.
 #include <cuda_fp16.h>
 
 #include "moe_dev.cuh"
@@ -52,91 +51,108 @@ __device__ __forceinline__ Raw<E> load(const E* from) {
   }
   return r;
 }
+// largest magnitude, as bits of the element's type (two 16-bit elements at a time)
 template <class E>
 __device__ __forceinline__ unsigned top_bits(const Raw<E>& r) {
   unsigned top = 0u;
 #pragma unroll
   for (int q = 0; q < Raw<E>::kQuads; ++q) {
-    float v[16 / sizeof(E)];
-    unpack<E>(r.q[q], v);
+    const unsigned w[4] = {r.q[q].x, r.q[q].y, r.q[q].z, r.q[q].w};
 #pragma unroll
-    for (int n = 0; n < 16 / (int)sizeof(E); ++n) top = max(top, __float_as_uint(v[n]) & 0x7fffffffu);
-  }
-  return top;
-}
-
-// What a block's values are divided by.  Small scales are taken 2^64 times, with the values, so that no residue of a quotient falls below the normal numbers.
-struct Divisor {
-  float up, scale, inv;
-  __device__ __forceinline__ explicit Divisor(float s) : up(s < 0x1p-60f ? 0x1p64f : 1.f), scale(s * up), inv(1.f / scale) {}
-  // x / s, such that rounding it to e4m3 gives what rounding the exact quotient gives.  A product with the reciprocal, corrected once by its residue, is the
-  // nearest fp32 number (Markstein 1990); only where that is a midpoint of two codes (2^-10 at least), a number of few bits, does it matter on which side of it the quotient
-  // lies, and the sign of the residue says.
-  __device__ __forceinline__ float operator()(float x) const {
-    x *= up;
-    float q = x * inv;
-    q = fmaf(fmaf(-q, scale, x), inv, q);
-    if ((__float_as_uint(q) & 0x7ffffu) == 0u) {
-      const float left = fmaf(-q, scale, x);
-      if (left != 0.f && fabsf(q) >= 0x1p-11f) q = __int_as_float(__float_as_int(q) + ((left < 0.f) == (q < 0.f) ? 1 : -1));
+    for (int i = 0; i < 4; ++i) {
+      if (sizeof(E) == 4) top = max(top, w[i] & 0x7fffffffu);
+      else asm("max.u16x2 %0, %0, %1;" : "+r"(top) : "r"(w[i] & 0x7fff7fffu));
     }
-    return q;
   }
-};
-template <class E>
-__device__ __forceinline__ uint4 codes_of(const Raw<E>& r, const Divisor& by) {
+  return sizeof(E) == 4 ? top : max(top >> 16, top & 0xffffu);
+}
+// ... as those of fp32
+template <class E> __device__ __forceinline__ unsigned wide_bits(unsigned b);
+template <> __device__ __forceinline__ unsigned wide_bits<float>(unsigned b) { return b; }
+template <> __device__ __forceinline__ unsigned wide_bits<__nv_bfloat16>(unsigned b) { return b << 16; }
+template <> __device__ __forceinline__ unsigned wide_bits<__half>(unsigned b) { return __float_as_uint(__half2float(__ushort_as_half((unsigned short)b))); }
+
+// Values over their block's scale, such that rounding the result to e4m3 gives what rounding the exact quotient gives.  A product with the reciprocal, corrected once by
+// its residue, is the nearest fp32 number (Markstein 1990); it becomes the quotient rounded to odd -- cut off, the last bit set where something was cut off --, which by
+// what its own residue says takes five integer operations and no branch, and which is never a midpoint of two codes unless the quotient is one.  (A branch where the
+// nearest number may be a midpoint: 98 304 x 2 048 bf16 147 us.)  kUp: scales below 2^-60 are taken 2^64 times, with the values, so that no residue falls below
+// the normal numbers.
+template <class E, bool kUp>
+__device__ __forceinline__ uint4 codes_with(const Raw<E>& r, float scale) {
   constexpr int kIn = 16 / (int)sizeof(E);
+  if (kUp) scale *= 0x1p64f;
+  const float inv = 1.f / scale;
   unsigned w[4];
 #pragma unroll
-  for (int q = 0; q < Raw<E>::kQuads; ++q) {
+  for (int k = 0; k < Raw<E>::kQuads; ++k) {
     float v[kIn];
-    unpack<E>(r.q[q], v);
+    unpack<E>(r.q[k], v);
 #pragma unroll
-    for (int n = 0; n < kIn; ++n) v[n] = by(v[n]);
+    for (int n = 0; n < kIn; ++n) {
+      const float x = kUp ? v[n] * 0x1p64f : v[n];
+      float q = x * inv;
+      q = fmaf(fmaf(-q, scale, x), inv, q);
+      const float left = fmaf(-q, scale, x);
+      const int bits = __float_as_int(q), below = (bits ^ __float_as_int(left)) >> 31;      // -1 where q is larger than the quotient
+      v[n] = left != 0.f ? __int_as_float((bits + below) | 1) : q;
+    }
 #pragma unroll
-    for (int n = 0; n < kIn; n += 4) w[(q * kIn + n) / 4] = e4m3_codes4(v + n);
+    for (int n = 0; n < kIn; n += 4) w[(k * kIn + n) / 4] = e4m3_codes4(v + n);
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
+template <class E>
+__device__ __forceinline__ uint4 codes_of(const Raw<E>& r, float scale) {
+  return scale < 0x1p-60f ? codes_with<E, true>(r, scale) : codes_with<E, false>(r, scale);
+}
 
-// Eight threads a block: thread i % 8 of block i / 8, block b % blocks of token b / blocks.
+// Four threads a block, twice 16 columns each, 64 apart: thread i % 4 of block i / 4, block b % blocks of token b / blocks.  (Eight threads and 16 columns each, with as much work
+// on scales and addresses a thread: 98 304 x 2 048 bf16 135 us.)
+constexpr int kRowLanes = kLanes / 2;
 template <class E, bool kWide>
 __global__ void __launch_bounds__(kThreads)
 quantize_kernel(const E* __restrict__ x, long long stride, int T, int k, int cols, unsigned blocks, unsigned all, const int* __restrict__ s2f,
                 const int* __restrict__ f2s, unsigned char* __restrict__ codes, float* __restrict__ scales) {
   grid_dep_wait();
-  const unsigned b = blockIdx.x * (kThreads / kLanes) + threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
+  const unsigned b = blockIdx.x * (kThreads / kRowLanes) + threadIdx.x / kRowLanes, lane = threadIdx.x % kRowLanes;
   const unsigned t = b / blocks, c = b - t * blocks;
   const int col = (int)c * kScaledBlock + (int)lane * kCols;
-  const bool on = b < all && col < cols;           // (whole warps meet in the exchange)
-  Raw<E> r;
+  bool on[2];                                      // (whole warps meet in the exchange)
+  Raw<E> r[2];
+  unsigned top = 0u;
 #pragma unroll
-  for (int i = 0; i < Raw<E>::kQuads; ++i) r.q[i] = make_uint4(0u, 0u, 0u, 0u);
-  if (on) r = load<E, kWide>(x + t * stride + col);
-  unsigned top = top_bits<E>(r);
+  for (int h = 0; h < 2; ++h) {
+    on[h] = b < all && col + 64 * h < cols;
 #pragma unroll
-  for (int s = kLanes / 2; s >= 1; s >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
-  if (!on) return;
-  const float scale = scaled_scale(top);
-  const uint4 out = codes_of<E>(r, Divisor(scale));
+    for (int i = 0; i < Raw<E>::kQuads; ++i) r[h].q[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (on[h]) r[h] = load<E, kWide>(x + t * stride + col + 64 * h);
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) top = max(top, top_bits<E>(r[h]));
+#pragma unroll
+  for (int s = kRowLanes / 2; s >= 1; s >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
+  if (!on[0]) return;
+  const float scale = scaled_scale(wide_bits<E>(top));
+  uint4 out[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) out[h] = codes_of<E>(r[h], scale);
+  const auto store = [&](size_t p, const uint4& first, const uint4& second, float s) {
+    uint4* to = reinterpret_cast<uint4*>(codes + p * cols + col);
+    to[0] = first;
+    if (on[1]) to[4] = second;
+    if (lane == 0) scales[p * blocks + c] = s;
+  };
   if (!f2s) {
-    *reinterpret_cast<uint4*>(codes + (size_t)t * cols + col) = out;
-    if (lane == 0) scales[b] = scale;
+    store(t, out[0], out[1], scale);
     return;
   }
   const unsigned R = (unsigned)T * (unsigned)k;
 #pragma unroll 4
   for (int j = 0; j < k; ++j) {
-    const unsigned p = (unsigned)f2s[(size_t)t * k + j];
-    if (p < R) {
-      *reinterpret_cast<uint4*>(codes + (size_t)p * cols + col) = out;
-      if (lane == 0) scales[(size_t)p * blocks + c] = scale;
-    }
-    if ((unsigned)s2f[(size_t)t * k + j] >= R) {       // a row that belongs to no token: zeros
-      const size_t at = (size_t)t * k + j;
-      *reinterpret_cast<uint4*>(codes + at * cols + col) = make_uint4(0u, 0u, 0u, 0u);
-      if (lane == 0) scales[at * blocks + c] = 1.f;
-    }
+    const size_t i = (size_t)t * k + j;
+    const unsigned p = (unsigned)f2s[i];
+    if (p < R) store(p, out[0], out[1], scale);
+    if ((unsigned)s2f[i] >= R) store(i, make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u), 1.f);      // a row that belongs to no token
   }
 }
 
@@ -167,11 +183,10 @@ quantize_weights_kernel(const E* __restrict__ w, int n, int cols, unsigned row_b
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < kThreads / 32; ++i) top = max(top, tops[i]);
-  const float scale = scaled_scale(top);
-  const Divisor by(scale);
+  const float scale = scaled_scale(wide_bits<E>(top));
 #pragma unroll
   for (int m = 0; m < kPer; ++m)
-    if (col < cols && row0 + m * kRowsAtOnce < n) *reinterpret_cast<uint4*>(codes + at + (size_t)m * kRowsAtOnce * cols) = codes_of<E>(r[m], by);
+    if (col < cols && row0 + m * kRowsAtOnce < n) *reinterpret_cast<uint4*>(codes + at + (size_t)m * kRowsAtOnce * cols) = codes_of<E>(r[m], scale);
   if (threadIdx.x == 0) scales[blockIdx.x] = scale;
 }
 
@@ -252,7 +267,7 @@ int moe_scaled_quantize(const void* x, int64_t x_stride, int32_t dtype, int32_t 
   if (misaligned(x, dtype == MOE_DTYPE_FP32 ? 4 : 2) || misaligned(codes, 16) || misaligned(scales, 4) || misaligned(sorted_to_flat, 4) ||
       misaligned(flat_to_sorted, 4))
     return MOE_EINVAL;
-  const int grid = (int)((all + kThreads / kLanes - 1) / (kThreads / kLanes));
+  const int grid = (int)((all + kThreads / kRowLanes - 1) / (kThreads / kRowLanes));
   return status(of_type(dtype, [&](auto type) {
     using E = decltype(type);
     const bool wide = ((reinterpret_cast<uintptr_t>(x) | (uintptr_t)(x_stride * (long long)sizeof(E))) & 15) == 0;

@@ -26,6 +26,7 @@ namespace {
 constexpr int kThreads = 384;
 constexpr int kTmaWarp = 8, kMmaWarp = 9, kScaleWarp = 10, kScaleThreads = 64;
 constexpr int kBlock = kScaledBlock;
+constexpr int kSplit = 4, kSplitRows = 8;       // CTAs that share a tile's blocks, and its most rows
 constexpr int kQuad = 4;                        // blocks whose scales are handed over together
 constexpr int kTurnPitch = 128 + 16, kTurnBytes = 32 * kTurnPitch;      // outputs on their way out: 32 rows of a warp; the 16 bytes spread eight of them over all banks
 constexpr int kQuads = 4;                       // ... of them in the ring
@@ -74,6 +75,7 @@ struct Args {
   int blocks, row_blocks;
   int dtype, wide;               // of out; its rows are 16-byte aligned
   int wide_scales;               // four scales of a row can be loaded at once
+  int split;                     // kSplit: so many CTAs, a cluster, share the blocks of a tile; else 1
 };
 
 // e4m3 operands, fp32 sums, both K-major, M rows, N columns
@@ -136,6 +138,20 @@ __device__ __forceinline__ float ld_shared_f(unsigned saddr) {
   return v;
 }
 __device__ __forceinline__ void st_shared_f(unsigned saddr, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(saddr), "f"(v) : "memory"); }
+// the same place of shared memory in another CTA of the cluster
+__device__ __forceinline__ unsigned map_address(unsigned saddr, unsigned rank) {
+  unsigned r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(saddr), "r"(rank));
+  return r;
+}
+// all threads of a cluster; a warp's together
+__device__ __forceinline__ void meet() {
+  __syncwarp();
+  cluster_sync_all();
+}
+__device__ __forceinline__ void st_cluster_f(unsigned cluster_addr, float v) {
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(cluster_addr), "f"(v) : "memory");
+}
 __device__ __forceinline__ bool try_at(unsigned saddr, unsigned parity) {
   unsigned ok;
   asm volatile(
@@ -199,7 +215,11 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
   const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
   constexpr int kStep = kSwiglu ? 128 : 256;                       // output columns of a tile
   const unsigned rank = kPair ? cluster_ctarank() : 0u;
-  const int unit = (int)blockIdx.x / S::kCtas, n_units = (int)gridDim.x / S::kCtas;
+  // Few tiles of a few rows: the CTAs of a cluster have a part of the blocks each (b_first to b_last), and at the end a part of the rows, which they add up.  A cluster
+  // has one tile at most.
+  const int split = kForm == kFew ? a.split : 1, part_of = kForm == kFew && split > 1 ? (int)cluster_ctarank() : 0;
+  const int b_first = part_of * a.blocks / split, b_last = (part_of + 1) * a.blocks / split;
+  const int ctas = kForm == kFew ? split : S::kCtas, unit = (int)blockIdx.x / ctas, n_units = (int)gridDim.x / ctas;
   const int n_blocks = ((kSwiglu ? a.I : a.N) + kStep - 1) / kStep;
 
   if (tid == 0) {
@@ -250,6 +270,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
     const unsigned ring0 = smem_u32(ring), ring_full = smem_u32(&s.scales_full[0]);
     unsigned part = 0, place = 0;  // partials, places in the ring so far
     unsigned turn = 0;             // exchanges of maxima so far
+    bool met = false;              // the cluster has had its two meetings
     bool ok = true;
     const auto next_partial = [&] {                                 // -> its address
       const unsigned buf = part % S::kParts;
@@ -430,10 +451,10 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
             if (kSwiglu) acc[i][kSwiglu ? 1 : 0][j] = 0.f;
           }
 #pragma unroll 1
-        for (int b0 = 0; b0 < a.blocks && ok; b0 += kQuad) {
+        for (int b0 = b_first; b0 < b_last && ok; b0 += kQuad) {
           unsigned sc = next_scales();
 #pragma unroll 1
-          for (int b = b0; b < min(b0 + kQuad, a.blocks); ++b, sc += 8 * S::kMine) {
+          for (int b = b0; b < min(b0 + kQuad, b_last); ++b, sc += 8 * S::kMine) {
             const unsigned from = next_partial();
             if (!ok) break;
             unsigned p[kGroups][kSwiglu ? 2 : 1][16];
@@ -468,6 +489,37 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
           scales_read();
         }
         const int n = at.n0 + (kSwiglu ? 0 : 128 * half) + 32 * quarter + lane;
+        // row r of the tile is this CTA's: the one of the cluster whose turn it is
+        const auto is_mine = [&](int r) { return r < at.rows && (r & (split - 1)) == part_of; };
+        if (split > 1) {
+          // Sums of the others' rows to their shared memory, [from][row / kSplit][256 weight rows], over the stages, which nobody uses any more; then added in order.
+          meet();
+          const unsigned at_lane = smem_u32(stages) + 4 * (32 * quarter + lane);
+          constexpr int kEach = kSplitRows / kSplit;
+          const auto all = [&](auto f) {
+            if (group(0) != 0) return;
+#pragma unroll
+            for (int r = 0; r < kSplitRows; ++r)
+              if (r < at.rows)
+#pragma unroll
+                for (int h = 0; h < (kSwiglu ? 2 : 1); ++h) f(r, kSwiglu ? h : half, acc[0][h][r]);
+          };
+          all([&](int r, int h, float& v) {
+            if (!ok) v = __uint_as_float(0x7fffffffu);
+            if (!is_mine(r)) st_cluster_f(map_address(at_lane + 4 * ((part_of * kEach + r / kSplit) * 256 + 128 * h), r % kSplit), v);
+          });
+          meet();
+          all([&](int r, int h, float& v) {
+            if (is_mine(r)) {
+              const float own = v;
+              v = 0.f;
+#pragma unroll
+              for (int from = 0; from < kSplit; ++from)
+                v += from == part_of ? own : ld_shared_f(at_lane + 4 * ((from * kEach + r / kSplit) * 256 + 128 * h));
+            }
+          });
+          met = true;
+        }
         if constexpr (kSwiglu) {
 #pragma unroll
           for (int i = 0; i < kGroups; ++i) {
@@ -486,12 +538,12 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
             for (int q = 0; q < 4; ++q) mine = max(mine, tops[16 * q + (lane & 15)]);
             const float scale = ok ? scaled_scale(mine) : __uint_as_float(0x7fffffffu), inv = __fdividef(1.f, scale);
             const int row = 16 * group(i);
-            if (quarter == 0 && lane < 16 && row + lane < at.rows)
+            if (quarter == 0 && lane < 16 && is_mine(row + lane))
               a.out_scales[((size_t)at.row0 + row + lane) * (a.I / kBlock) + at.n0 / kBlock] = scale;
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
               const unsigned code = e4m3_codes2(acc[i][0][j] * __shfl_sync(0xffffffffu, inv, j), 0.f) & 0xffu;
-              if (row + j < at.rows) static_cast<unsigned char*>(a.out)[((size_t)at.row0 + row + j) * a.I + n] = (unsigned char)code;
+              if (is_mine(row + j)) static_cast<unsigned char*>(a.out)[((size_t)at.row0 + row + j) * a.I + n] = (unsigned char)code;
             }
           }
         } else {
@@ -502,12 +554,16 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
               if (i >= groups) break;
 #pragma unroll
               for (int j = 0; j < 16; ++j)
-                if (16 * i + j < at.rows && n < a.N)
+                if (is_mine(16 * i + j) && n < a.N)
                   out[((size_t)at.row0 + 16 * i + j) * a.N + n] = rounded<E>(ok ? acc[i][0][j] : __uint_as_float(0x7fffffffu));
             }
           });
         }
       }
+    }
+    if (kForm == kFew && split > 1 && !met) {             // (no tile)
+      meet();
+      meet();
     }
     // rows that belong to no expert: zeros (scales 1), by the epilogue warps of the whole grid
     const int lo = s.first_row[0], hi = s.first_row[a.E], none = lo + (a.R - hi);
@@ -539,7 +595,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
           const unsigned long long policy = at.alone ? l2_evict_first() : l2_evict_normal();
           const int n0 = at.n0 + (kSwiglu ? 0 : 128 * (int)rank), which = kSwiglu ? (int)rank : 0;      // (rank is 0 where there is no pair)
 #pragma unroll 1
-          for (int i = 0; i < a.blocks; ++i, ++n) {
+          for (int i = b_first; i < b_last; ++i, ++n) {
             const unsigned slot = n % S::kStages, round = n / S::kStages;
             if (round && !wait(&s.empty[slot], (round - 1) & 1, &s.dead)) break;
             const unsigned to = smem_u32(stages + slot * S::kStageBytes);
@@ -575,7 +631,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
           const Tile at = tile_at<S::kRows>(s, a.E, t, kStep);
           const unsigned idesc = kTall ? idesc_of(128 * S::kCtas, 128) : idesc_of(128, (unsigned)(at.rows + 15) & ~15u);
 #pragma unroll 1
-          for (int i = 0; i < a.blocks && ok; ++i, ++n) {
+          for (int i = b_first; i < b_last && ok; ++i, ++n) {
             const unsigned slot = n % S::kStages, round = n / S::kStages, buf = n % S::kParts, use = n / S::kParts;
             const unsigned st = smem_u32(stages + slot * S::kStageBytes);
 #pragma unroll
@@ -627,12 +683,12 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
         for (int q = 0; q < kOwn; ++q)
           x[q] = a.x_scales + ((size_t)at.row0 + min((int)rank * S::kMine + r0 + q * kScaleThreads, at.rows - 1)) * a.blocks;
 #pragma unroll 1
-        for (int b = 0; b < a.blocks; b += kQuad, ++place) {
+        for (int b = b_first; b < b_last; b += kQuad, ++place) {
           float u[kOwn][4], v0[4], v1[4];
-          four(w0 + b, a.blocks - b, v0);
-          four(w1 + b, a.blocks - b, v1);
+          four(w0 + b, b_last - b, v0);
+          four(w1 + b, b_last - b, v1);
 #pragma unroll
-          for (int q = 0; q < kOwn; ++q) four(x[q] + b, a.blocks - b, u[q]);
+          for (int q = 0; q < kOwn; ++q) four(x[q] + b, b_last - b, u[q]);
           const unsigned slot = place % kQuads, round = place / kQuads;
           if (round) ok = __all_sync(0xffffffffu, wait(&s.scales_empty[slot], (round - 1) & 1, &s.dead));
           if (!ok) break;
@@ -648,6 +704,10 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
           if (lane == 0) mbar_arrive(&s.scales_full[slot]);
         }
       }
+    }
+    if (kForm == kFew && split > 1) {
+      meet();
+      meet();
     }
   }
   __syncwarp();
@@ -688,22 +748,33 @@ cudaError_t product_launch(Args& a, const void* codes, const void* w_codes, int 
   if (e != cudaSuccess) return e;
   // most tiles that the rows can make
   const int step = kSwiglu ? 128 : 256;
-  const long long m_tiles = a.R / S::kRows + (a.R < a.E ? a.R : a.E), tiles = m_tiles * (((kSwiglu ? a.I : a.N) + step - 1) / step);
+  const long long m_tiles = (a.R + (long long)(a.R < a.E ? a.R : a.E) * (S::kRows - 1)) / S::kRows, tiles = m_tiles * (((kSwiglu ? a.I : a.N) + step - 1) / step);
   if (tiles > 0x3fffffffll) return cudaErrorInvalidValue;
-  const int units = tiles < sms / S::kCtas ? (int)tiles : sms / S::kCtas;
+  int ctas = S::kCtas;
+  a.split = 1;
+  if (kForm == kFew) {
+    // Clusters of four, as long as all of them fit (32 do; 36 take a second round), share the blocks.  us, one row, K 4096, by weight rows, alone / clusters of two / four:
+    // 2048 14.1 / 11.1 / 8.6, 4096 14.8 / 12.1 / 9.8, 6144 14.7 / 12.3 / 10.8, 8192 14.8 / 12.9 / 12.4, 9216 14.9 / 13.4 / 19.4; K 2048: 4096 8.8 / 8.7 / 7.8; K 1024 (swiglu)
+    // 6.8 / 8.3 / 8.0; 16 rows, K 2048, 2048 weight rows 9.5 / 12.5 / 11.8.
+    if (a.R <= kSplitRows && a.blocks >= 16 && tiles <= 32 && sms >= 32 * kSplit) {
+      a.split = ctas = kSplit;
+      a.wide_scales = 0;           // (parts begin anywhere)
+    }
+  }
+  const int units = tiles < sms / ctas ? (int)tiles : sms / ctas;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = S::kCtas;
+  attr[1].val.clusterDim.x = ctas;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(units * S::kCtas));
+  cfg.gridDim = dim3((unsigned)(units * ctas));
   cfg.blockDim = dim3((unsigned)kThreads);
   cfg.dynamicSmemBytes = S::kSmem;
   cfg.stream = stream;
   cfg.attrs = attr;
-  cfg.numAttrs = S::kCtas > 1 ? 2 : 1;
+  cfg.numAttrs = ctas > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<const Args&>(a));
 }
 

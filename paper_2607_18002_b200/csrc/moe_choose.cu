@@ -150,9 +150,9 @@ __device__ __forceinline__ Norm norm_of(const float (&z)[kPer]) {
 // addition and the reciprocal; softmax: the sum's 13 additions, its terms' errors (|x| weighted by their share is ln E at most) and the quotient, 15.  Of any score, where
 // s |x| counts less than 1.  What is lost below 2^-126 is less than 2^-120.
 __device__ __forceinline__ float error_of(float s, float c, float far, bool is_sigmoid) {
-  return ldexpf(s * (is_sigmoid ? 6.f + far : 25.f + 2.f * far) + fabsf(c), -23) + 0x1p-120f;
+  return (s * (is_sigmoid ? 6.f + far : 25.f + 2.f * far) + fabsf(c)) * 0x1p-23f + 0x1p-120f;
 }
-__device__ __forceinline__ float error_of_any(float c) { return ldexpf(26.f + fabsf(c), -23); }
+__device__ __forceinline__ float error_of_any(float c) { return (26.f + fabsf(c)) * 0x1p-23f; }
 
 // The same in fp64, by the whole warp: rare.  Lane j < k gets the j-th expert.
 template <class L, int kPer, bool kVec>
@@ -266,7 +266,7 @@ struct Two {
   __device__ __forceinline__ V value(const ChooseArgs& a, int size) const { return a.group_sum > 1 && size > 1 ? one + two : one; }
   // (a group of one expert, or one that holds -inf, has no second value that counts)
   __device__ __forceinline__ float error(V v) const {
-    return one == -INFINITY ? 0.f : error_of_any(one) + (two == -INFINITY ? 0.f : error_of_any(two) + ldexpf(fabsf(v), -23));
+    return one == -INFINITY ? 0.f : error_of_any(one) + (two == -INFINITY ? 0.f : error_of_any(two) + (fabsf(v)) * 0x1p-23f);
   }
 };
 // whether fp32 cannot tell which groups are kept: the least of those inside, the largest of those outside, the largest error

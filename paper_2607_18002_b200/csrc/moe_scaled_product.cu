@@ -753,10 +753,10 @@ cudaError_t product_launch(Args& a, const void* codes, const void* w_codes, int 
   int ctas = S::kCtas;
   a.split = 1;
   if (kForm == kFew) {
-    // Clusters of four, as long as all of them fit (32 do; 36 take a second round), share the blocks.  us, one row, K 4096, by weight rows, alone / clusters of two / four:
-    // 2048 14.1 / 11.1 / 8.6, 4096 14.8 / 12.1 / 9.8, 6144 14.7 / 12.3 / 10.8, 8192 14.8 / 12.9 / 12.4, 9216 14.9 / 13.4 / 19.4; K 2048: 4096 8.8 / 8.7 / 7.8; K 1024 (swiglu)
-    // 6.8 / 8.3 / 8.0; 16 rows, K 2048, 2048 weight rows 9.5 / 12.5 / 11.8.
-    if (a.R <= kSplitRows && a.blocks >= 16 && tiles <= 32 && sms >= 32 * kSplit) {
+    // Clusters of four share the blocks as long as all of them fit (32 do; 36 take a second round).  us, one row, alone / shared, by weight rows: K 4096: 2048 13.7 / 6.9,
+    // 4096 14.3 / 7.9, 6144 14.4 / 8.7, 8192 14.6 / 10.0, 9216 14.6 / 16.5; K 2048: 4096 8.7 / 5.8; K 1024: 4096 5.9 / 5.0; K 512: 2048 4.4 / 4.5.  (Clusters of two: 6144 10.5,
+    // 12288 13.8 for 15.0, 64 tiles of K 2048 11.1 for 10.4.  Up to 64 rows shared: the code alone took one row of 6144 from 8.7 to 10.8, 16 rows of 2048 x 2048 from 9.5 to 11.8.)
+    if (a.R <= kSplitRows && a.blocks >= 8 && tiles <= 32 && sms >= 32 * kSplit) {
       a.split = ctas = kSplit;
       a.wide_scales = 0;           // (parts begin anywhere)
     }

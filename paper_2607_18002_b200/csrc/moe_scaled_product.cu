@@ -425,12 +425,21 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
                   if (r < rows && at_col < cols) *reinterpret_cast<uint4*>(out + (size_t)r * a.N + col0 + at_col) = v;
                 }
               } else {
-#pragma unroll 4
-                for (int r = 0; r < rows; ++r) {
-                  const E* from = reinterpret_cast<const E*>(turned + warp * kTurnBytes + r * kTurnPitch);
+                // an element a lane, eight rows' at once on their way
+                const E* from = reinterpret_cast<const E*>(turned + warp * kTurnBytes) + lane;
+                E* to = out + col0 + lane;
+#pragma unroll 1
+                for (int r = 0; r < rows; r += 8, from += 8 * (kTurnPitch / (int)sizeof(E)), to += 8 * (size_t)a.N) {
+                  E v[8][kCols / 32];
 #pragma unroll
-                  for (int i = lane; i < kCols; i += 32)
-                    if (i < cols) out[(size_t)r * a.N + col0 + i] = from[i];
+                  for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int h = 0; h < kCols / 32; ++h) v[i][h] = from[i * (kTurnPitch / (int)sizeof(E)) + 32 * h];
+#pragma unroll
+                  for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int h = 0; h < kCols / 32; ++h)
+                      if (r + i < rows && lane + 32 * h < cols) to[(size_t)i * a.N + 32 * h] = v[i][h];
                 }
               }
               __syncwarp();

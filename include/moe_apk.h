@@ -368,7 +368,7 @@ int moe_mx_swiglu(const void* codes, const void* scales, const void* w_codes, co
 
 /* Rows in e4m3 with a scale per 128 columns, weights in e4m3 with a scale per 128 x 128: the form of a context's e4m3 operands, for experts of the caller's own.
  * A value is code * scale.  [rows, cols] rows have codes [rows, cols] and fp32 scales [rows, ceil(cols/128)]; matrices [E, n, cols] have scales
- * [E, ceil(n/128), ceil(cols/128)]; blocks at the edges are smaller.  The scale of a block is amax / 448 (one fp32 division), 1 for a block of
+ * [E, ceil(n/128), ceil(cols/128)]; blocks at the edges are smaller.  The scale of a block is amax * (1 / 448) (both operations in fp32), 1 for a block of
  * zeros, 2^-126 at least; a code is the e4m3 value nearest to the exact quotient, ties to the even code.  A block that holds NaN or infinity
  * has a NaN scale: all of it is NaN (its codes say nothing).  cols: a multiple of 16, at most 2^30;
  * weights and dequantised values: 2^40 at most.

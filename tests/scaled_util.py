@@ -100,7 +100,7 @@ def block_scales(x, rows):
     b = b.reshape(*x.shape[:-2], b.shape[-2] // rows, rows, b.shape[-1] // 128, 128)
     top = b.max((-1, -3))
     with np.errstate(invalid="ignore", over="ignore"):
-        s = np.maximum(top.astype(np.float32) / np.float32(448.0), np.float32(2.0 ** -126))
+        s = np.maximum(top.astype(np.float32) * (np.float32(1.0) / np.float32(448.0)), np.float32(2.0 ** -126))
     s = np.where(top == 0, np.float32(1), s)
     return np.where(np.isfinite(top), s, np.float32(np.nan)).astype(np.float32)
 

@@ -195,16 +195,29 @@ template <> __device__ __forceinline__ float rounded(float v) { return v; }
 template <> __device__ __forceinline__ __half rounded(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 rounded(float v) { return __float2bfloat16_rn(v); }
 
-// A thread writes 16 bytes of values at a time, four times: its loads are in flight together, and a warp writes 512 bytes in a row.
+// A thread writes 16 bytes of values at a time, four times: its loads are in flight together, and a warp writes 512 bytes in a row.  Where the second to fourth lie follows from the
+// first by additions (kThreads values further on: `rows` rows and `left` places of a row of per_row); divisions for each took 102 us for 98 304 x 2 048 bf16, 92 so (6.5 TB/s).
 constexpr int kAtOnce = 4;
+struct Steps {
+  unsigned per_row, rows, left;
+};
 template <class E>
 __global__ void __launch_bounds__(kThreads)
-dequantize_kernel(const unsigned char* __restrict__ codes, const float* __restrict__ scales, long long all, unsigned n, unsigned cols, int shift,
+dequantize_kernel(const unsigned char* __restrict__ codes, const float* __restrict__ scales, long long all, unsigned n, unsigned blocks, Steps step, int shift,
                   uint4* __restrict__ out) {
   constexpr int kN = 16 / (int)sizeof(E);
   grid_dep_wait();
-  const unsigned per_row = cols / kN, blocks = (cols + kScaledBlock - 1) / kScaledBlock, row_blocks = (n + (1u << shift) - 1) >> shift;
+  const unsigned row_blocks = (n + (1u << shift) - 1) >> shift;
   const long long i0 = (long long)blockIdx.x * (kThreads * kAtOnce) + threadIdx.x;
+  unsigned long long row = i0 >> 32 ? i0 / step.per_row : (unsigned)i0 / step.per_row;
+  unsigned c = (unsigned)(i0 - row * step.per_row);
+  // the row of scales: that of the row itself, or of its 128 in matrix e (row `in` of it)
+  unsigned long long e = 0;
+  unsigned in = 0;
+  if (shift) {
+    e = row >> 32 ? row / n : (unsigned)row / n;
+    in = (unsigned)(row - e * n);
+  }
   uint2 word[kAtOnce];
   float scale[kAtOnce];
 #pragma unroll
@@ -213,10 +226,18 @@ dequantize_kernel(const unsigned char* __restrict__ codes, const float* __restri
     if (i < all) {
       if (kN == 8) word[m] = reinterpret_cast<const uint2*>(codes)[i];
       else word[m].x = reinterpret_cast<const unsigned*>(codes)[i];
-      const unsigned long long row = i >> 32 ? i / per_row : (unsigned)i / per_row;
-      const unsigned c = (unsigned)(i - row * per_row) * kN / kScaledBlock;
-      const unsigned e = (unsigned)(row >> 32 ? row / n : (unsigned)row / n), in = (unsigned)(row - (unsigned long long)e * n);
-      scale[m] = scales[((size_t)e * row_blocks + (in >> shift)) * blocks + c];
+      scale[m] = scales[(shift ? e * row_blocks + (in >> shift) : row) * blocks + c * kN / kScaledBlock];
+    }
+    if (m + 1 < kAtOnce) {
+      const bool over = c + step.left >= step.per_row;
+      c += step.left - (over ? step.per_row : 0u);
+      const unsigned down = step.rows + over;
+      row += down;
+      in += down;
+      if (shift && in >= n) {
+        e += in / n;
+        in %= n;
+      }
     }
   }
 #pragma unroll
@@ -224,15 +245,15 @@ dequantize_kernel(const unsigned char* __restrict__ codes, const float* __restri
     const long long i = i0 + m * kThreads;
     if (i >= all) return;
     uint4 raw;
-    E* e = reinterpret_cast<E*>(&raw);
+    E* v = reinterpret_cast<E*>(&raw);
 #pragma unroll
     for (int q = 0; q < kN; q += 2) {
       const unsigned short two = (unsigned short)((q < 4 ? word[m].x : word[m].y) >> (8 * (q & 3)));
       unsigned h;                                  // e4m3 values are exact in fp16
       asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(two));
-      const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&h));
-      e[q] = rounded<E>(v.x * scale[m]);
-      e[q + 1] = rounded<E>(v.y * scale[m]);
+      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+      v[q] = rounded<E>(f.x * scale[m]);
+      v[q + 1] = rounded<E>(f.y * scale[m]);
     }
     out[i] = raw;
   }
@@ -301,8 +322,10 @@ int moe_scaled_dequantize(const void* codes, const float* scales, int32_t n_expe
   return status(of_type(dtype, [&](auto type) {
     using E = decltype(type);
     const long long all = (long long)count / (16 / (int)sizeof(E)), grid = (all + kThreads * kAtOnce - 1) / (kThreads * kAtOnce);
+    const unsigned per_row = (unsigned)(cols / (16 / (int)sizeof(E)));
     return launch_after(dequantize_kernel<E>, (int)grid, kThreads, 0, static_cast<cudaStream_t>(stream), static_cast<const unsigned char*>(codes), scales,
-                        all, (unsigned)n_rows, (unsigned)cols, scale_rows == 1 ? 0 : 7, static_cast<uint4*>(values));
+                        all, (unsigned)n_rows, (unsigned)blocks_of(cols), Steps{per_row, kThreads / per_row, kThreads % per_row}, scale_rows == 1 ? 0 : 7,
+                        static_cast<uint4*>(values));
   }));
 }
 

@@ -3,15 +3,19 @@
 //   product   out[p, n] = sum_b sx[p, b] sw[e, n / 128, b] sum_{k in block b} x[p, k] w[e, n, k]        (rounded once)
 //   swiglu    g, u = products with rows n and I + n of w[e];  a = g / (1 + exp(-g)) u in fp32, quantised per 128 columns to codes and a scale
 //
-// tcgen05.mma.kind::f8f6f4 knows no scales, so the 128 products of a block are added up in the tensor core, each block in a fresh buffer in TMEM, and eight
-// epilogue warps read every such partial and multiply-add it with its two scales into fp32 registers.
+// tcgen05.mma.kind::f8f6f4 knows no scales, so the 128 products of a block are added up in the tensor core, each block in a fresh buffer in TMEM (a partial), and eight
+// epilogue warps read every partial and multiply-add it with its two scales into fp32 registers: one multiply-add and four bytes out of TMEM for 128 products.
 //
-// Two forms.  Few rows an expert (kTall false): weight rows are the M of the instruction, twice 128 TMEM lanes, up to 64 rows its N in steps of 16; one
-// CTA a tile; the bound is the weight stream.  Many (kTall): 256 rows are the M of a pair of CTAs (cta_group::2), 256 weight rows its N; each CTA holds 128 of
-// either.  A thread then has a row: one multiplier for all of its columns.
+// Forms.  Few rows an expert: weight rows are the M of the instruction, twice 128 TMEM lanes, up to 64 rows its N in steps of 16; one CTA a tile, four partials.  Where such tiles
+// are few, four CTAs, a cluster, share a tile's blocks and add up a part of its rows each.  More rows (tall): 128 rows are the M of a CTA and 256 weight rows its N, or 256 rows that
+// of a pair of CTAs (cta_group::2), each of which holds 128 of either.  A thread then has a row: one multiplier for all of its columns.  The columns are two halves of 128, each
+// with buffers and epilogue warps of its own, so that what one half loads and the other adds alternates.
 //
-// Roles: warps 0-7 epilogue, 8 TMA (one thread; a stage is a block of 128 columns: 128-byte rows, swizzled), 9 MMA (one thread), 10 and 11 bring the
-// products of the two scales, four blocks at a time, into a ring in shared memory.
+// Roles: warps 0-7 epilogue, 8 TMA (one thread; a stage is a block of 128 columns: 128-byte rows, swizzled), 9 MMA (one thread), 10 and 11 bring the products of the two scales, four
+// blocks at a time, into a ring in shared memory.
+// What bounds them: few rows, the weight stream (100 tokens on 128 experts: gate/up 305 us, 6.2 TB/s; one CTA streams 97 GB/s); many, power and the way of a partial from the tensor core to
+// the epilogue and back: 8192 x 4096 x 4096 133-140 us (2.0 PFLOP/s, tensor pipe 53 % of the cycles), 65 536 rows of 64 experts, K 4096, 3584 gate/up rows 1 075 us, K 1792, 4096
+// columns 600, at 1 000 W and 1.46 GHz.  Without loads from TMEM and additions the same launch takes 0.81 of that, without the additions alone 0.84.
 // Every wait is bounded (2 s); where one runs out the launch ends, after another such limit for its copies in flight, and what it has not computed is NaN.
 #include <cuda_fp16.h>
 
@@ -813,7 +817,16 @@ int product(const void* codes, const float* scales, const void* w_codes, const f
   a.wide = (long long)n * el % 16 == 0 && (address(out) & 15) == 0;
   a.wide_scales = a.blocks % 4 == 0 && ((address(scales) | address(w_scales)) & 15) == 0;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  // The form goes by the rows that an expert gets on average; the host does not know more.
+  // The form goes by the rows that an expert gets on average; the host does not know more.  us, by rows an expert (gate/up; down), weights that are not in L2:
+  //                                   16        32        48        64        96        128       192       256       320       384       512       1024
+  //   uneven (Zipf 0.8), 64 experts, 2048 x 768
+  //     few                           40; 24    45; 28    50; 32    53; 38    77; 49    92; 64    127; 89   154; 111  187; 139  207; 161  285; 213  523; 405
+  //     128 rows                      43; 25    44; 26    46; 26    47; 27    58; 33    60; 39    74; 46    100; 60   114; 71   137; 81   168; 98   301; 179
+  //     256 rows, pairs               65; 37    69; 43    71; 42    75; 45    78; 46    79; 47    94; 52    106; 66   119; 70   139; 80   166; 100  293; 172
+  //   even, 32 experts, 4096 x 1792
+  //     few                           87; 45    90; 47    96; 50    101; 56   161; 90   161; 91   226; 140  287; 177  347; 224            525; 347  1069; 647
+  //     128 rows                                          105; 52   107; 53   110; 55   113; 57   179; 90   178; 90   249; 130            316; 180  614; 318
+  //     256 rows, pairs               137; 68   142; 73   146; 73   157; 77   156; 77   160; 80   163; 83   159; 81   290; 151            284; 161  552; 288
   const long long per = n_rows / n_experts;
   const cudaError_t e = per <= 32    ? product_launch<kFew, kSwiglu>(a, codes, w_codes, K, st)
                         : per <= 384 ? product_launch<kTile, kSwiglu>(a, codes, w_codes, K, st)

@@ -49,7 +49,7 @@ struct Shape {
   static constexpr int kCtas = kForm == kTilePair ? 2 : 1;
   static constexpr int kRows = kTall ? 128 * kCtas : 64;            // of a tile
   // Tall: a half of the columns has 64 of the first 128 weight rows and 64 of the second; where one CTA has them all, and their order is free, its 128 rows
-  static constexpr bool kMixed = kForm == kTilePair || kSwiglu;
+  [[maybe_unused]] static constexpr bool kMixed = kForm == kTilePair || kSwiglu;
   // weight rows and parts (gate, up) of a TMA box, boxes of a stage
   static constexpr int kBoxWeights = kForm == kTilePair ? 128 : !kSwiglu ? 256 : kTall ? 64 : 128, kBoxParts = kSwiglu && kForm != kTilePair ? 2 : 1;
   static constexpr int kBoxes = kForm == kTile && kSwiglu ? 2 : 1;

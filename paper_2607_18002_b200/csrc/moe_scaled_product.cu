@@ -36,35 +36,37 @@ constexpr int kTurnPitch = 128 + 16, kTurnBytes = 32 * kTurnPitch;      // outpu
 constexpr int kQuads = 4;                       // ... of them in the ring
 
 struct Shared : Segments {
-  unsigned long long full[8], empty[8], part_full[4], part_empty[4], scales_full[kQuads], scales_empty[kQuads], drained;
+  unsigned long long full[8], empty[8], part_full[8], part_empty[8], scales_full[kQuads], scales_empty[kQuads], drained;
   unsigned tmem;
   volatile int dead;             // a wait ran out
   unsigned tops[2][2][128];      // swiglu: largest magnitudes on their way from warp to warp
 };
 
-enum Form { kFew, kTile, kTilePair };
+enum Form { kFew, kNarrow, kTile, kTilePair };
 template <Form kForm, bool kSwiglu>
 struct Shape {
   static constexpr bool kTall = kForm != kFew;
   static constexpr int kCtas = kForm == kTilePair ? 2 : 1;
   static constexpr int kRows = kTall ? 128 * kCtas : 64;            // of a tile
-  // Tall: a half of the columns has 64 of the first 128 weight rows and 64 of the second; where one CTA has them all, and their order is free, its 128 rows
+  static constexpr int kCols = kForm == kNarrow ? 64 : 256;         // weight rows of a tile
+  // Tall: a half of the columns has 64 of the first 128 weight rows and 64 of the second; where one CTA has them all, and their order is free, its share of them in a row
   [[maybe_unused]] static constexpr bool kMixed = kForm == kTilePair || kSwiglu;
   // weight rows and parts (gate, up) of a TMA box, boxes of a stage
-  static constexpr int kBoxWeights = kForm == kTilePair ? 128 : !kSwiglu ? 256 : kTall ? 64 : 128, kBoxParts = kSwiglu && kForm != kTilePair ? 2 : 1;
+  static constexpr int kBoxWeights = kForm == kTilePair ? 128 : !kSwiglu ? kCols : kTall ? 64 : 128, kBoxParts = kSwiglu && kForm != kTilePair ? 2 : 1;
   static constexpr int kBoxes = kForm == kTile && kSwiglu ? 2 : 1;
   static constexpr int kMine = kRows / kCtas;                       // ... in this CTA
-  static constexpr int kWBytes = 256 / kCtas * kBlock, kXBytes = kMine * kBlock, kStageBytes = kWBytes + kXBytes;
+  static constexpr int kWBytes = kCols / kCtas * kBlock, kXBytes = kMine * kBlock, kStageBytes = kWBytes + kXBytes;
   static constexpr int kBoxRows = kTall ? 64 : 32;                  // of a TMA box of rows
-  // A partial: 128 TMEM columns.  Tall: half of the columns of a block's products, which four of the epilogue's warps read, two for each half; else all of them.
-  static constexpr int kHalves = kTall ? 2 : 1;
-  static constexpr int kParts = 4 / kHalves;                        // of a half
+  // A partial.  Tall: half of the columns of a block's products, which four of the epilogue's warps read, two or four for each half; else all of them, four.
+  static constexpr int kHalves = kTall ? 2 : 1, kHalfCols = kCols / 2;
+  static constexpr int kPartCols = kTall ? kHalfCols : 2 * kRows;   // TMEM columns
+  static constexpr int kParts = kForm == kNarrow || !kTall ? 4 : 2; // of a half
   static constexpr int kScaleFloats = kQuad * 2 * kMine;            // of a place in the ring: [block][half][row]
   static constexpr int kScaleBytes = kQuads * kScaleFloats * 4;
   static constexpr int kOutBytes = kTall && !kSwiglu ? 8 * kTurnBytes : 0;
   static constexpr int kStages = (227 * 1024 - 1024 - (int)sizeof(Shared) - kScaleBytes - kOutBytes) / kStageBytes;
   static constexpr int kSmem = 1024 + kStages * kStageBytes + kScaleBytes + kOutBytes + (int)sizeof(Shared);
-  static_assert(kStages >= 3 && kStages <= 8, "barriers");
+  static_assert(kStages >= 3 && kStages <= 8 && kHalves * kParts <= 8 && kHalves * kParts * kPartCols <= 512, "barriers, TMEM");
 };
 
 struct Args {
@@ -217,7 +219,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
   unsigned char* turned = reinterpret_cast<unsigned char*>(ring) + S::kScaleBytes;
   Shared& s = *reinterpret_cast<Shared*>(turned + S::kOutBytes);
   const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
-  constexpr int kStep = kSwiglu ? 128 : 256;                       // output columns of a tile
+  constexpr int kStep = kSwiglu ? 128 : S::kCols;                  // output columns of a tile
   const unsigned rank = kPair ? cluster_ctarank() : 0u;
   // Few tiles of a few rows: the CTAs of a cluster have a part of the blocks each (b_first to b_last), and at the end a part of the rows, which they add up.  A cluster
   // has one tile at most.
@@ -231,7 +233,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
       mbar_init(&s.full[i], S::kCtas);
       mbar_init(&s.empty[i], 1);
     }
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < S::kHalves * S::kParts; ++i) {
       mbar_init(&s.part_full[i], 1);
       mbar_init(&s.part_empty[i], 8 / S::kHalves * S::kCtas);
     }
@@ -280,7 +282,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
       const unsigned buf = part % S::kParts;
       if (ok) ok = warp_wait(full0 + 8 * buf, (part / S::kParts) & 1, &s.dead);
       tc_fence_after();
-      return lanes + (first + buf) * 128;
+      return lanes + (first + buf) * S::kPartCols;
     };
     const auto hand_back = [&] {                                    // the warp has what it loads of the partial
       tc_fence_before();
@@ -304,10 +306,56 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
         const int mine = 32 * quarter + lane, row = 128 * (int)rank + mine;
         const bool used = uniform(128 * (int)rank + 32 * quarter) < at.rows, valid = row < at.rows;
         // Pairs of neighbouring columns, of this half.  kMixed: 0-63 are of the first 128 weight rows (swiglu: gate rows), 64-127 of the second (up rows)
-        unsigned long long sum[64];
+        unsigned long long sum[S::kHalfCols / 2];
 #pragma unroll
-        for (int i = 0; i < 64; ++i) sum[i] = 0ull;
-        if (used) {
+        for (int i = 0; i < S::kHalfCols / 2; ++i) sum[i] = 0ull;
+        if (!used) {               // (no row of the tile: the hand-overs alone)
+#pragma unroll 1
+          for (int b = 0; b < a.blocks && ok; ++b) {
+            if (b % kQuad == 0) {
+              next_scales();
+              scales_read();
+            }
+            next_partial();
+            hand_back();
+          }
+          if (kSwiglu) {
+            ++turn;
+            bar_sync(1 + quarter, 64);
+          }
+          continue;
+        }
+        if constexpr (S::kHalfCols == 32) {
+          // the next block's columns are on their way while one's are added
+          unsigned v[2][32];
+          unsigned sc = next_scales() + 4 * mine, from = next_partial();
+          if (ok) tc_ld32(from, v[0]);
+#pragma unroll 1
+          for (int b0 = 0; b0 < a.blocks && ok; b0 += 2)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const int b = b0 + u;
+              if (b >= a.blocks) break;
+              const float m = ld_shared_f(sc);
+              sc += 8 * S::kMine;
+              const bool more = b < a.blocks - 1;
+              tc_wait_ld();
+              loaded(v[u]);
+              hand_back();
+              if (b % kQuad == kQuad - 1 || !more) {
+                scales_read();
+                if (more) sc = next_scales() + 4 * mine;
+              }
+              if (more) {
+                from = next_partial();
+                if (!ok) break;
+                tc_ld32(from, v[u ^ 1]);
+              }
+              const unsigned long long two = f32x2(m, m);
+#pragma unroll
+              for (int j = 0; j < 16; ++j) sum[j] = fma_f32x2(f32x2(__uint_as_float(v[u][2 * j]), __uint_as_float(v[u][2 * j + 1])), two, sum[j]);
+            }
+        } else {
           // 64 columns are on their way or being added at any time: a wait is for all loads before it, so there are two a block, and the next block's first
           // loads go out between this one's last additions.  (Five waits a block, 16 and 32 columns at a time: gate/up of 65 536 rows 2 490 us for 2 120.)
           unsigned v[2][32];
@@ -351,28 +399,11 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
             add(3, s1);
             if (more) tc_ld32(from + 32, v[1]);
           }
-        } else {                   // (no row of the tile: the hand-overs alone)
-#pragma unroll 1
-          for (int b = 0; b < a.blocks && ok; ++b) {
-            if (b % kQuad == 0) {
-              next_scales();
-              scales_read();
-            }
-            next_partial();
-            hand_back();
-          }
-        }
-        if (!used) {
-          if (kSwiglu) {
-            ++turn;
-            bar_sync(1 + quarter, 64);
-          }
-          continue;
         }
         const size_t p = (size_t)at.row0 + row;
-        float acc[128];
+        float acc[S::kHalfCols];
 #pragma unroll
-        for (int i = 0; i < 64; ++i) {
+        for (int i = 0; i < S::kHalfCols / 2; ++i) {
           const float2 two = f32x2_parts(sum[i]);
           acc[2 * i] = two.x;
           acc[2 * i + 1] = two.y;
@@ -400,7 +431,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
         } else {
           if (!ok) {
 #pragma unroll
-            for (int i = 0; i < 128; ++i) acc[i] = __uint_as_float(0x7fffffffu);
+            for (int i = 0; i < S::kHalfCols; ++i) acc[i] = __uint_as_float(0x7fffffffu);
           }
           // A warp turns its 32 rows round in shared memory, 128 bytes of each at a time, so that its stores are 128 bytes of four rows.  (16 bytes of 32 rows a
           // store: 4 000 clocks a tile.)
@@ -408,13 +439,14 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
           const int rows = min(32, at.rows - 128 * (int)rank - 32 * quarter);
           with_type(a.dtype, a.out, [&](auto* out) {
             using E = typename std::remove_pointer<decltype(out)>::type;
-            constexpr int kIn = 16 / (int)sizeof(E), kCols = 128 / (int)sizeof(E);
+            constexpr int kIn = 16 / (int)sizeof(E), kCols = S::kHalfCols < 128 / (int)sizeof(E) ? S::kHalfCols : 128 / (int)sizeof(E);
+            constexpr int kPieces = kCols / kIn;           // 16-byte pieces of a row at a time
             out += (size_t)(at.row0 + 128 * (int)rank + 32 * quarter) * a.N;
 #pragma unroll
-            for (int c = 0; c < 128 / kCols; ++c) {
-              const int col0 = at.n0 + (S::kMixed ? 128 * (c * kCols / 64) + 64 * half + c * kCols % 64 : 128 * half + c * kCols), cols = min(kCols, a.N - col0);
+            for (int c = 0; c < S::kHalfCols / kCols; ++c) {
+              const int col0 = at.n0 + (S::kMixed ? 128 * (c * kCols / 64) + 64 * half + c * kCols % 64 : S::kHalfCols * half + c * kCols), cols = min(kCols, a.N - col0);
 #pragma unroll
-              for (int i = 0; i < 8; ++i) {
+              for (int i = 0; i < kPieces; ++i) {
                 uint4 v;
 #pragma unroll
                 for (int j = 0; j < kIn; ++j) reinterpret_cast<E*>(&v)[j] = rounded<E>(acc[c * kCols + i * kIn + j]);
@@ -423,9 +455,9 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
               __syncwarp();
               if (a.wide) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                  const int r = 4 * i + lane / 8, at_col = lane % 8 * kIn;
-                  const uint4 v = ld_shared16(own + r * kTurnPitch + lane % 8 * 16);
+                for (int i = 0; i < kPieces; ++i) {
+                  const int r = 32 / kPieces * i + lane / kPieces, at_col = lane % kPieces * kIn;
+                  const uint4 v = ld_shared16(own + r * kTurnPitch + lane % kPieces * 16);
                   if (r < rows && at_col < cols) *reinterpret_cast<uint4*>(out + (size_t)r * a.N + col0 + at_col) = v;
                 }
               } else {
@@ -642,7 +674,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
         bool ok = true;
         for (int t = unit; t < n_tiles && ok; t += n_units) {
           const Tile at = tile_at<S::kRows>(s, a.E, t, kStep);
-          const unsigned idesc = kTall ? idesc_of(128 * S::kCtas, 128) : idesc_of(128, (unsigned)(at.rows + 15) & ~15u);
+          const unsigned idesc = kTall ? idesc_of(128 * S::kCtas, S::kHalfCols) : idesc_of(128, (unsigned)(at.rows + 15) & ~15u);
 #pragma unroll 1
           for (int i = b_first; i < b_last && ok; ++i, ++n) {
             const unsigned slot = n % S::kStages, round = n / S::kStages, buf = n % S::kParts, use = n / S::kParts;
@@ -654,7 +686,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
               if (h == 0) ok = ok && wait(&s.full[slot], round & 1, &s.dead);
               if (!ok) break;
               tc_fence_after();
-              const unsigned d = tmem + (buf + S::kParts * h) * 128;
+              const unsigned d = tmem + (buf + S::kParts * h) * S::kPartCols;
               if (kTall) {
                 mma_block<kPair>(d, umma_desc(st + S::kWBytes, 128), umma_desc(st + h * (S::kWBytes / 2), 128), idesc);
               } else {
@@ -689,7 +721,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
       for (int t = unit; t < n_tiles && ok; t += n_units) {
         const Tile at = uniform(tile_at<S::kRows>(s, a.E, t, kStep));
         const float* w0 = a.w_scales + ((size_t)at.expert * a.row_blocks + at.n0 / kBlock) * a.blocks;
-        const int second = kSwiglu ? a.I / kBlock : at.n0 / kBlock + 1 < a.row_blocks ? 1 : 0;      // (a half behind the last row: any scale, nothing of it is stored)
+        const int second = kSwiglu ? a.I / kBlock : S::kCols > kBlock && at.n0 / kBlock + 1 < a.row_blocks ? 1 : 0;      // (a half behind the last row: any scale, nothing of it is stored)
         const float* w1 = w0 + (size_t)second * a.blocks;
         const float* x[kOwn];
 #pragma unroll
@@ -760,7 +792,7 @@ cudaError_t product_launch(Args& a, const void* codes, const void* w_codes, int 
   if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
   if (e != cudaSuccess) return e;
   // most tiles that the rows can make
-  const int step = kSwiglu ? 128 : 256;
+  const int step = kSwiglu ? 128 : S::kCols;
   const long long m_tiles = (a.R + (long long)(a.R < a.E ? a.R : a.E) * (S::kRows - 1)) / S::kRows, tiles = m_tiles * (((kSwiglu ? a.I : a.N) + step - 1) / step);
   if (tiles > 0x3fffffffll) return cudaErrorInvalidValue;
   int ctas = S::kCtas;
@@ -828,6 +860,9 @@ int product(const void* codes, const float* scales, const void* w_codes, const f
   //     128 rows                                          105; 52   107; 53   110; 55   113; 57   179; 90   178; 90   249; 130            316; 180  614; 318
   //     256 rows, pairs               137; 68   142; 73   146; 73   157; 77   156; 77   160; 80   163; 83   159; 81   290; 151            284; 161  552; 288
   const long long per = n_rows / n_experts;
+  if constexpr (!kSwiglu) {
+    if (per > 8 && (n_rows + 127ll * (n_rows < n_experts ? n_rows : n_experts)) / 128 * ((n + 255) / 256) <= 74) return product_launch<kNarrow, false>(a, codes, w_codes, K, st) == cudaSuccess ? MOE_OK : MOE_ECUDA;
+  }
   const cudaError_t e = per <= 32    ? product_launch<kFew, kSwiglu>(a, codes, w_codes, K, st)
                         : per <= 384 ? product_launch<kTile, kSwiglu>(a, codes, w_codes, K, st)
                                      : product_launch<kTilePair, kSwiglu>(a, codes, w_codes, K, st);

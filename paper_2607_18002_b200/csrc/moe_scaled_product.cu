@@ -7,8 +7,8 @@
 // epilogue warps read every partial and multiply-add it with its two scales into fp32 registers: one multiply-add and four bytes out of TMEM for 128 products.
 //
 // Forms.  Few rows an expert: weight rows are the M of the instruction, twice 128 TMEM lanes, up to 64 rows its N in steps of 16; one CTA a tile, four partials.  Where such tiles
-// are few, four CTAs, a cluster, share a tile's blocks and add up a part of its rows each.  More rows (tall): 128 rows are the M of a CTA and 256 weight rows its N, or 256 rows that
-// of a pair of CTAs (cta_group::2), each of which holds 128 of either.  A thread then has a row: one multiplier for all of its columns.  The columns are two halves of 128, each
+// are few, four CTAs, a cluster, share a tile's blocks and add up a part of its rows each.  More rows (tall): 128 rows are the M of a CTA and 256 weight rows its N (64 where
+// tiles are few), or 256 rows that of a pair of CTAs (cta_group::2), each of which holds 128 of either.  A thread then has a row: one multiplier for all of its columns.  The columns are two halves of 128, each
 // with buffers and epilogue warps of its own, so that what one half loads and the other adds alternates.
 //
 // Roles: warps 0-7 epilogue, 8 TMA (one thread; a stage is a block of 128 columns: 128-byte rows, swizzled), 9 MMA (one thread), 10 and 11 bring the products of the two scales, four
@@ -50,7 +50,7 @@ struct Shape {
   static constexpr int kRows = kTall ? 128 * kCtas : 64;            // of a tile
   static constexpr int kCols = kForm == kNarrow ? 64 : 256;         // weight rows of a tile
   // Tall: a half of the columns has 64 of the first 128 weight rows and 64 of the second; where one CTA has them all, and their order is free, its share of them in a row
-  [[maybe_unused]] static constexpr bool kMixed = kForm == kTilePair || kSwiglu;
+  static constexpr bool kMixed = kForm == kTilePair || kSwiglu;
   // weight rows and parts (gate, up) of a TMA box, boxes of a stage
   static constexpr int kBoxWeights = kForm == kTilePair ? 128 : !kSwiglu ? kCols : kTall ? 64 : 128, kBoxParts = kSwiglu && kForm != kTilePair ? 2 : 1;
   static constexpr int kBoxes = kForm == kTile && kSwiglu ? 2 : 1;
@@ -167,6 +167,28 @@ __device__ __forceinline__ bool try_at(unsigned saddr, unsigned parity) {
       : "=r"(ok)
       : "r"(saddr), "r"(parity)
       : "memory");
+  return ok != 0;
+}
+// whether the phase is over; the answer is not waited for before it is used
+template <bool kRelaxed = false>
+__device__ __forceinline__ bool test_at(unsigned saddr, unsigned parity) {
+  unsigned ok;
+  if (kRelaxed)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(saddr), "r"(parity)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(saddr), "r"(parity)
+        : "memory");
   return ok != 0;
 }
 // what a wait was for cannot be used before it
@@ -670,22 +692,30 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
           if (kPair) tc_commit_pair(bar);
           else tc_commit(bar);
         };
+        // Small tiles: the barriers of the next block are asked while this one's products are issued, and the answers read when their turn has come; waiting for each in its place takes
+        // some hundred clocks a barrier (16 rows of 4096 x 4096 14.7 us for 11.5).  Where the next buffer is never back that early, asking costs 2-3 %.
+        // (A pair's hand-backs are relaxed arrivals: what they order, the tcgen05 fences on both sides do.)
+        const auto hand_back_of = [&](unsigned n, int h) { return smem_u32(&s.part_empty[n % S::kParts + S::kParts * h]); };
+        constexpr bool kAsk = kForm == kNarrow;
+        unsigned slot = 0, parity = 0;                   // of the stage
+        bool full = false, empty[S::kHalves] = {}, ok = true;      // known to have come
         unsigned n = 0;            // blocks so far
-        bool ok = true;
         for (int t = unit; t < n_tiles && ok; t += n_units) {
           const Tile at = tile_at<S::kRows>(s, a.E, t, kStep);
           const unsigned idesc = kTall ? idesc_of(128 * S::kCtas, S::kHalfCols) : idesc_of(128, (unsigned)(at.rows + 15) & ~15u);
 #pragma unroll 1
-          for (int i = b_first; i < b_last && ok; ++i, ++n) {
-            const unsigned slot = n % S::kStages, round = n / S::kStages, buf = n % S::kParts, use = n / S::kParts;
-            const unsigned st = smem_u32(stages + slot * S::kStageBytes);
+          for (int i = b_first; i < b_last; ++i, ++n) {
+            const unsigned st = smem_u32(stages + slot * S::kStageBytes), buf = n % S::kParts;
+            const unsigned next_slot = slot + 1 == S::kStages ? 0u : slot + 1, next_parity = parity ^ (next_slot == 0);
 #pragma unroll
             for (int h = 0; h < S::kHalves; ++h) {
-              // (a pair's arrivals are relaxed: what they hand back is ordered by the tcgen05 fences on both sides)
-              if (use) ok = ok && wait<kPair ? mbar_try_relaxed : mbar_try>(&s.part_empty[buf + S::kParts * h], (use - 1) & 1, &s.dead);
-              if (h == 0) ok = ok && wait(&s.full[slot], round & 1, &s.dead);
+              if (n >= S::kParts && !empty[h])
+                ok = ok && wait<kPair ? mbar_try_relaxed : mbar_try>(&s.part_empty[buf + S::kParts * h], (n / S::kParts - 1) & 1, &s.dead);
+              if (h == 0 && !full) ok = ok && wait(&s.full[slot], parity, &s.dead);
               if (!ok) break;
               tc_fence_after();
+              if (kAsk && h == 0) full = test_at(smem_u32(&s.full[next_slot]), next_parity);
+              if (kAsk) empty[h] = n + 1 >= S::kParts && test_at<kPair>(hand_back_of(n + 1, h), ((n + 1) / S::kParts - 1) & 1);
               const unsigned d = tmem + (buf + S::kParts * h) * S::kPartCols;
               if (kTall) {
                 mma_block<kPair>(d, umma_desc(st + S::kWBytes, 128), umma_desc(st + h * (S::kWBytes / 2), 128), idesc);
@@ -696,6 +726,9 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
               if (h == S::kHalves - 1) commit(&s.empty[slot]);
               commit(&s.part_full[buf + S::kParts * h]);
             }
+            if (!ok) break;
+            slot = next_slot;
+            parity = next_parity;
           }
         }
         commit(&s.drained);     // nothing of this block's is left in the tensor core when it frees its TMEM
@@ -777,8 +810,13 @@ bool encode(CUtensorMap* out, const void* base, int cols, int rows, int parts, i
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// most tiles that the rows can make
+long long most_tiles(const Args& a, int rows, int cols, int step) {
+  return (a.R + (long long)(a.R < a.E ? a.R : a.E) * (rows - 1)) / rows * (((long long)cols + step - 1) / step);
+}
+
 template <Form kForm, bool kSwiglu>
-cudaError_t product_launch(Args& a, const void* codes, const void* w_codes, int K, cudaStream_t stream) {
+cudaError_t product_launch(Args& a, const void* codes, const void* w_codes, int K, int sms, cudaStream_t stream) {
   using S = Shape<kForm, kSwiglu>;
   static_assert(S::kSmem <= 227 * 1024, "shared memory");
   const int parts = kSwiglu ? 2 : 1;
@@ -786,14 +824,9 @@ cudaError_t product_launch(Args& a, const void* codes, const void* w_codes, int 
       !encode(&a.tm_x, codes, K, a.R, 0, 0, S::kBoxRows, 0))
     return cudaErrorInvalidValue;
   auto* kernel = scaled_product_kernel<kForm, kSwiglu>;
-  int dev = 0, sms = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
   if (e != cudaSuccess) return e;
-  // most tiles that the rows can make
-  const int step = kSwiglu ? 128 : S::kCols;
-  const long long m_tiles = (a.R + (long long)(a.R < a.E ? a.R : a.E) * (S::kRows - 1)) / S::kRows, tiles = m_tiles * (((kSwiglu ? a.I : a.N) + step - 1) / step);
+  const long long tiles = most_tiles(a, S::kRows, kSwiglu ? a.I : a.N, kSwiglu ? 128 : S::kCols);
   if (tiles > 0x3fffffffll) return cudaErrorInvalidValue;
   int ctas = S::kCtas;
   a.split = 1;
@@ -860,12 +893,19 @@ int product(const void* codes, const float* scales, const void* w_codes, const f
   //     128 rows                                          105; 52   107; 53   110; 55   113; 57   179; 90   178; 90   249; 130            316; 180  614; 318
   //     256 rows, pairs               137; 68   142; 73   146; 73   157; 77   156; 77   160; 80   163; 83   159; 81   290; 151            284; 161  552; 288
   const long long per = n_rows / n_experts;
+  // Where tiles of 256 columns would be few, those of 64 are four times as many.  us, one matrix 4096 x 4096, by rows, 64 / 256 columns / few: 16 11.5 / 18.7 / 13.5, 64 12.7 / 19.8 / 20.1,
+  // 256 13.1 / 19.7 / 20.6, 300 22.1 / 19.7 / 21.3; 8 experts, 1024 x 2048, 64 rows 7.9 / 11.6 / 9.0; 200 rows of 9472 x 1024 8.3 / 8.1 / 10.1.
+  int dev = 0, sms = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e != cudaSuccess) return MOE_ECUDA;
   if constexpr (!kSwiglu) {
-    if (per > 8 && (n_rows + 127ll * (n_rows < n_experts ? n_rows : n_experts)) / 128 * ((n + 255) / 256) <= 74) return product_launch<kNarrow, false>(a, codes, w_codes, K, st) == cudaSuccess ? MOE_OK : MOE_ECUDA;
+    if (n_rows > kSplitRows && 4 * most_tiles(a, 128, n, 256) <= sms)
+      return product_launch<kNarrow, false>(a, codes, w_codes, K, sms, st) == cudaSuccess ? MOE_OK : MOE_ECUDA;
   }
-  const cudaError_t e = per <= 32    ? product_launch<kFew, kSwiglu>(a, codes, w_codes, K, st)
-                        : per <= 384 ? product_launch<kTile, kSwiglu>(a, codes, w_codes, K, st)
-                                     : product_launch<kTilePair, kSwiglu>(a, codes, w_codes, K, st);
+  e = per <= 32    ? product_launch<kFew, kSwiglu>(a, codes, w_codes, K, sms, st)
+      : per <= 384 ? product_launch<kTile, kSwiglu>(a, codes, w_codes, K, sms, st)
+                   : product_launch<kTilePair, kSwiglu>(a, codes, w_codes, K, sms, st);
   return e == cudaSuccess ? MOE_OK : MOE_ECUDA;
 }
 

@@ -47,6 +47,14 @@ def test_rows_at_the_borders_of_tiles_and_forms(R):
     _swiglu([0, R], 256, 400)
 
 
+# (tiles of 64 columns up to 37 tiles of 128 rows x 256 columns)
+@pytest.mark.parametrize("offsets,N", [([0, 9], 9472), ([0, 9], 9473), ([0, 129], 4608), ([0, 129], 4865), ([0, 5, 9, 9, 30], 2304), ([0, 128, 256, 384], 3000), ([0, 1, 1, 140], 65)])
+@pytest.mark.parametrize("K", [16, 128, 400, 1152])
+def test_columns_at_the_border_of_narrow_tiles(offsets, N, K):
+    _product(offsets, N, K, "bf16")
+    _product(offsets, N + 3, K, "fp32")
+
+
 # (per expert on average: 32 and 384 are the lines between the forms)
 @pytest.mark.parametrize("offsets", [[0, 3, 3, 1200, 1201, 1600], [0, 900, 900, 2400], [0, 256, 768, 1280], [0, 1, 2, 1400], [0, 30, 400, 401, 640], [0, 63, 64, 65, 120]])
 @pytest.mark.parametrize("K", [128, 272, 1152])

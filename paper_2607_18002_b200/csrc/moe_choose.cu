@@ -360,6 +360,15 @@ __device__ __forceinline__ unsigned keep_groups(const ChooseArgs& a, const float
   return __ballot_sync(kAll, kept);
 }
 
+// Whether all experts of a row are equal by their inputs (a padded token, say): the first ones are chosen then.
+template <class L>
+__device__ __noinline__ bool all_equal(const ChooseArgs& a, const L* row, int lane) {
+  bool same = true;
+#pragma unroll 1
+  for (int e = lane; e < a.E; e += 32) same &= as_float(row[e]) == as_float(row[0]) && (!a.bias || a.bias[e] == a.bias[0]);
+  return __all_sync(kAll, same);
+}
+
 // descending, by compare-exchanges of the largest first
 template <int kN>
 __device__ __forceinline__ void sort_down(int (&v)[kN]) {
@@ -396,7 +405,7 @@ __global__ void __launch_bounds__(kWarps * 32) choose_kernel(const __grid_consta
   constexpr int kInf = 0x7f800000;                 // the key of infinity: those of NaN, which key_of makes positive, are above it
   Norm norm{0.f, 0.f};
   int key[kLists][kList];
-  bool slow = false;
+  bool slow = false, flat = false;
   {
     float z[kPer], c[kPer];
     load_row<L, kPer, kVec>(row, a.E, lane, z);
@@ -434,7 +443,10 @@ __global__ void __launch_bounds__(kWarps * 32) choose_kernel(const __grid_consta
         groups = keep_groups<float>(a, [&](int e) { return space[warp].by_expert[e]; }, lane, close);
         __syncwarp();
       }
-      if (close && !slow) groups = keep_groups_exactly(a, row, (double)norm.top, lane);
+      if (close && !slow) {
+        flat = all_equal(a, row, lane);
+        if (!flat) groups = keep_groups_exactly(a, row, (double)norm.top, lane);
+      }
       const unsigned inverse = ((1u << 20) + size - 1) / size;      // e / size = e inverse >> 20 for e < 2^10
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
@@ -447,7 +459,7 @@ __global__ void __launch_bounds__(kWarps * 32) choose_kernel(const __grid_consta
     }
   }
   int my_id = 0, pos = lane;            // the expert of this lane's slot, and which slot it is
-  if (!slow) {
+  if (!slow && !flat) {
     int head[kLists], at[kLists];
 #pragma unroll
     for (int l = 0; l < kLists; ++l) {
@@ -477,11 +489,14 @@ __global__ void __launch_bounds__(kWarps * 32) choose_kernel(const __grid_consta
           if (kLists == 1 || head[l] == mine) head[l] = ++at[l] < kList ? reinterpret_cast<const int*>(space[warp].sorted[l][lane])[at[l]] : kNone;
       }
     };
-    int m = 0;
+    int m = 0, top = 0;
     for (int j = 0; j < a.k; ++j) {
       const int mine = best();
       m = __reduce_max_sync(kAll, mine | kWhich);
-      if (j == 0 && m > (kInf | kWhich)) slow = true;
+      if (j == 0) {
+        top = m;
+        slow = m > (kInf | kWhich);
+      }
       take(j, mine, m);
     }
     // behind the k-th there follow those that may still be larger, until one is not (or none is left)
@@ -493,6 +508,10 @@ __global__ void __launch_bounds__(kWarps * 32) choose_kernel(const __grid_consta
       m = __reduce_max_sync(kAll, mine | kWhich);
       const float above = of_key(m);                      // nothing that is left is larger
       if (slow || m == (kNone | kWhich) || (a.bias ? above + error_of_any(above) < least || (above == -INFINITY && least > above) : above < least)) break;
+      if (picked == a.k && m == top && all_equal(a, row, lane)) {
+        flat = true;
+        break;
+      }
       if (picked == kMaxK) {            // no lane for one more
         slow = true;
         break;
@@ -504,7 +523,7 @@ __global__ void __launch_bounds__(kWarps * 32) choose_kernel(const __grid_consta
     my_id = expert_of<kVec>(kWhich - (pick.x & kWhich), pick.y);
     // neighbours in the order: surely so, ...
     const float low = of_key(pick.x & ~kWhich), next = __shfl_down_sync(kAll, of_key(pick.x | kWhich), 1);
-    if (!slow && __any_sync(kAll, lane < picked - 1 && !(low - next > (a.bias ? error_of_any(low) + error_of_any(next) : 0.f)))) {
+    if (!slow && !flat && __any_sync(kAll, lane < picked - 1 && !(low - next > (a.bias ? error_of_any(low) + error_of_any(next) : 0.f)))) {
       // ... by their own bounds, or because their inputs are equal?
       const float z = lane < picked ? as_float(row[my_id]) : 0.f, b = a.bias && lane < picked ? a.bias[my_id] : 0.f;
       float c = z, err = 0.f;
@@ -534,6 +553,7 @@ __global__ void __launch_bounds__(kWarps * 32) choose_kernel(const __grid_consta
     }
     if (lane >= picked) pos = kMaxK;
   }
+  if (flat) my_id = pos = lane;
   if (slow) {                           // NaN, or more that are close than a warp has lanes
     my_id = choose_slowly<L, kPer, kVec>(a, row, lane);
     pos = lane;

@@ -63,6 +63,24 @@ def test_ties_go_to_the_lower_index(kind, bias):
         _check(torch.zeros_like(z), 8, kind, b, 8, 2)
 
 
+@pytest.mark.parametrize("kind", ["sigmoid", "softmax"])
+def test_padded_tokens_between_others(kind):
+    """Rows of equal logits (and of nothing but -inf) among others, for k up to 32, with and without a bias and groups."""
+    for E in (40, 64, 256, 300, 1024):
+        z = _logits(50, E, 6)
+        z[::3] = 0.0
+        z[1::9] = -2.5
+        z[4::9] = -float("inf")
+        z[7, :] = 1.0; z[7, E - 1] = 1.0 + 2.0 ** -23
+        z[10, :] = 1.0; z[10, 3] = 1.0 - 2.0 ** -24
+        bias = 0.1 * torch.randn(E, device="cuda", generator=torch.Generator("cuda").manual_seed(E))
+        for b in (None, bias, torch.zeros_like(bias), torch.full_like(bias, 0.3)):
+            for k in (1, 8, 31, 32):
+                _check(z, k, kind, b)
+            _check(z, 8, kind, b, 4, 2)
+            _check(z, 2, kind, b, 10 if E % 10 == 0 else 32 if E % 32 == 0 else 1, 1)
+
+
 def test_signed_zeros_are_equal():
     z = torch.zeros(3, 8, device="cuda")
     z[:, ::2] = -0.0

@@ -298,8 +298,9 @@ def choose_experts(logits, top_k: int, *, scores: str = "softmax", bias=None, gr
         _refuse(f"scores must be one of {sorted(_SCORES)}")
     if bias is not None:
         _plain(bias, "bias", _FP32, (E,), gpu)
-    ids = _empty(T, max(top_k, 0), dtype=_I32, device=logits.device)
-    w = _empty(T, max(top_k, 0), dtype=_FP32, device=logits.device)
+    k = top_k if top_k > 0 else 0               # (the library refuses what is not)
+    device = logits.device
+    ids, w = _empty(T, k, dtype=_I32, device=device), _empty(T, k, dtype=_FP32, device=device)
     rc = (moe._lib or moe.lib()).moe_choose_experts(logits.data_ptr(), step, _DTYPES[logits.dtype], None if bias is None else bias.data_ptr(), T, E, top_k,
                                                     groups, top_groups, group_sum, _SCORES[scores], renormalize, scale, ids.data_ptr(), w.data_ptr(),
                                                     _stream(gpu))
@@ -387,10 +388,11 @@ def _scaled(codes, scales, what, per_row):
     """Codes [..., n, K] with a scale for every 128 columns of a row (per_row) or of 128 rows -> their shape and the number of their GPU."""
     if not isinstance(codes, _Tensor) or not isinstance(scales, _Tensor):
         _refuse(f"the codes and scales of {what} must be tensors")
-    shape, gpu = codes.shape, codes.get_device()
-    if codes.dtype is not _F8 and codes.dtype is not _U8 or scales.dtype is not _FP32 or not codes.is_cuda or gpu != scales.get_device() \
-            or not codes.is_contiguous() or not scales.is_contiguous() or len(shape) < 2 \
-            or scales.shape != (*shape[:-2], shape[-2] if per_row else _blocks(shape[-2]), _blocks(shape[-1])):
+    shape, blocks, gpu, dtype = codes.shape, scales.shape, codes.get_device(), codes.dtype
+    n = len(shape)
+    if dtype is not _F8 and dtype is not _U8 or scales.dtype is not _FP32 or gpu < 0 or gpu != scales.get_device() \
+            or not codes.is_contiguous() or not scales.is_contiguous() or n < 2 or len(blocks) != n or blocks[n - 1] != (shape[n - 1] + 127) // 128 \
+            or blocks[n - 2] != (shape[n - 2] if per_row else (shape[n - 2] + 127) // 128) or n > 2 and shape[:n - 2] != blocks[:n - 2]:
         _refuse(f"the codes and scales of {what} must be contiguous e4m3 (or uint8) and fp32 tensors on one GPU, a scale for 128 columns "
                 f"of {'a row' if per_row else '128 rows'}")
     return shape, gpu
@@ -400,15 +402,17 @@ def scaled_dequantize(codes, scales, dtype=_BF16, stream=None):
     """The values [..., n, K] that codes stand for with the scales of rows [..., n, ceil(K/128)] or of weights [..., ceil(n/128), ceil(K/128)]."""
     if dtype not in _DTYPES:
         _refuse(f"dtype must be one of {sorted(map(str, _DTYPES))}")
-    if isinstance(codes, _Tensor) and codes.dim() == 1:
+    if isinstance(codes, _Tensor) and isinstance(scales, _Tensor) and codes.dim() == 1:
         return scaled_dequantize(codes[None], scales[None], dtype, stream)[0]
     per_row = isinstance(codes, _Tensor) and isinstance(scales, _Tensor) and codes.dim() > 1 and scales.dim() > 1 and scales.shape[-2] == codes.shape[-2]
-    (*lead, n, K), gpu = _scaled(codes, scales, "the values", per_row)
+    shape, gpu = _scaled(codes, scales, "the values", per_row)
     if stream is not None or gpu != _current_device():
         return _elsewhere(scaled_dequantize, codes.device, stream, codes, scales, dtype)
-    out = _empty(codes.shape, dtype=dtype, device=codes.device)
-    if out.numel():
-        rc = (moe._lib or moe.lib()).moe_scaled_dequantize(codes.data_ptr(), scales.data_ptr(), out.numel() // (n * K), n, K, 1 if per_row else 128,
+    out = _empty(*shape, dtype=dtype, device=codes.device)
+    values = out.numel()
+    if values:
+        n, K = shape[-2], shape[-1]
+        rc = (moe._lib or moe.lib()).moe_scaled_dequantize(codes.data_ptr(), scales.data_ptr(), values // (n * K), n, K, 1 if per_row else 128,
                                                            _DTYPES[dtype], out.data_ptr(), _stream(gpu))
         if rc:
             _failed(rc, "moe_scaled_dequantize")
@@ -419,15 +423,17 @@ def _scaled_operands(codes, scales, w_codes, w_scales, offsets):
     """-> number of the GPU, R, E, n, K, address of the offsets"""
     shape, gpu = _scaled(codes, scales, "the rows", True)
     w_shape, w_gpu = _scaled(w_codes, w_scales, "the weights", False)
-    if len(shape) != 2 or len(w_shape) not in (2, 3) or w_shape[-1] != shape[1] or w_gpu != gpu:
+    dims = len(w_shape)
+    if len(shape) != 2 or dims > 3 or w_shape[dims - 1] != shape[1] or w_gpu != gpu:
         _refuse(f"rows must be [R, K] and weights [E, n, K] or [n, K], all on cuda:{gpu}")
-    E = w_shape[0] if len(w_shape) == 3 else 1
-    if offsets is None:
-        if E != 1:
-            _refuse("more than one matrix needs offsets")
-    else:
+    E = w_shape[0] if dims == 3 else 1
+    at = None
+    if offsets is not None:
         _index(offsets, "offsets", E + 1, gpu)
-    return gpu, shape[0], E, w_shape[-2], shape[1], None if offsets is None else offsets.data_ptr()
+        at = offsets.data_ptr()
+    elif E != 1:
+        _refuse("more than one matrix needs offsets")
+    return gpu, shape[0], E, w_shape[dims - 2], shape[1], at
 
 
 def scaled_product(codes, scales, w_codes, w_scales, offsets=None, dtype=_BF16, stream=None):

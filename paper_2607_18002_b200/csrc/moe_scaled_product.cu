@@ -8,7 +8,7 @@
 //
 // Forms.  Few rows an expert: weight rows are the M of the instruction, twice 128 TMEM lanes, up to 64 rows its N in steps of 16; one CTA a tile, four partials.  Where such tiles
 // are few, four CTAs, a cluster, share a tile's blocks and add up a part of its rows each.  More rows (tall): 128 rows are the M of a CTA and 256 weight rows its N (64 where
-// tiles are few), or 256 rows that of a pair of CTAs (cta_group::2), each of which holds 128 of either.  A thread then has a row: one multiplier for all of its columns.  The columns are two halves of 128, each
+// tiles are few; for swiglu the four CTAs that have a block of 128 outputs are a cluster and tell one another their rows' largest magnitudes), or 256 rows that of a pair of CTAs (cta_group::2), each of which holds 128 of either.  A thread then has a row: one multiplier for all of its columns.  The columns are two halves of 128, each
 // with buffers and epilogue warps of its own, so that what one half loads and the other adds alternates.
 //
 // Roles: warps 0-7 epilogue, 8 TMA (one thread; a stage is a block of 128 columns: 128-byte rows, swizzled), 9 MMA (one thread), 10 and 11 bring the products of the two scales, four
@@ -18,6 +18,8 @@
 // columns 560-600, at 1 000 W and 1.46 GHz.  Without loads from TMEM and additions the same launch takes 0.81 of that, without the additions alone 0.84.
 // Every wait is bounded (2 s); where one runs out the launch ends, after another such limit for its copies in flight, and what it has not computed is NaN.
 #include <cuda_fp16.h>
+
+#include <type_traits>
 
 #include "moe_dev.cuh"
 #include "moe_grouped.cuh"
@@ -32,14 +34,14 @@ constexpr int kTmaWarp = 8, kMmaWarp = 9, kScaleWarp = 10, kScaleThreads = 64;
 constexpr int kBlock = kScaledBlock;
 constexpr int kSplit = 4, kSplitRows = 8;       // CTAs that share a tile's blocks, and its most rows
 constexpr int kQuad = 4;                        // blocks whose scales are handed over together
-constexpr int kTurnPitch = 128 + 16, kTurnBytes = 32 * kTurnPitch;      // outputs on their way out: 32 rows of a warp; the 16 bytes spread eight of them over all banks
 constexpr int kQuads = 4;                       // ... of them in the ring
+constexpr int kTurnPitch = 128 + 16, kTurnBytes = 32 * kTurnPitch;      // outputs on their way out: 32 rows of a warp; the 16 bytes spread eight of them over all banks
 
 struct Shared : Segments {
   unsigned long long full[8], empty[8], part_full[8], part_empty[8], scales_full[kQuads], scales_empty[kQuads], drained;
   unsigned tmem;
   volatile int dead;             // a wait ran out
-  unsigned tops[2][2][128];      // swiglu: largest magnitudes on their way from warp to warp
+  unsigned tops[4][2][128];      // swiglu: largest magnitudes on their way from warp to warp (narrow tiles: from CTA to CTA)
 };
 
 enum Form { kFew, kNarrow, kTile, kTilePair };
@@ -48,12 +50,13 @@ struct Shape {
   static constexpr bool kTall = kForm != kFew;
   static constexpr int kCtas = kForm == kTilePair ? 2 : 1;
   static constexpr int kRows = kTall ? 128 * kCtas : 64;            // of a tile
-  static constexpr int kCols = kForm == kNarrow ? 64 : 256;         // weight rows of a tile
+  static constexpr int kCols = kForm == kNarrow ? 64 : 256;         // weight rows of a tile; narrow ones for swiglu: of one of the four CTAs that have a block of outputs
+  static constexpr bool kQuarter = kForm == kNarrow && kSwiglu;
   // Tall: a half of the columns has 64 of the first 128 weight rows and 64 of the second; where one CTA has them all, and their order is free, its share of them in a row
   static constexpr bool kMixed = kForm == kTilePair || kSwiglu;
   // weight rows and parts (gate, up) of a TMA box, boxes of a stage
-  static constexpr int kBoxWeights = kForm == kTilePair ? 128 : !kSwiglu ? kCols : kTall ? 64 : 128, kBoxParts = kSwiglu && kForm != kTilePair ? 2 : 1;
-  static constexpr int kBoxes = kForm == kTile && kSwiglu ? 2 : 1;
+  static constexpr int kBoxWeights = kForm == kTilePair ? 128 : !kSwiglu ? kCols : kTall ? kCols / 4 : 128, kBoxParts = kSwiglu && kForm != kTilePair ? 2 : 1;
+  static constexpr int kBoxes = (kForm == kTile || kForm == kNarrow) && kSwiglu ? 2 : 1;
   static constexpr int kMine = kRows / kCtas;                       // ... in this CTA
   static constexpr int kWBytes = kCols / kCtas * kBlock, kXBytes = kMine * kBlock, kStageBytes = kWBytes + kXBytes;
   static constexpr int kBoxRows = kTall ? 64 : 32;                  // of a TMA box of rows
@@ -158,6 +161,9 @@ __device__ __forceinline__ void meet() {
 __device__ __forceinline__ void st_cluster_f(unsigned cluster_addr, float v) {
   asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(cluster_addr), "f"(v) : "memory");
 }
+__device__ __forceinline__ void st_cluster_u(unsigned cluster_addr, unsigned v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr), "r"(v) : "memory");
+}
 __device__ __forceinline__ bool try_at(unsigned saddr, unsigned parity) {
   unsigned ok;
   asm volatile(
@@ -245,9 +251,10 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
   const unsigned rank = kPair ? cluster_ctarank() : 0u;
   // Few tiles of a few rows: the CTAs of a cluster have a part of the blocks each (b_first to b_last), and at the end a part of the rows, which they add up.  A cluster
   // has one tile at most.
-  const int split = kForm == kFew ? a.split : 1, part_of = kForm == kFew && split > 1 ? (int)cluster_ctarank() : 0;
-  const int b_first = part_of * a.blocks / split, b_last = (part_of + 1) * a.blocks / split;
-  const int ctas = kForm == kFew ? split : S::kCtas, unit = (int)blockIdx.x / ctas, n_units = (int)gridDim.x / ctas;
+  const int split = kForm == kFew ? a.split : 1, part_of = S::kQuarter || (kForm == kFew && split > 1) ? (int)cluster_ctarank() : 0;
+  const int b_first = S::kQuarter ? 0 : part_of * a.blocks / split, b_last = S::kQuarter ? a.blocks : (part_of + 1) * a.blocks / split;
+  const bool meets = S::kQuarter || (kForm == kFew && split > 1);      // twice, at the end of the tile
+  const int ctas = S::kQuarter ? kSplit : kForm == kFew ? split : S::kCtas, unit = (int)blockIdx.x / ctas, n_units = (int)gridDim.x / ctas;
   const int n_blocks = ((kSwiglu ? a.I : a.N) + kStep - 1) / kStep;
 
   if (tid == 0) {
@@ -341,7 +348,11 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
             next_partial();
             hand_back();
           }
-          if (kSwiglu) {
+          if (S::kQuarter) {
+            meet();
+            meet();
+            met = true;
+          } else if (kSwiglu) {
             ++turn;
             bar_sync(1 + quarter, 64);
           }
@@ -358,7 +369,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
             for (int u = 0; u < 2; ++u) {
               const int b = b0 + u;
               if (b >= a.blocks) break;
-              const float m = ld_shared_f(sc);
+              const float m0 = ld_shared_f(sc), m1 = kSwiglu ? ld_shared_f(sc + 4 * S::kMine) : m0;
               sc += 8 * S::kMine;
               const bool more = b < a.blocks - 1;
               tc_wait_ld();
@@ -373,9 +384,9 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
                 if (!ok) break;
                 tc_ld32(from, v[u ^ 1]);
               }
-              const unsigned long long two = f32x2(m, m);
+              const unsigned long long s0 = f32x2(m0, m0), s1 = f32x2(m1, m1);
 #pragma unroll
-              for (int j = 0; j < 16; ++j) sum[j] = fma_f32x2(f32x2(__uint_as_float(v[u][2 * j]), __uint_as_float(v[u][2 * j + 1])), two, sum[j]);
+              for (int j = 0; j < 16; ++j) sum[j] = fma_f32x2(f32x2(__uint_as_float(v[u][2 * j]), __uint_as_float(v[u][2 * j + 1])), j < 8 ? s0 : s1, sum[j]);
             }
         } else {
           // 64 columns are on their way or being added at any time: a wait is for all loads before it, so there are two a block, and the next block's first
@@ -431,24 +442,36 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
           acc[2 * i + 1] = two.y;
         }
         if constexpr (kSwiglu) {
+          constexpr int kOuts = S::kHalfCols / 2;
           unsigned top = 0u;
 #pragma unroll
-          for (int i = 0; i < 64; ++i) {
-            acc[i] = silu_times(acc[i], acc[64 + i]);
+          for (int i = 0; i < kOuts; ++i) {
+            acc[i] = silu_times(acc[i], acc[kOuts + i]);
             top = max(top, __float_as_uint(acc[i]) & 0x7fffffffu);
           }
-          s.tops[turn & 1][half][mine] = top;
-          bar_sync(1 + quarter, 64);
-          top = max(top, s.tops[turn++ & 1][half ^ 1][mine]);
+          if constexpr (S::kQuarter) {       // the row's other outputs are with the other half, and with three other CTAs, which are known to run once they have met
+            if (!ok) top = 0x7fffffffu;
+            meet();
+#pragma unroll
+            for (int to = 0; to < kSplit; ++to) st_cluster_u(map_address(smem_u32(&s.tops[part_of][half][mine]), to), top);
+            meet();
+            met = true;
+#pragma unroll
+            for (int i = 0; i < 2 * kSplit; ++i) top = max(top, s.tops[i / 2][i % 2][mine]);
+          } else {
+            s.tops[turn & 1][half][mine] = top;
+            bar_sync(1 + quarter, 64);
+            top = max(top, s.tops[turn++ & 1][half ^ 1][mine]);
+          }
           const float scale = ok ? scaled_scale(top) : __uint_as_float(0x7fffffffu), inv = __fdividef(1.f, scale);
           if (valid) {
-            uint4* to = reinterpret_cast<uint4*>(static_cast<unsigned char*>(a.out) + p * a.I + at.n0 + 64 * half);
+            uint4* to = reinterpret_cast<uint4*>(static_cast<unsigned char*>(a.out) + p * a.I + at.n0 + (S::kQuarter ? 32 * part_of : 0) + kOuts * half);
 #pragma unroll
-            for (int i = 0; i < 64; ++i) acc[i] *= inv;
+            for (int i = 0; i < kOuts; ++i) acc[i] *= inv;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < kOuts / 16; ++i)
               to[i] = make_uint4(e4m3_codes4(acc + 16 * i), e4m3_codes4(acc + 16 * i + 4), e4m3_codes4(acc + 16 * i + 8), e4m3_codes4(acc + 16 * i + 12));
-            if (half == 0) a.out_scales[p * (a.I / kBlock) + at.n0 / kBlock] = scale;
+            if (half == 0 && (!S::kQuarter || part_of == 0)) a.out_scales[p * (a.I / kBlock) + at.n0 / kBlock] = scale;
           }
         } else {
           if (!ok) {
@@ -628,7 +651,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
         }
       }
     }
-    if (kForm == kFew && split > 1 && !met) {             // (no tile)
+    if (meets && !met) {             // (no tile)
       meet();
       meet();
     }
@@ -660,7 +683,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
           const int row0 = at.row0 + (int)rank * S::kMine, mine = min(S::kMine, at.rows - (int)rank * S::kMine);
           const int boxes = mine > 0 ? (mine + S::kBoxRows - 1) / S::kBoxRows : 0;
           const unsigned long long policy = at.alone ? l2_evict_first() : l2_evict_normal();
-          const int n0 = at.n0 + (kSwiglu ? 0 : 128 * (int)rank), which = kSwiglu ? (int)rank : 0;      // (rank is 0 where there is no pair)
+          const int n0 = at.n0 + (S::kQuarter ? 32 * part_of : kSwiglu ? 0 : 128 * (int)rank), which = kSwiglu ? (int)rank : 0;      // (rank is 0 where there is no pair)
 #pragma unroll 1
           for (int i = b_first; i < b_last; ++i, ++n) {
             const unsigned slot = n % S::kStages, round = n / S::kStages;
@@ -783,7 +806,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
         }
       }
     }
-    if (kForm == kFew && split > 1) {
+    if (meets) {
       meet();
       meet();
     }
@@ -828,7 +851,7 @@ cudaError_t product_launch(Args& a, const void* codes, const void* w_codes, int 
   if (e != cudaSuccess) return e;
   const long long tiles = most_tiles(a, S::kRows, kSwiglu ? a.I : a.N, kSwiglu ? 128 : S::kCols);
   if (tiles > 0x3fffffffll) return cudaErrorInvalidValue;
-  int ctas = S::kCtas;
+  int ctas = S::kQuarter ? kSplit : S::kCtas;
   a.split = 1;
   if (kForm == kFew) {
     // Clusters of four share the blocks as long as all of them fit (32 do; 36 take a second round).  us, one row, alone / shared, by weight rows: K 4096: 2048 13.7 / 6.9,
@@ -894,15 +917,14 @@ int product(const void* codes, const float* scales, const void* w_codes, const f
   //     256 rows, pairs               137; 68   142; 73   146; 73   157; 77   156; 77   160; 80   163; 83   159; 81   290; 151            284; 161  552; 288
   const long long per = n_rows / n_experts;
   // Where tiles of 256 columns would be few, those of 64 are four times as many.  us, one matrix 4096 x 4096, by rows, 64 / 256 columns / few: 16 11.5 / 18.7 / 13.5, 64 12.7 / 19.8 / 20.1,
-  // 256 13.1 / 19.7 / 20.6, 300 22.1 / 19.7 / 21.3; 8 experts, 1024 x 2048, 64 rows 7.9 / 11.6 / 9.0; 200 rows of 9472 x 1024 8.3 / 8.1 / 10.1.
+  // 256 13.1 / 19.7 / 20.6, 300 22.1 / 19.7 / 21.3; 8 experts, 1024 x 2048, 64 rows 7.9 / 11.6 / 9.0; 200 rows of 9472 x 1024 8.3 / 8.1 / 10.1.  Gate/up, four CTAs a block of outputs:
+  // 4096 x 4096, 16 rows 12.3 / 19.9 / 14.1, 64 13.5 / 20.1 / 19.7, 512 of 2048 13.8 / 20.5 / 19.9; 8 experts, 1024 x 2048, 64 rows 8.9 / 12.6 / 9.5.
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return MOE_ECUDA;
-  if constexpr (!kSwiglu) {
-    if (n_rows > kSplitRows && 4 * most_tiles(a, 128, n, 256) <= sms)
-      return product_launch<kNarrow, false>(a, codes, w_codes, K, sms, st) == cudaSuccess ? MOE_OK : MOE_ECUDA;
-  }
+  if (n_rows > kSplitRows && (kSwiglu ? most_tiles(a, 128, n / 2, 128) <= 32 && sms >= 32 * kSplit : 4 * most_tiles(a, 128, n, 256) <= sms))
+    return product_launch<kNarrow, kSwiglu>(a, codes, w_codes, K, sms, st) == cudaSuccess ? MOE_OK : MOE_ECUDA;
   e = per <= 32    ? product_launch<kFew, kSwiglu>(a, codes, w_codes, K, sms, st)
       : per <= 384 ? product_launch<kTile, kSwiglu>(a, codes, w_codes, K, sms, st)
                    : product_launch<kTilePair, kSwiglu>(a, codes, w_codes, K, sms, st);

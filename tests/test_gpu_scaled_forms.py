@@ -55,6 +55,14 @@ def test_columns_at_the_border_of_narrow_tiles(offsets, N, K):
     _product(offsets, N + 3, K, "fp32")
 
 
+# (gate/up: 32 outputs a CTA in up to 32 tiles of 128 rows x 128 outputs)
+@pytest.mark.parametrize("offsets,I", [([0, 9], 128), ([0, 64], 4096), ([0, 64], 4224), ([0, 129], 2048), ([0, 129], 2176), ([0, 5, 9, 9, 30], 384), ([0, 128, 256, 384], 512),
+                                       ([0, 1, 1, 140], 256), ([0, 300], 128)])
+@pytest.mark.parametrize("K", [16, 128, 400, 1152])
+def test_gate_up_tiles_of_a_quarter(offsets, I, K):
+    _swiglu(offsets, I, K)
+
+
 # (per expert on average: 32 and 384 are the lines between the forms)
 @pytest.mark.parametrize("offsets", [[0, 3, 3, 1200, 1201, 1600], [0, 900, 900, 2400], [0, 256, 768, 1280], [0, 1, 2, 1400], [0, 30, 400, 401, 640], [0, 63, 64, 65, 120]])
 @pytest.mark.parametrize("K", [128, 272, 1152])

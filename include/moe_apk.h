@@ -390,7 +390,8 @@ int moe_scaled_dequantize(const void* codes, const float* scales, int32_t n_expe
  *   moe_scaled_product  out[p, :] = rows[p, :] . w[e]^T, rounded once to dtype (BF16, FP16 or FP32)
  *   moe_scaled_swiglu   weights [E, 2*inter, K], gate rows first: silu(gate) * up, computed in fp32 and quantised as by moe_scaled_quantize (codes: of a
  *                       quotient that is off by some steps of fp32; 0 for gates below -87.3): codes [R, inter], scales [R, inter/128], the rows of the down product
- * The products of a block of 128 columns are added up in the tensor core, the blocks with their scales in fp32.  Rows that belong to no expert are 0
+ * The products of a block of 128 columns are added up in the tensor core, the blocks with their scales in fp32. (Products of a row's and a weight's scale must be
+ * numbers of fp32.)  Rows that belong to no expert are 0
  * (swiglu: codes 0, scales 1).  The gradient of a product to its rows is a product with the transposed codes and scales.
  * k_cols a multiple of 16, inter of 128, n_cols >= 1, all at most 2^30 (inter 2^29), R < 2^27, E <= 1024; codes, w_codes and out_codes 16-byte, the others
  * 4-byte aligned (out: to its elements), else MOE_EINVAL.  No context, no workspace.  Each wait inside the kernel is bounded (2 s); what a launch that gave

@@ -284,7 +284,7 @@ int moe_scaled_quantize(const void* x, int64_t x_stride, int32_t dtype, int32_t 
   if (!sorted_to_flat != !flat_to_sorted || (!flat_to_sorted && top_k != 1)) return MOE_EINVAL;
   if (flat_to_sorted && (long long)n_tokens * top_k >= (1ll << kRowSlotShift)) return MOE_EINVAL;
   const long long all = (long long)n_tokens * blocks_of(cols);
-  if (all >= (1ll << 32) || !x || !codes || !scales || x_stride < cols) return MOE_EINVAL;
+  if (all > (1ll << 32) - kThreads || !x || !codes || !scales || x_stride < cols) return MOE_EINVAL;
   if (misaligned(x, dtype == MOE_DTYPE_FP32 ? 4 : 2) || misaligned(codes, 16) || misaligned(scales, 4) || misaligned(sorted_to_flat, 4) ||
       misaligned(flat_to_sorted, 4))
     return MOE_EINVAL;

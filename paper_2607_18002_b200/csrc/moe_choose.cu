@@ -668,15 +668,17 @@ __global__ void __launch_bounds__(kWarps * 32) choose_grad_kernel(const __grid_c
 int bytes_of(int dtype) { return dtype == MOE_DTYPE_FP32 ? 4 : dtype == MOE_DTYPE_BF16 || dtype == MOE_DTYPE_FP16 ? 2 : 0; }
 bool misaligned(const void* p, unsigned to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 
-// Experts a lane: 4 up to 128 experts, 8 up to 256, 32 beyond.
+// Experts a lane: 4 up to 128 experts, 8 up to 256, 16 up to 512, 32 beyond.  (us, 16 384 tokens of 384 experts, 16 / 32 a lane: the best eight of all 17 / 30, with scores and a
+// bias 23 / 41, of four of eight groups 37 / 60, the gradient 10 / 13; one token 2.6 / 3.3.)
 template <template <class, int, bool> class Kernel, class Args>
 cudaError_t launch(const Args& a, int dtype, bool vec, cudaStream_t stream) {
-  const int blocks = (a.T + kWarps - 1) / kWarps;
+  const int blocks = (a.T - 1) / kWarps + 1;
   const auto go = [&](auto* kernel) { return launch_after(kernel, blocks, kWarps * 32, 0, stream, a); };
   const auto of = [&](auto type) {
     using L = decltype(type);
     if (a.E <= 128) return vec ? go(Kernel<L, 4, true>::fn) : go(Kernel<L, 4, false>::fn);
     if (a.E <= 256) return vec ? go(Kernel<L, 8, true>::fn) : go(Kernel<L, 8, false>::fn);
+    if (a.E <= 512) return vec ? go(Kernel<L, 16, true>::fn) : go(Kernel<L, 16, false>::fn);
     return vec ? go(Kernel<L, 32, true>::fn) : go(Kernel<L, 32, false>::fn);
   };
   return dtype == MOE_DTYPE_FP32 ? of(float{}) : dtype == MOE_DTYPE_FP16 ? of(__half{}) : of(__nv_bfloat16{});

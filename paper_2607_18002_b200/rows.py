@@ -298,6 +298,8 @@ def choose_experts(logits, top_k: int, *, scores: str = "softmax", bias=None, gr
         _refuse(f"scores must be one of {sorted(_SCORES)}")
     if bias is not None:
         _plain(bias, "bias", _FP32, (E,), gpu)
+    if (T | top_k | groups | top_groups | group_sum) >> 31 > 0:
+        _refuse("the tokens, top_k and groups must be below 2^31")
     k = top_k if top_k > 0 else 0               # (the library refuses what is not)
     device = logits.device
     ids, w = _empty(T, k, dtype=_I32, device=device), _empty(T, k, dtype=_FP32, device=device)
@@ -323,6 +325,8 @@ def choose_experts_grad(logits, topk_ids, d_topk_w, *, scores: str = "softmax", 
     k = topk_ids.shape[1]
     _plain(topk_ids, "topk_ids", _I32, (T, k), gpu)
     _plain(d_topk_w, "d_topk_w", _FP32, (T, k), gpu)
+    if T >> 31:
+        _refuse("there must be fewer than 2^31 tokens")
     dz = logits.new_empty(T, E)
     rc = (moe._lib or moe.lib()).moe_choose_experts_grad(logits.data_ptr(), step, _DTYPES[logits.dtype], topk_ids.data_ptr(), d_topk_w.data_ptr(), T, E, k,
                                                          _SCORES[scores], renormalize, scale, dz.data_ptr(), _stream(gpu))

@@ -225,3 +225,26 @@ def test_no_tokens_another_stream_and_a_graph():
     graph.replay()
     want = moe.choose_experts(z, 4, scores="sigmoid", bias=b)
     assert torch.equal(ids, want[0]) and torch.equal(w, want[1])
+
+
+@pytest.mark.parametrize("kind", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("E,groups,top_groups", [(260, 1, 1), (384, 8, 4), (511, 7, 3), (512, 8, 4), (512, 4, 1), (512, 32, 5), (513, 1, 1)])
+def test_some_hundred_experts(kind, E, groups, top_groups):
+    test_choice_and_weights(kind, 70, E, 8, groups, top_groups, "fp32")
+    zero = torch.zeros(E, device="cuda")
+    for sigma in (0.0, 1e-3, 40.0):       # equal by their inputs, hardly different, far apart with most scores tiny: more that are close than a warp has lanes
+        z = _logits(40, E, E, sigma=sigma)
+        _check(z, 8, kind, zero, groups, top_groups)
+        _check(z, 8, kind, None, groups, top_groups, group_sum=1)
+    for renormalize in (True, False):
+        test_gradient_against_its_formula(kind, renormalize, 33, E, 8, "bf16")
+
+
+def test_sizes_that_do_not_fit_32_bits_are_refused():
+    z = torch.zeros(6, 8, device="cuda")
+    for bad in (dict(top_k=2, groups=2**32 + 1), dict(top_k=2, groups=2, top_groups=2**32 + 1), dict(top_k=2, group_sum=2**32 + 1), dict(top_k=2**32 + 1)):
+        with pytest.raises(ValueError):
+            moe.choose_experts(z, **bad)
+    z = torch.empty(2**31, 1, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(ValueError):
+        moe.choose_experts(z, 1)

@@ -14,8 +14,8 @@
 // Roles: warps 0-7 epilogue, 8 TMA (one thread; a stage is a block of 128 columns: 128-byte rows, swizzled), 9 MMA (one thread), 10 and 11 bring the products of the two scales, four
 // blocks at a time, into a ring in shared memory.
 // What bounds them: few rows, the weight stream (100 tokens on 128 experts: gate/up 302 us, 6.2 TB/s; one CTA streams 97 GB/s); many, power and the way of a partial from the tensor core to
-// the epilogue and back: 8192 x 4096 x 4096 133-140 us (2.0 PFLOP/s, tensor pipe 53 % of the cycles), 65 536 rows of 64 experts, K 4096, 3584 gate/up rows 1 040-1 110 us, K 1792, 4096
-// columns 560-600, at 1 000 W and 1.46 GHz.  Without loads from TMEM and additions the same launch takes 0.81 of that, without the additions alone 0.84.
+// the epilogue and back: 8192 x 4096 x 4096 130-140 us (2.0 PFLOP/s, tensor pipe 53 % of the cycles), 65 536 rows of 64 experts, K 4096, 3584 gate/up rows 1 040-1 110 us, K 1792, 4096
+// columns 545-580, at 1 000 W and 1.46 GHz.  Without loads from TMEM and additions the same launch takes 0.81 of that, without the additions alone 0.84.
 // Every wait is bounded (2 s); where one runs out the launch ends, after another such limit for its copies in flight, and what it has not computed is NaN.
 #include <cuda_fp16.h>
 
@@ -35,7 +35,7 @@ constexpr int kBlock = kScaledBlock;
 constexpr int kSplit = 4, kSplitRows = 8;       // CTAs that share a tile's blocks, and its most rows
 constexpr int kQuad = 4;                        // blocks whose scales are handed over together
 constexpr int kQuads = 4;                       // ... of them in the ring
-constexpr int kTurnPitch = 128 + 16, kTurnBytes = 32 * kTurnPitch;      // outputs on their way out: 32 rows of a warp; the 16 bytes spread eight of them over all banks
+constexpr int kTurnBytes = 32 * 128;            // outputs on their way out: 128 bytes of 32 rows of a warp, swizzled as TMA does
 
 struct Shared : Segments {
   unsigned long long full[8], empty[8], part_full[8], part_empty[8], scales_full[kQuads], scales_empty[kQuads], drained;
@@ -66,7 +66,8 @@ struct Shape {
   static constexpr int kParts = kForm == kNarrow || !kTall ? 4 : 2; // of a half
   static constexpr int kScaleFloats = kQuad * 2 * kMine;            // of a place in the ring: [block][half][row]
   static constexpr int kScaleBytes = kQuads * kScaleFloats * 4;
-  static constexpr int kOutBytes = kTall && !kSwiglu ? 8 * kTurnBytes : 0;
+  static constexpr int kTurns = kForm == kTilePair ? 2 : 1;         // ... of a warp (pairs: four stages are left; one, and five: 599 -> 611 us)
+  static constexpr int kOutBytes = kTall && !kSwiglu ? 8 * kTurns * kTurnBytes : 0;
   static constexpr int kStages = (227 * 1024 - 1024 - (int)sizeof(Shared) - kScaleBytes - kOutBytes) / kStageBytes;
   static constexpr int kSmem = 1024 + kStages * kStageBytes + kScaleBytes + kOutBytes + (int)sizeof(Shared);
   static_assert(kStages >= 3 && kStages <= 8 && kHalves * kParts <= 8 && kHalves * kParts * kPartCols <= 512, "barriers, TMEM");
@@ -75,6 +76,7 @@ struct Shape {
 struct Args {
   CUtensorMap tm_w;              // [E][parts][rows][K], parts: gate and up for swiglu, else 1
   CUtensorMap tm_x;              // [R][K]
+  CUtensorMap tm_out;            // [R][N] as bytes
   const float* x_scales;         // [R, blocks]
   const float* w_scales;         // [E, row_blocks, blocks]
   const int* offsets;            // [E + 1], or NULL: one matrix for all rows
@@ -83,6 +85,7 @@ struct Args {
   int R, E, N, I;                // N: weight rows; I: N / 2 for swiglu
   int blocks, row_blocks;
   int dtype, wide;               // of out; its rows are 16-byte aligned
+  int by_tma;                    // tm_out is there
   int wide_scales;               // four scales of a row can be loaded at once
   int split;                     // kSplit: so many CTAs, a cluster, share the blocks of a tile; else 1
 };
@@ -197,6 +200,16 @@ __device__ __forceinline__ bool test_at(unsigned saddr, unsigned parity) {
         : "memory");
   return ok != 0;
 }
+// 128 bytes of 32 rows out of shared memory; the thread that asks is the one that waits
+__device__ __forceinline__ void tma_store(const CUtensorMap* m, int x, int y, unsigned from) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(reinterpret_cast<unsigned long long>(m)), "r"(x), "r"(y), "r"(from)
+               : "memory");
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+// all but the last kLeft of this thread's have been read from shared memory
+template <int kLeft>
+__device__ __forceinline__ void tma_stores_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kLeft) : "memory"); }
+__device__ __forceinline__ void tma_stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 // what a wait was for cannot be used before it
 __device__ __forceinline__ void loaded(unsigned (&r)[16]) {
   asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]),
@@ -478,44 +491,66 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
 #pragma unroll
             for (int i = 0; i < S::kHalfCols; ++i) acc[i] = __uint_as_float(0x7fffffffu);
           }
-          // A warp turns its 32 rows round in shared memory, 128 bytes of each at a time, so that its stores are 128 bytes of four rows.  (16 bytes of 32 rows a
-          // store: 4 000 clocks a tile.)
-          const unsigned own = smem_u32(turned + warp * kTurnBytes);
-          const int rows = min(32, at.rows - 128 * (int)rank - 32 * quarter);
+          // A warp turns its 32 rows round in shared memory, 128 bytes of each at a time.  Where all 32 are the tile's, TMA takes them from there while the next tile's
+          // sums begin (down product of 65 536 rows, K 1792, over and over 599 -> 577 us); else the warp stores 128 bytes of four rows at a time.
+          const unsigned own = smem_u32(turned + warp * S::kTurns * kTurnBytes);
+          const int row_out = at.row0 + 128 * (int)rank + 32 * quarter, rows = min(32, at.rows - 128 * (int)rank - 32 * quarter);
+          const bool by_tma = kForm != kNarrow && a.by_tma && rows == 32;
           with_type(a.dtype, a.out, [&](auto* out) {
             using E = typename std::remove_pointer<decltype(out)>::type;
             constexpr int kIn = 16 / (int)sizeof(E), kCols = S::kHalfCols < 128 / (int)sizeof(E) ? S::kHalfCols : 128 / (int)sizeof(E);
             constexpr int kPieces = kCols / kIn;           // 16-byte pieces of a row at a time
-            out += (size_t)(at.row0 + 128 * (int)rank + 32 * quarter) * a.N;
+            out += (size_t)row_out * a.N;
 #pragma unroll
             for (int c = 0; c < S::kHalfCols / kCols; ++c) {
               const int col0 = at.n0 + (S::kMixed ? 128 * (c * kCols / 64) + 64 * half + c * kCols % 64 : S::kHalfCols * half + c * kCols), cols = min(kCols, a.N - col0);
+              if (cols <= 0) break;                        // (so that every pass so far has had its store, which the waits count)
+              const unsigned turn_at = own + c % S::kTurns * kTurnBytes;
+              const auto piece = [&](int r, int i) { return turn_at + 128 * r + 16 * (i ^ (r & 7)); };
+              if (kForm != kNarrow) {                      // nothing of an earlier store is read from there any more
+                if (lane == 0) {
+                  if (c < S::kTurns) tma_stores_read<0>();
+                  else tma_stores_read<S::kTurns - 1>();
+                }
+                __syncwarp();
+              }
 #pragma unroll
               for (int i = 0; i < kPieces; ++i) {
                 uint4 v;
 #pragma unroll
                 for (int j = 0; j < kIn; ++j) reinterpret_cast<E*>(&v)[j] = rounded<E>(acc[c * kCols + i * kIn + j]);
-                st_shared16(own + lane * kTurnPitch + 16 * i, v);
+                st_shared16(piece(lane, i), v);
+              }
+              if (by_tma) {
+                fence_async_proxy_smem();
+                __syncwarp();
+                if (lane == 0) tma_store(&a.tm_out, col0 * (int)sizeof(E), row_out, turn_at);
+                continue;
               }
               __syncwarp();
               if (a.wide) {
 #pragma unroll
                 for (int i = 0; i < kPieces; ++i) {
                   const int r = 32 / kPieces * i + lane / kPieces, at_col = lane % kPieces * kIn;
-                  const uint4 v = ld_shared16(own + r * kTurnPitch + lane % kPieces * 16);
+                  const uint4 v = ld_shared16(piece(r, lane % kPieces));
                   if (r < rows && at_col < cols) *reinterpret_cast<uint4*>(out + (size_t)r * a.N + col0 + at_col) = v;
                 }
               } else {
                 // an element a lane, eight rows' at once on their way
-                const E* from = reinterpret_cast<const E*>(turned + warp * kTurnBytes) + lane;
+                const unsigned char* from = turned + (turn_at - smem_u32(turned));
+                constexpr int kLanePieces = 32 / kIn;      // piece (lane / kIn + kLanePieces h) ^ r % 8
+                int own_at[kLanePieces];
+#pragma unroll
+                for (int j = 0; j < kLanePieces; ++j) own_at[j] = 16 * ((lane / kIn) ^ j) + (lane % kIn) * (int)sizeof(E);
                 E* to = out + col0 + lane;
 #pragma unroll 1
-                for (int r = 0; r < rows; r += 8, from += 8 * (kTurnPitch / (int)sizeof(E)), to += 8 * (size_t)a.N) {
+                for (int r = 0; r < rows; r += 8, from += 8 * 128, to += 8 * (size_t)a.N) {
                   E v[8][kCols / 32];
 #pragma unroll
                   for (int i = 0; i < 8; ++i)
 #pragma unroll
-                    for (int h = 0; h < kCols / 32; ++h) v[i][h] = from[i * (kTurnPitch / (int)sizeof(E)) + 32 * h];
+                    for (int h = 0; h < kCols / 32; ++h)
+                      v[i][h] = *reinterpret_cast<const E*>(from + 128 * i + own_at[i % kLanePieces] + 16 * kLanePieces * (h ^ i / kLanePieces));
 #pragma unroll
                   for (int i = 0; i < 8; ++i)
 #pragma unroll
@@ -651,6 +686,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
         }
       }
     }
+    if (kTall && !kSwiglu && kForm != kNarrow && lane == 0) tma_stores_done();
     if (meets && !met) {             // (no tile)
       meet();
       meet();
@@ -823,7 +859,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
 }
 
 // codes as bytes [e][parts][rows][cols], boxes of 128 bytes x box_rows rows x box_parts
-bool encode(CUtensorMap* out, const void* base, int cols, int rows, int parts, int e, int box_rows, int box_parts) {
+bool encode(CUtensorMap* out, const void* base, long long cols, int rows, int parts, int e, int box_rows, int box_parts) {
   const EncodeFn fn = encoder();
   if (!fn) return false;
   const cuuint64_t dims[4] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)parts, (cuuint64_t)e};
@@ -846,6 +882,8 @@ cudaError_t product_launch(Args& a, const void* codes, const void* w_codes, int 
   if (!encode(&a.tm_w, w_codes, K, a.N / parts, parts, a.E, S::kBoxWeights, S::kBoxParts) ||
       !encode(&a.tm_x, codes, K, a.R, 0, 0, S::kBoxRows, 0))
     return cudaErrorInvalidValue;
+  const long long row_bytes = (long long)a.N * (a.dtype == MOE_DTYPE_FP32 ? 4 : 2);
+  a.by_tma = !kSwiglu && (kForm == kTile || kForm == kTilePair) && a.wide && row_bytes < 1ll << 31 && encode(&a.tm_out, a.out, row_bytes, a.R, 0, 0, 32, 0);
   auto* kernel = scaled_product_kernel<kForm, kSwiglu>;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
   if (e != cudaSuccess) return e;

@@ -91,6 +91,28 @@ def test_odd_columns_leave_what_lies_behind_them(N, R):
             assert (space[:shift] == 7).all() and (space[shift + R * N:] == 7).all()
 
 
+@pytest.mark.parametrize("N", [8, 56, 72, 136, 200, 264, 328])
+@pytest.mark.parametrize("per", [100, 400])
+def test_boxes_of_outputs_that_columns_and_rows_end_in(N, per):
+    """Many experts, whose segments end inside a warp's 32 rows, and row lengths that are whole 16-byte pieces but not whole boxes of 128 bytes; rows of no expert behind
+    them."""
+    rng = np.random.default_rng([N, per])
+    E, K, behind = 24, 144, 40
+    offsets = np.concatenate([[0], np.cumsum(per + rng.integers(-33, 34, E))]).astype(np.int32)
+    R = int(offsets[-1])
+    x, w = su.random_rows(R + behind, K, rng), su.random_weights(E, N, K, rng)
+    xg, wg, off = su.on_gpu(*x), su.on_gpu(*w), ru.gpu(offsets)
+    x = x[0][:R], x[1][:R]
+    for dtype, code in ((torch.bfloat16, moe.MOE_DTYPE_BF16), (torch.float16, moe.MOE_DTYPE_FP16), (torch.float32, moe.MOE_DTYPE_FP32)):
+        space = torch.full((8 + (R + behind) * N + 64,), 7.0, dtype=dtype, device="cuda")
+        out = space[8:8 + (R + behind) * N]
+        rc = moe.lib().moe_scaled_product(xg[0].data_ptr(), xg[1].data_ptr(), wg[0].data_ptr(), wg[1].data_ptr(), off.data_ptr(), R + behind, E, N, K, code, out.data_ptr(),
+                                          torch.cuda.current_stream().cuda_stream)
+        assert rc == moe.MOE_OK
+        _check_product(x, w, offsets, dtype, out.view(R + behind, N)[:R])
+        assert (out.view(R + behind, N)[R:] == 0).all() and (space[:8] == 7).all() and (space[8 + (R + behind) * N:] == 7).all()
+
+
 def test_scales_far_apart():
     """Scales over sixty powers of two in one sum."""
     rng = np.random.default_rng(1)

@@ -14,7 +14,7 @@
 // Roles: warps 0-7 epilogue, 8 TMA (one thread; a stage is a block of 128 columns: 128-byte rows, swizzled), 9 MMA (one thread), 10 and 11 bring the products of the two scales, four
 // blocks at a time, into a ring in shared memory.
 // What bounds them: few rows, the weight stream (100 tokens on 128 experts: gate/up 302 us, 6.2 TB/s; one CTA streams 97 GB/s); many, power and the way of a partial from the tensor core to
-// the epilogue and back: 8192 x 4096 x 4096 130-140 us (2.0 PFLOP/s, tensor pipe 53 % of the cycles), 65 536 rows of 64 experts, K 4096, 3584 gate/up rows 1 040-1 110 us, K 1792, 4096
+// the epilogue and back: 8192 x 4096 x 4096 123-142 us (2.0-2.2 PFLOP/s, tensor pipe 55 % of the cycles), 65 536 rows of 64 experts, K 4096, 3584 gate/up rows 1 040-1 110 us, K 1792, 4096
 // columns 545-580, at 1 000 W and 1.46 GHz.  Without loads from TMEM and additions the same launch takes 0.81 of that, without the additions alone 0.84.
 // Every wait is bounded (2 s); where one runs out the launch ends, after another such limit for its copies in flight, and what it has not computed is NaN.
 #include <cuda_fp16.h>

@@ -78,7 +78,7 @@ __device__ __forceinline__ void store4(L* p, const float (&v)[4]) {
   *reinterpret_cast<uint2*>(p) = r;
 }
 
-// The expert of a lane's i-th element.  kVec: rows are aligned to four elements, a lane has four neighbours at a time.
+// The expert of a lane's i-th element.  kVec: rows, and the bias, are aligned to four elements, a lane has four neighbours at a time.
 template <bool kVec>
 __device__ __forceinline__ int expert_of(int i, int lane) { return kVec ? 128 * (i / 4) + 4 * lane + i % 4 : lane + 32 * i; }
 // the row's logits; -inf behind the last expert
@@ -712,7 +712,7 @@ int moe_choose_experts(const void* logits, int64_t logits_stride, int32_t dtype,
   if (misaligned(logits, el) || misaligned(bias, 4) || misaligned(topk_ids, 4) || misaligned(topk_w, 4)) return MOE_EINVAL;
   const ChooseArgs a{logits, bias, logits_stride, n_tokens, n_experts, top_k, n_groups, top_groups, group_sum, scores == MOE_SCORES_SIGMOID,
                      renormalize != 0, scale, topk_ids, topk_w};
-  const bool vec = n_experts % 4 == 0 && logits_stride % 4 == 0 && !misaligned(logits, 4 * el);
+  const bool vec = n_experts % 4 == 0 && logits_stride % 4 == 0 && !misaligned(logits, 4 * el) && !misaligned(bias, 16);
   return launch<Choose>(a, dtype, vec, static_cast<cudaStream_t>(stream)) == cudaSuccess ? MOE_OK : MOE_ECUDA;
 }
 

@@ -326,6 +326,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
       tc_fence_after();
       return lanes + (first + buf) * S::kPartCols;
     };
+    // What a warp waited for in vain it does not give back: others may still read it.
     const auto hand_back = [&] {                                    // the warp has what it loads of the partial
       tc_fence_before();
       __syncwarp();
@@ -356,10 +357,10 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
           for (int b = 0; b < a.blocks && ok; ++b) {
             if (b % kQuad == 0) {
               next_scales();
-              scales_read();
+              if (ok) scales_read();
             }
             next_partial();
-            hand_back();
+            if (ok) hand_back();
           }
           if (S::kQuarter) {
             meet();
@@ -611,7 +612,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
                   }
               }
           }
-          scales_read();
+          if (ok) scales_read();
         }
         const int n = at.n0 + (kSwiglu ? 0 : 128 * half) + 32 * quarter + lane;
         // row r of the tile is this CTA's: the one of the cluster whose turn it is

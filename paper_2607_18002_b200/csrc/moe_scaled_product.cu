@@ -463,8 +463,8 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
             acc[i] = silu_times(acc[i], acc[kOuts + i]);
             top = max(top, __float_as_uint(acc[i]) & 0x7fffffffu);
           }
+          if (!ok) top = 0x7fffffffu;        // (of the whole block, whoever else has its sums: its scale is NaN)
           if constexpr (S::kQuarter) {       // the row's other outputs are with the other half, and with three other CTAs, which are known to run once they have met
-            if (!ok) top = 0x7fffffffu;
             meet();
 #pragma unroll
             for (int to = 0; to < kSplit; ++to) st_cluster_u(map_address(smem_u32(&s.tops[part_of][half][mine]), to), top);
@@ -477,7 +477,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
             bar_sync(1 + quarter, 64);
             top = max(top, s.tops[turn++ & 1][half ^ 1][mine]);
           }
-          const float scale = ok ? scaled_scale(top) : __uint_as_float(0x7fffffffu), inv = __fdividef(1.f, scale);
+          const float scale = scaled_scale(top), inv = __fdividef(1.f, scale);
           if (valid) {
             uint4* to = reinterpret_cast<uint4*>(static_cast<unsigned char*>(a.out) + p * a.I + at.n0 + (S::kQuarter ? 32 * part_of : 0) + kOuts * half);
 #pragma unroll
@@ -657,12 +657,13 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
               const unsigned top = __reduce_max_sync(0xffffffffu, __float_as_uint(acc[i][0][j]) & 0x7fffffffu);
               if (lane == j) mine = top;
             }
+            if (!ok) mine = 0x7fffffffu;
             unsigned* tops = s.tops[turn++ & 1][half];
             if (lane < 16) tops[16 * quarter + lane] = mine;
             bar_sync(1 + half, 128);
 #pragma unroll
             for (int q = 0; q < 4; ++q) mine = max(mine, tops[16 * q + (lane & 15)]);
-            const float scale = ok ? scaled_scale(mine) : __uint_as_float(0x7fffffffu), inv = __fdividef(1.f, scale);
+            const float scale = scaled_scale(mine), inv = __fdividef(1.f, scale);
             const int row = 16 * group(i);
             if (quarter == 0 && lane < 16 && is_mine(row + lane))
               a.out_scales[((size_t)at.row0 + row + lane) * (a.I / kBlock) + at.n0 / kBlock] = scale;

@@ -3,7 +3,7 @@ experts in 4 bits or in e4m3 with block scales (moe_route_grad ... moe_scaled_sw
 
 Checks of arguments and marshalling only; a call enqueues one kernel on `stream` (the current stream of the tensors' device if
 None) and allocates its outputs there.  Nothing is recorded for autograd: gradients are calls of their own.  Wrong types, shapes, strides
-or devices raise ValueError, what the library refuses MoeError.  Inputs may require gradients (experts' outputs of a graph of the caller's own do); results never do.
+or devices and sizes past 32 bits raise ValueError, what the library refuses MoeError.  Inputs may require gradients (experts' outputs of a graph of the caller's own do); results never do.
 As with any work on another stream, inputs have to live until `stream` has read them, and `stream` has to be waited for before results are used elsewhere.
 A permutation is the pair (sorted_to_flat, flat_to_sorted) of a plan, int32 [T*k] each, the inverses of one another: of moe_plan (a Context's), of moe_plan_static
 (up to 32 768 rows and 256 experts, no context) or, for any size and without either, by a stable sort of the expert ids:
@@ -52,6 +52,11 @@ def _refuse(what):
     raise ValueError(what)
 
 
+def _past_32_bits(*numbers):
+    """Whether one of them is no number of 32 bits with a sign, which the library takes (ctypes would cut it off); each for itself: a negative one hides no others."""
+    return any((n + 0x80000000) >> 32 for n in numbers)
+
+
 def _rows(t, name, dtypes):
     """[n, H] with neighbouring columns -> n, H, elements from a row to the next."""
     if not isinstance(t, _Tensor) or t.dtype not in dtypes or not t.is_cuda or t.dim() != 2:
@@ -60,6 +65,8 @@ def _rows(t, name, dtypes):
     step, one = t.stride()
     if h < 1 or (one != 1 and h > 1) or (n > 1 and step < h):
         _refuse(f"{name}: the columns of a row must be neighbours and rows must not overlap")
+    if (n | h) >> 31:
+        _refuse(f"{name}: there must be fewer than 2^31 rows and columns")
     return n, h, step if step > h else h
 
 
@@ -71,8 +78,8 @@ def _plain(t, name, dtype, shape, gpu):
 
 def _index(t, name, n, gpu):
     if not isinstance(t, _Tensor) or t.dtype is not _I32 or t.get_device() != gpu or not t.is_contiguous() \
-            or t.numel() != n and (n or t.numel() != 1):                # (a plan without rows has arrays of one entry)
-        _refuse(f"{name} must be a contiguous int32 tensor of {n} on cuda:{gpu}")
+            or t.numel() != n and (n or t.numel() != 1) or n >> 31:     # (a plan without rows has arrays of one entry)
+        _refuse(f"{name} must be a contiguous int32 tensor of {n} (fewer than 2^31) on cuda:{gpu}")
 
 
 def _elsewhere(call, device, stream, *args):
@@ -176,6 +183,8 @@ def route_grad(topk_ids, topk_w, d_topk_w, n_experts: int, stream=None):
     _plain(topk_w, "topk_w", _FP32, shape, gpu)
     _plain(d_topk_w, "d_topk_w", _FP32, shape, gpu)
     T, k = shape
+    if (T | k | n_experts) >> 31 and _past_32_bits(T, k, n_experts):
+        _refuse("the tokens, slots and experts must be below 2^31")
     dz = topk_w.new_empty(T, n_experts)
     rc = (moe._lib or moe.lib()).moe_route_grad(topk_ids.data_ptr(), topk_w.data_ptr(), d_topk_w.data_ptr(), T, n_experts, k, dz.data_ptr(),
                                                 _stream(gpu))
@@ -234,6 +243,8 @@ def mx_dequantize(codes, scales, dtype=_BF16, stream=None):
     K = 2 * half
     if stream is not None or gpu != _current_device():
         return _elsewhere(mx_dequantize, codes.device, stream, codes, scales, dtype)
+    if K >> 31:
+        _refuse("there must be fewer than 2^31 columns")
     out = _empty(*lead, K, dtype=dtype, device=codes.device)
     if K:
         rc = (moe._lib or moe.lib()).moe_mx_dequantize(codes.data_ptr(), scales.data_ptr(), out.numel() // K, K, _DTYPES[dtype], out.data_ptr(),
@@ -249,6 +260,8 @@ def _operands(codes, scales, w_codes, w_scales, offsets):
     (E, n, w_half), w_gpu = _codes(w_codes, w_scales, "the weights", 3)
     if w_half != half or w_gpu != gpu:
         _refuse(f"the weights must have {2 * half} columns and be on cuda:{gpu}, as the rows")
+    if (R | E | n | 2 * half) >> 31:
+        _refuse("the rows, experts and columns must be below 2^31")
     _index(offsets, "offsets", E + 1, gpu)
     return gpu, R, E, n, 2 * half
 
@@ -298,8 +311,8 @@ def choose_experts(logits, top_k: int, *, scores: str = "softmax", bias=None, gr
         _refuse(f"scores must be one of {sorted(_SCORES)}")
     if bias is not None:
         _plain(bias, "bias", _FP32, (E,), gpu)
-    if (T | top_k | groups | top_groups | group_sum) >> 31 > 0:
-        _refuse("the tokens, top_k and groups must be below 2^31")
+    if (top_k | groups | top_groups | group_sum) >> 31 and _past_32_bits(top_k, groups, top_groups, group_sum):      # (a negative one, or one past 32 bits)
+        _refuse("top_k and the groups must be below 2^31")
     k = top_k if top_k > 0 else 0               # (the library refuses what is not)
     device = logits.device
     ids, w = _empty(T, k, dtype=_I32, device=device), _empty(T, k, dtype=_FP32, device=device)
@@ -325,8 +338,8 @@ def choose_experts_grad(logits, topk_ids, d_topk_w, *, scores: str = "softmax", 
     k = topk_ids.shape[1]
     _plain(topk_ids, "topk_ids", _I32, (T, k), gpu)
     _plain(d_topk_w, "d_topk_w", _FP32, (T, k), gpu)
-    if T >> 31:
-        _refuse("there must be fewer than 2^31 tokens")
+    if k >> 31:
+        _refuse("there must be fewer than 2^31 slots")
     dz = logits.new_empty(T, E)
     rc = (moe._lib or moe.lib()).moe_choose_experts_grad(logits.data_ptr(), step, _DTYPES[logits.dtype], topk_ids.data_ptr(), d_topk_w.data_ptr(), T, E, k,
                                                          _SCORES[scores], renormalize, scale, dz.data_ptr(), _stream(gpu))
@@ -379,6 +392,8 @@ def scaled_quantize_weights(w, stream=None):
     *lead, n, K = w.shape
     if K % 16 or not K or not n:
         _refuse("w must have rows, and a multiple of 16 columns")
+    if (w.shape[0] | n | K) >> 31:
+        _refuse("the experts, rows and columns must be below 2^31")
     codes = _empty(w.shape, dtype=_F8, device=w.device)
     scales = _empty(*lead, _blocks(n), _blocks(K), dtype=_FP32, device=w.device)
     rc = (moe._lib or moe.lib()).moe_scaled_quantize_weights(w.data_ptr(), _DTYPES[w.dtype], lead[0] if lead else 1, n, K, codes.data_ptr(),
@@ -412,11 +427,13 @@ def scaled_dequantize(codes, scales, dtype=_BF16, stream=None):
     shape, gpu = _scaled(codes, scales, "the values", per_row)
     if stream is not None or gpu != _current_device():
         return _elsewhere(scaled_dequantize, codes.device, stream, codes, scales, dtype)
+    values, n, K = codes.numel(), shape[-2], shape[-1]
+    E = values // (n * K) if values else 0
+    if (E | n | K) >> 31:
+        _refuse("the matrices, rows and columns must be below 2^31")
     out = _empty(*shape, dtype=dtype, device=codes.device)
-    values = out.numel()
     if values:
-        n, K = shape[-2], shape[-1]
-        rc = (moe._lib or moe.lib()).moe_scaled_dequantize(codes.data_ptr(), scales.data_ptr(), values // (n * K), n, K, 1 if per_row else 128,
+        rc = (moe._lib or moe.lib()).moe_scaled_dequantize(codes.data_ptr(), scales.data_ptr(), E, n, K, 1 if per_row else 128,
                                                            _DTYPES[dtype], out.data_ptr(), _stream(gpu))
         if rc:
             _failed(rc, "moe_scaled_dequantize")
@@ -430,14 +447,16 @@ def _scaled_operands(codes, scales, w_codes, w_scales, offsets):
     dims = len(w_shape)
     if len(shape) != 2 or dims > 3 or w_shape[dims - 1] != shape[1] or w_gpu != gpu:
         _refuse(f"rows must be [R, K] and weights [E, n, K] or [n, K], all on cuda:{gpu}")
-    E = w_shape[0] if dims == 3 else 1
+    E, n = w_shape[0] if dims == 3 else 1, w_shape[dims - 2]
+    if (shape[0] | shape[1] | E | n) >> 31:
+        _refuse("the rows, experts and columns must be below 2^31")
     at = None
     if offsets is not None:
         _index(offsets, "offsets", E + 1, gpu)
         at = offsets.data_ptr()
     elif E != 1:
         _refuse("more than one matrix needs offsets")
-    return gpu, shape[0], E, w_shape[dims - 2], shape[1], at
+    return gpu, shape[0], E, n, shape[1], at
 
 
 def scaled_product(codes, scales, w_codes, w_scales, offsets=None, dtype=_BF16, stream=None):

@@ -66,7 +66,7 @@ struct Shape {
   static constexpr int kParts = kForm == kNarrow || !kTall ? 4 : 2; // of a half
   static constexpr int kScaleFloats = kQuad * 2 * kMine;            // of a place in the ring: [block][half][row]
   static constexpr int kScaleBytes = kQuads * kScaleFloats * 4;
-  static constexpr int kTurns = kForm == kTilePair ? 2 : 1;         // ... of a warp (pairs: four stages are left; one, and five: 599 -> 611 us)
+  static constexpr int kTurns = kForm == kTilePair ? 2 : 1;         // ... of a warp (pairs: four stages are left; one, and five: 588 -> 598 us)
   static constexpr int kOutBytes = kTall && !kSwiglu ? 8 * kTurns * kTurnBytes : 0;
   static constexpr int kStages = (227 * 1024 - 1024 - (int)sizeof(Shared) - kScaleBytes - kOutBytes) / kStageBytes;
   static constexpr int kSmem = 1024 + kStages * kStageBytes + kScaleBytes + kOutBytes + (int)sizeof(Shared);
@@ -508,9 +508,10 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
               if (cols <= 0) break;                        // (so that every pass so far has had its store, which the waits count)
               const unsigned turn_at = own + c % S::kTurns * kTurnBytes;
               const auto piece = [&](int r, int i) { return turn_at + 128 * r + 16 * (i ^ (r & 7)); };
-              if (kForm != kNarrow) {                      // nothing of an earlier store is read from there any more
+              // Nothing of an earlier store is read from there any more: of the tile before all of them, which frees every place; then the one whose place comes again.
+              if (kForm != kNarrow && (c == 0 || c >= S::kTurns)) {
                 if (lane == 0) {
-                  if (c < S::kTurns) tma_stores_read<0>();
+                  if (c == 0) tma_stores_read<0>();
                   else tma_stores_read<S::kTurns - 1>();
                 }
                 __syncwarp();

@@ -179,25 +179,15 @@ __device__ __forceinline__ bool try_at(unsigned saddr, unsigned parity) {
   return ok != 0;
 }
 // whether the phase is over; the answer is not waited for before it is used
-template <bool kRelaxed = false>
 __device__ __forceinline__ bool test_at(unsigned saddr, unsigned parity) {
   unsigned ok;
-  if (kRelaxed)
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.test_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(saddr), "r"(parity)
-        : "memory");
-  else
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(saddr), "r"(parity)
-        : "memory");
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(saddr), "r"(parity)
+      : "memory");
   return ok != 0;
 }
 // 128 bytes of 32 rows out of shared memory; the thread that asks is the one that waits
@@ -755,7 +745,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
           else tc_commit(bar);
         };
         // Small tiles: the barriers of the next block are asked while this one's products are issued, and the answers read when their turn has come; waiting for each in its place takes
-        // some hundred clocks a barrier (16 rows of 4096 x 4096 14.7 us for 11.5).  Where the next buffer is never back that early, asking costs 2-3 %.
+        // some hundred clocks a barrier (16 rows of 4096 x 4096 14.7 us for 11.5).  Where the next buffer is never back that early, asking costs 2-3 %.  (Single CTAs alone.)
         // (A pair's hand-backs are relaxed arrivals: what they order, the tcgen05 fences on both sides do.)
         const auto hand_back_of = [&](unsigned n, int h) { return smem_u32(&s.part_empty[n % S::kParts + S::kParts * h]); };
         constexpr bool kAsk = kForm == kNarrow;
@@ -777,7 +767,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
               if (!ok) break;
               tc_fence_after();
               if (kAsk && h == 0) full = test_at(smem_u32(&s.full[next_slot]), next_parity);
-              if (kAsk) empty[h] = n + 1 >= S::kParts && test_at<kPair>(hand_back_of(n + 1, h), ((n + 1) / S::kParts - 1) & 1);
+              if (kAsk) empty[h] = n + 1 >= S::kParts && test_at(hand_back_of(n + 1, h), ((n + 1) / S::kParts - 1) & 1);
               const unsigned d = tmem + (buf + S::kParts * h) * S::kPartCols;
               if (kTall) {
                 mma_block<kPair>(d, umma_desc(st + S::kWBytes, 128), umma_desc(st + h * (S::kWBytes / 2), 128), idesc);

@@ -269,7 +269,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_product_kernel(const __grid_
         tc_wait_ld();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) {
+        if (lane == 0 && ok) {   // (what was waited for in vain others may still read)
           if (kPair) mbar_arrive_cluster(map_to_cta(&s.acc_empty[buf], 0));
           else mbar_arrive(&s.acc_empty[buf]);
         }

@@ -368,15 +368,15 @@ int moe_mx_swiglu(const void* codes, const void* scales, const void* w_codes, co
 
 /* Rows in e4m3 with a scale per 128 columns, weights in e4m3 with a scale per 128 x 128: the form of a context's e4m3 operands, for experts of the caller's own.
  * A value is code * scale.  [rows, cols] rows have codes [rows, cols] and fp32 scales [rows, ceil(cols/128)]; matrices [E, n, cols] have scales
- * [E, ceil(n/128), ceil(cols/128)]; blocks at the edges are smaller.  The scale of a block is amax * (1 / 448) (both operations in fp32), 1 for a block of
- * zeros, 2^-126 at least; a code is the e4m3 value nearest to the exact quotient, ties to the even code.  A block that holds NaN or infinity
+ * [E, ceil(n/128), ceil(cols/128)]; blocks at the edges are smaller.  The scale of a block is amax * (1 / 448) (both operations in fp32; a context's own re-quantisation
+ * divides amax by 448, which may differ in the last bit), 1 for a block of zeros, 2^-126 at least; a code is the e4m3 value nearest to the exact quotient, ties to the even code.  A block that holds NaN or infinity
  * has a NaN scale: all of it is NaN (its codes say nothing).  cols: a multiple of 16, at most 2^30;
  * weights and dequantised values: 2^40 at most.
  *
  * moe_scaled_quantize: x [T, cols] (BF16, FP16 or FP32) -> codes and scales, sorted by expert as by moe_mx_quantize where a permutation is given (zero
  * codes and scales of 1 where a row belongs to no token), row by row with both NULL (top_k = 1).  codes 16-byte aligned.
  * moe_scaled_quantize_weights: w [E, n, cols], contiguous.  codes and w 16-byte aligned.
- * moe_scaled_dequantize: the values [E, n, cols] that codes and scales stand for, rounded to dtype; scale_rows 1 (scales [E, n, .]; E * n rows) or 128.
+ * moe_scaled_dequantize: the values [E, n, cols] that codes and scales stand for, code * scale in fp32 and that rounded to dtype; scale_rows 1 (scales [E, n, .]; E * n rows) or 128.
  * codes and values 16-byte aligned. */
 int moe_scaled_quantize(const void* x, int64_t x_stride, int32_t dtype, int32_t n_tokens, int32_t top_k, int32_t cols,
                         const int32_t* sorted_to_flat, const int32_t* flat_to_sorted, void* codes, float* scales, void* stream);
@@ -387,7 +387,8 @@ int moe_scaled_dequantize(const void* codes, const float* scales, int32_t n_expe
 
 /* Sorted e4m3 rows times the experts' e4m3 matrices: rows [R, K], weights [E, n, K], offsets [E+1] as for moe_mx_product; offsets NULL: one
  * matrix (n_experts = 1) for all rows.
- *   moe_scaled_product  out[p, :] = rows[p, :] . w[e]^T, rounded once to dtype (BF16, FP16 or FP32)
+ *   moe_scaled_product  out[p, :] = rows[p, :] . w[e]^T, rounded once to dtype (BF16, FP16 or FP32: experts' outputs that are merged in fp32 keep what a 16-bit type loses,
+ *                       a layer's result is then off by 1.7e-3 of its norm instead of 2.3e-3)
  *   moe_scaled_swiglu   weights [E, 2*inter, K], gate rows first: silu(gate) * up, computed in fp32 and quantised as by moe_scaled_quantize (codes: of a
  *                       quotient that is off by some steps of fp32; 0 for gates below -87.3): codes [R, inter], scales [R, inter/128], the rows of the down product
  * The products of a block of 128 columns are added up in the tensor core, the blocks with their scales in fp32. (Products of a row's and a weight's scale must be

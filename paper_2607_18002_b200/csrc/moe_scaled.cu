@@ -252,7 +252,7 @@ dequantize_kernel(const unsigned char* __restrict__ codes, const float* __restri
       unsigned h;                                  // e4m3 values are exact in fp16
       asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(two));
       const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-      v[q] = rounded<E>(f.x * scale[m]);
+      v[q] = rounded<E>(f.x * scale[m]);           // (fp32 first: 28 bits of a code and a scale; 16-bit types are rounded from that)
       v[q + 1] = rounded<E>(f.y * scale[m]);
     }
     out[i] = raw;

@@ -2,7 +2,7 @@
 //
 // The scale of a block is amax times the fp32 number nearest to 1/448 (448: the largest e4m3 value), rounded once, 1 for a block of zeros, 2^-126 at least (a
 // normal number, so that its reciprocal is one too).  That it is this product, and not the nearest number to amax / 448, counts: of 16-bit values one in some hundred is as far
-// from two codes for a scale of amax / 448, and the last bit of the scale says which it gets.  A block that holds a NaN or an infinity has a NaN scale, which makes all of its values NaN.
+// from two codes for a scale of amax / 448, and the last bit of the scale says which it gets.  (The re-quantisation inside moe_run divides: there the code is a product with 448 / amax.)  A block that holds a NaN or an infinity has a NaN scale, which makes all of its values NaN.
 #pragma once
 #include <stdint.h>
 

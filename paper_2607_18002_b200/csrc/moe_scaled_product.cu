@@ -14,9 +14,10 @@
 // Roles: warps 0-7 epilogue, 8 TMA (one thread; a stage is a block of 128 columns: 128-byte rows, swizzled), 9 MMA (one thread), 10 and 11 bring the products of the two scales, four
 // blocks at a time, into a ring in shared memory.
 // What bounds them: few rows, the weight stream (100 tokens on 128 experts: gate/up 302 us, 6.2 TB/s; one CTA streams 97 GB/s); many, power and the way of a partial from the tensor core to
-// the epilogue and back: 8192 x 4096 x 4096 123-142 us (2.0-2.2 PFLOP/s, tensor pipe 55 % of the cycles), 65 536 rows of 64 experts, K 4096, 3584 gate/up rows 1 040-1 110 us, K 1792, 4096
-// columns 545-580, at 1 000 W and 1.46 GHz.  Without loads from TMEM and additions the same launch takes 0.81 of that, without the additions alone 0.84.
-// Every wait is bounded (2 s); where one runs out the launch ends, after another such limit for its copies in flight, and what it has not computed is NaN.
+// the epilogue and back: 8192 x 4096 x 4096 by itself 130-135 us (2.0-2.1 PFLOP/s, tensor pipe 55 % of the cycles), over and over 143-147 (1.9), 65 536 rows of 64 experts, K 4096, 3584 gate/up rows
+// 1 070-1 190 us, K 1792, 4096 columns 580-590, at 1 000 W and 1.46 GHz.  Without loads from TMEM and additions the same launch takes 0.81 of that, without the additions alone 0.84.
+// Every wait is bounded (2 s); where one runs out the launch ends, after another such limit for its copies in flight, and what it has not computed is NaN (a scale of NaN).  A warp that gave
+// up hands nothing back, so that what others still read stays as it is.
 #include <cuda_fp16.h>
 
 #include <type_traits>
@@ -483,7 +484,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_product_kernel(const __gri
             for (int i = 0; i < S::kHalfCols; ++i) acc[i] = __uint_as_float(0x7fffffffu);
           }
           // A warp turns its 32 rows round in shared memory, 128 bytes of each at a time.  Where all 32 are the tile's, TMA takes them from there while the next tile's
-          // sums begin (down product of 65 536 rows, K 1792, over and over 599 -> 577 us); else the warp stores 128 bytes of four rows at a time.
+          // sums begin (down product of 65 536 rows, K 1792, over and over 587 us; all stored by the warps 615); else the warp stores 128 bytes of four rows at a time.
           const unsigned own = smem_u32(turned + warp * S::kTurns * kTurnBytes);
           const int row_out = at.row0 + 128 * (int)rank + 32 * quarter, rows = min(32, at.rows - 128 * (int)rank - 32 * quarter);
           const bool by_tma = kForm != kNarrow && a.by_tma && rows == 32;

@@ -19,7 +19,7 @@ A permutation is the pair (sorted_to_flat, flat_to_sorted) of a plan, int32 [T*k
 
     codes, scales = scaled_quantize(x, s2f, f2s, k)                      # ... in e4m3, weights from scaled_quantize_weights or a context's
     codes, scales = scaled_swiglu(codes, scales, w1_codes, w1_scales, offsets)
-    rows = scaled_product(codes, scales, w2_codes, w2_scales, offsets)
+    rows = scaled_product(codes, scales, w2_codes, w2_scales, offsets)   # bf16; dtype=torch.float32 where outputs are not to be rounded before they are merged
     y = merge_rows(rows, f2s, topk_w)
     rows = scaled_product(codes, scales, w_codes, w_scales)              # one matrix [n, K] for all rows: a shared expert, a projection
 
